@@ -401,6 +401,129 @@ int fnpu_mla_expand(const fnpu_attn_desc *desc, const void *latent_cache, const 
                     const void *w_uk, const void *w_uv, void *workspace, void *k_out, void *v_out,
                     void *stream);
 
+/*
+ * Rotary positions on one to four axes (time, height, width; one for text).
+ * Pair i of a row's rotary_dim / 2 pairs turns by the angle
+ *   positions[pair_axis[i]][t] * inv_freq[i]:
+ *   y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin
+ * in fp32, rounded once. Pairs are columns (rotary_offset + i, rotary_offset +
+ * rotary_dim / 2 + i), or with interleaved = 1 (rotary_offset + 2 i, + 2 i + 1); the
+ * other columns are copied. inverse = 1 turns by the negative angle, which is also
+ * the gradient: dx is the inverse of dy. Angles are good to about 1e-6 rad below
+ * position 2^20 (the product is not rounded to fp32); any int32 position is valid.
+ */
+typedef struct {
+    int32_t rotary_dim;        /* columns that turn: even, 2..256 */
+    int32_t rotary_offset;     /* the first of them */
+    int32_t interleaved;       /* 0: halves, 1: neighbouring columns */
+    int32_t inverse;           /* 1: turn back */
+    int32_t num_axes;          /* 1..4 */
+    const uint8_t *pair_axis;  /* host [rotary_dim / 2], each < num_axes, read by the call;
+                                  may be NULL with one axis */
+} fnpu_rope_desc;
+
+/*
+ * Rotate packed rows: x and out are device bf16 [num_tokens, num_heads, head_dim]
+ * with x_stride and out_stride elements between tokens (>= num_heads * head_dim;
+ * the slice of a fused projection's output, for instance). out may be x with the
+ * same stride (in place), and otherwise must not overlap it.
+ *   inv_freq   device fp32 [rotary_dim / 2], 16-byte aligned
+ *   positions  device int32 [num_axes, num_tokens]
+ * Rows whose rotary_dim is a multiple of 16 and whose offset, head_dim and strides
+ * are multiples of 8, 16-byte aligned, are read and written in 16-byte chunks;
+ * others a pair at a time.
+ * Errors: FNPU_EINVAL for NULL or misaligned pointers, a descriptor outside the
+ * ranges above or head_dim, a stride below a row, negative num_tokens;
+ * FNPU_EUNSUPPORTED for rotary_dim > 256; FNPU_ECUDA.
+ */
+int fnpu_rope(const fnpu_rope_desc *rope, const float *inv_freq, const int32_t *positions, const void *x,
+              int64_t x_stride, int32_t num_heads, int32_t head_dim, int32_t num_tokens, void *out,
+              int64_t out_stride, void *stream);
+
+/*
+ * Cache formats of the calls below. FNPU_KV_BF16 is the bf16 cache of
+ * fnpu_attn_desc (kv_fp8 = 0 in all of them). The two 8-bit formats keep one scale,
+ * a power of two 2^e, for each block and kv head -- less to read and store than a
+ * scale a row (the kv_fp8 format), every head layout, and stored values that are
+ * exact in bf16:
+ *   a block of k_cache or v_cache (fnpu_kv8_block_bytes bytes, 16-byte aligned):
+ *     codes, bytes [Hkv][block_size][d]; then fp32 scales [Hkv], padded to 16 bytes
+ *   FNPU_KV_INT8_BLOCK  value (code - 128) * 2^e, codes 1..255
+ *   FNPU_KV_E4M3_BLOCK  e4m3 value of the code * 2^e
+ * Split K/V with d_qk = d_v in {64, 128}, block_size 16, 32 or 64, any Hkv, Hq / Hkv
+ * up to 128 (FNPU_EUNSUPPORTED otherwise).
+ * A block's exponent is the least e with |x| <= 127 * 2^e (448 * 2^e) for every
+ * value stored in it, within [-60, 60], and codes are nearest (ties to even). An
+ * append to a block that holds rows already (its first slot is not among the
+ * appended) keeps the larger of the exponent so far and the one that the new rows
+ * need; where it grows, the rows before are stored anew from their stored values.
+ * An append of a block's first slot starts the block afresh, whatever it held.
+ * NaN is stored as zero and an infinity as the largest magnitude; they, and finite
+ * magnitudes above the largest at e = 60 (which saturate), raise the library-wide
+ * device flag (FNPU_EDEVICE_RANGE from fnpu_check).
+ */
+#define FNPU_KV_BF16 0
+#define FNPU_KV_INT8_BLOCK 1
+#define FNPU_KV_E4M3_BLOCK 2
+
+/* Bytes of one block of k_cache, and of v_cache, in an 8-bit block format. */
+int fnpu_kv8_block_bytes(const fnpu_attn_desc *desc, int32_t kv_format, int64_t *bytes);
+
+/*
+ * Append with the rotation on the way: the step's query rows are rotated into
+ * q_out, its key rows are rotated into their cache slots and its value rows stored
+ * in theirs, in one launch; keys in an 8-bit cache are rounded once, from the
+ * fp32 rotation.
+ *   rope, inv_freq, positions  as for fnpu_rope, over d_qk columns (the latent cache:
+ *               the rotated columns of a row, rotary_offset = 512 of 576); rotary_dim
+ *               a multiple of 16, rotary_offset of 8 (8-bit formats: 16). rope
+ *               NULL: rows are stored as they are (q must be NULL)
+ *   q, k_new, v_new  device bf16 [num_tokens, heads, d] with q_stride, k_stride,
+ *               v_stride elements between tokens (multiples of 8); q NULL: no queries;
+ *               v_new NULL for a latent cache
+ *   q_out       device bf16 [num_tokens, Hq, d_qk]; may be q where q_stride = Hq * d_qk
+ *   slot_mapping, k_cache, v_cache  as for fnpu_kv_append. The 8-bit formats take
+ *               a block's rows together: the tokens that a call stores in one block
+ *               must be consecutive tokens at consecutive slots (as the tokens of a
+ *               sequence are, in order); otherwise that block is undefined
+ * Errors: FNPU_EINVAL for NULL or misaligned pointers (16 bytes; slots 8), bad
+ * strides, shapes or formats; FNPU_EUNSUPPORTED for kv_fp8 = 1 (fnpu_rope, then
+ * fnpu_kv_append), other rotary widths, and strided rows of a bf16 cache without a
+ * rotation; FNPU_ECUDA. Slots out of range as for fnpu_kv_append.
+ */
+int fnpu_rope_append(const fnpu_attn_desc *desc, int32_t kv_format, const fnpu_rope_desc *rope, const float *inv_freq,
+                     const int32_t *positions, const void *q, int64_t q_stride, const void *k_new, int64_t k_stride,
+                     const void *v_new, int64_t v_stride, const int64_t *slot_mapping, int32_t num_tokens,
+                     void *q_out, void *k_cache, void *v_cache, void *stream);
+
+/*
+ * Read cached rows back as bf16, exactly: row i of k_out [n, Hkv, d_qk] and v_out
+ * [n, Hkv, d_v] (16-byte aligned; v_out NULL for a latent cache) is what slot
+ * slots[i] stores; a negative slot gives a zero row, one past the pool a zero row
+ * and the device flag (FNPU_EDEVICE_RANGE). For moving a cache to another format
+ * or another worker.
+ * Errors: as fnpu_rope_append (kv_fp8 = 1: FNPU_EUNSUPPORTED).
+ */
+int fnpu_kv_read(const fnpu_attn_desc *desc, int32_t kv_format, const int64_t *slots, int32_t n, const void *k_cache,
+                 const void *v_cache, void *k_out, void *v_out, void *stream);
+
+/*
+ * A plan over an 8-bit block cache (kv_format FNPU_KV_INT8_BLOCK or
+ * FNPU_KV_E4M3_BLOCK): arguments as for fnpu_mixed_attn_plan_ex, and the plan is
+ * used like any other -- fnpu_mixed_attn_replan, _run (k_cache and v_cache are the
+ * byte pools), fnpu_mixed_step (whose append stores the rows unrotated),
+ * fnpu_plan_check, _info, _destroy. Sequences with at most 64 rows a kv head
+ * (query_len x Hq / Hkv: one-token decodes, speculative verification, short
+ * chunks) attend over the codes directly, of either phase; longer chunks over a
+ * bf16 copy of their blocks that each run makes in the plan's workspace.
+ * Errors: as fnpu_mixed_attn_plan_ex; FNPU_EINVAL for another kv_format;
+ * FNPU_EUNSUPPORTED for shapes that the formats do not take and for
+ * FNPU_PLAN_NO_TCGEN05.
+ */
+int fnpu_kv8_attn_plan(const fnpu_attn_desc *desc, int32_t kv_format, int32_t num_seqs, const int32_t *query_len,
+                       const int32_t *context_len, const uint8_t *phase, const int32_t *block_table,
+                       int32_t block_table_stride, const fnpu_plan_opts *opts, void *stream, fnpu_plan **out);
+
 #ifdef __cplusplus
 }
 #endif

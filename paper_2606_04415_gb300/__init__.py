@@ -8,6 +8,10 @@ kernels. Functions carry the C names without the ``fnpu_`` prefix:
     mixed_attn_plan(desc, query_len, context_len, phase, block_table, opts=None, stream=None)
     mixed_attn_replan(plan, query_len, context_len, phase, block_table, opts=None, stream=None)
     mixed_attn_run(plan, q, k_cache, v_cache, out, lse, stream=None)
+    rope(desc, inv_freq, positions, x, out=None, stream=None)
+    rope_append(desc, rope, inv_freq, positions, q, k_new, v_new, slot_mapping, q_out, k_cache, v_cache, kv_format=0)
+    kv_read(desc, slots, k_cache, v_cache, k_out, v_out, kv_format=0)
+    kv8_attn_plan(desc, kv_format, query_len, context_len, phase, block_table, opts=None, stream=None)
     check(stream=None), plan_check(plan, stream=None), status_str(code)
 
 Device arguments are CUDA torch tensors (torch supplies device memory and
@@ -38,12 +42,18 @@ PLAN_NO_TCGEN05 = 2
 PLAN_GREEN_CONTEXTS = 4
 PLAN_FUSED_APPEND = 8
 
+# cache formats of rope_append, kv_read and kv8_attn_plan
+KV_BF16 = 0
+KV_INT8_BLOCK = 1
+KV_E4M3_BLOCK = 2
+
 EXPORTED = (
     "fnpu_kv_append", "fnpu_mixed_attn_plan", "fnpu_mixed_attn_plan_ex", "fnpu_mixed_attn_run",
     "fnpu_plan_check", "fnpu_check", "fnpu_plan_destroy", "fnpu_plan_info", "fnpu_status_str",
     "fnpu_version", "fnpu_decode_attn_noalloc", "fnpu_last_cuda_error", "fnpu_plan_phase_ms",
     "fnpu_dispatch_next_share", "fnpu_mla_expand", "fnpu_mixed_attn_replan",
-    "fnpu_plan_decode_share", "fnpu_mixed_step",
+    "fnpu_plan_decode_share", "fnpu_mixed_step", "fnpu_rope", "fnpu_rope_append", "fnpu_kv_read",
+    "fnpu_kv8_block_bytes", "fnpu_kv8_attn_plan",
 )
 
 
@@ -67,6 +77,12 @@ class AttnDesc(ctypes.Structure):
 class PlanOpts(ctypes.Structure):
     _fields_ = [("decode_split_keys", ctypes.c_int32), ("decode_share_pct", ctypes.c_int32),
                 ("num_sms", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("rotary_offset", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("num_axes", ctypes.c_int32), ("pair_axis", ctypes.c_void_p)]
 
 
 _lib = None
@@ -112,6 +128,15 @@ def load(build_if_missing: bool = True):
     lib.fnpu_plan_phase_ms.argtypes = [P, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_float)]
     lib.fnpu_dispatch_next_share.argtypes = [i32, ctypes.c_float, ctypes.c_float, ctypes.c_float,
                                              ctypes.POINTER(i32)]
+    RP, i64p = ctypes.POINTER(RopeDesc), ctypes.POINTER(i64)
+    lib.fnpu_rope.argtypes = [RP, P, P, P, i64, i32, i32, i32, P, i64, P]
+    lib.fnpu_rope_append.argtypes = [ctypes.POINTER(AttnDesc), i32, RP, P, P, P, i64, P, i64, P, i64, P, i32, P, P, P, P]
+    lib.fnpu_kv_read.argtypes = [ctypes.POINTER(AttnDesc), i32, P, i32, P, P, P, P, P]
+    lib.fnpu_kv8_block_bytes.argtypes = [ctypes.POINTER(AttnDesc), i32, i64p]
+    lib.fnpu_kv8_attn_plan.argtypes = [ctypes.POINTER(AttnDesc), i32, i32, P, P, P, P, i32, ctypes.POINTER(PlanOpts), P,
+                                       ctypes.POINTER(P)]
+    for name in ("fnpu_rope", "fnpu_rope_append", "fnpu_kv_read", "fnpu_kv8_block_bytes", "fnpu_kv8_attn_plan"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("fnpu_kv_append", "fnpu_mixed_attn_plan", "fnpu_mixed_attn_plan_ex",
                  "fnpu_mixed_attn_run", "fnpu_plan_check", "fnpu_check", "fnpu_plan_info",
                  "fnpu_version", "fnpu_decode_attn_noalloc", "fnpu_plan_phase_ms",
@@ -351,3 +376,110 @@ def dispatch_next_share(share_pct: int, prefill_ms: float, decode_ms: float, tol
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_dispatch_next_share")
     return out.value
+
+
+def make_rope(rotary_dim: int, rotary_offset: int = 0, interleaved: bool = False, inverse: bool = False, num_axes: int = 1,
+              pair_axis=None) -> RopeDesc:
+    """Descriptor of a rotation (``fnpu_rope_desc``); ``pair_axis``: the axis
+    of each of the rotary_dim / 2 pairs (all 0 by default)."""
+    axis = None if pair_axis is None else _np(pair_axis, np.uint8).copy()
+    if axis is not None and axis.shape != (rotary_dim // 2,):
+        raise ValueError("pair_axis has an entry for each of the rotary_dim / 2 pairs")
+    d = RopeDesc(int(rotary_dim), int(rotary_offset), int(bool(interleaved)), int(bool(inverse)), int(num_axes),
+                 None if axis is None else axis.ctypes.data)
+    d._axis = axis  # (the descriptor holds its address)
+    return d
+
+
+_dtypes = None  # (rows, positions, frequencies): torch's dtypes, looked up once
+
+
+def _types():
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = (torch.bfloat16, torch.int32, torch.float32)
+    return _dtypes
+
+
+def _rows(x):
+    """Address and token stride of bf16 rows [n, heads, d] whose tokens may lie
+    apart (a slice of a fused projection's output)."""
+    if not x.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if x.dtype is not _types()[0]:
+        raise TypeError("rows are bf16")
+    n, h, d = x.shape
+    s, t, u = x.stride()
+    if (u != 1 and d > 1) or (t != d and h > 1):
+        raise ValueError("the heads and columns of a token must be contiguous")
+    return x.data_ptr(), s if n > 1 else max(s, h * d)
+
+
+def _check_positions(desc: RopeDesc, inv_freq, positions, n: int) -> None:
+    if inv_freq.numel() != desc.rotary_dim >> 1 or positions.numel() != desc.num_axes * n:
+        raise ValueError("inv_freq is [rotary_dim / 2] and positions are [num_axes, tokens]")
+    if inv_freq.dtype is not _types()[2] or positions.dtype is not _types()[1]:
+        raise TypeError("inv_freq is fp32 and positions are int32")
+
+
+def rope(desc: RopeDesc, inv_freq, positions, x, out=None, stream=None) -> None:
+    """Rotate rows x [n, heads, head_dim] into ``out`` (default: in place);
+    ``positions`` int32 [num_axes, n], ``inv_freq`` fp32 (``fnpu_rope``)."""
+    n, h, d = x.shape
+    out = x if out is None else out
+    if tuple(out.shape) != (n, h, d):
+        raise ValueError("out has the shape of x")
+    _check_positions(desc, inv_freq, positions, n)
+    (xp, xs), (op, os_) = _rows(x), _rows(out)
+    rc = load().fnpu_rope(ctypes.byref(desc), _dptr(inv_freq), _dptr(positions), xp, xs, h, d, n, op, os_, _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_rope")
+
+
+def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q, k_new, v_new, slot_mapping, q_out,
+                k_cache, v_cache, kv_format: int = KV_BF16, stream=None) -> None:
+    """Rotate the step's queries into ``q_out`` and its keys into their cache
+    slots, and store its values (``fnpu_rope_append``); q, k_new and v_new are
+    [n, heads, d], their tokens possibly apart. ``rope`` None: rows as they are."""
+    n = int(slot_mapping.shape[0])
+    if any(x is not None and int(x.shape[0]) != n for x in (q, k_new, v_new)):
+        raise ValueError("q, k_new, v_new and slot_mapping have the same number of tokens")
+    if rope is not None:
+        _check_positions(rope, inv_freq, positions, n)
+    (qp, qs), (kp, ks), (vp, vs) = ((None, 0) if x is None else _rows(x) for x in (q, k_new, v_new))
+    rc = load().fnpu_rope_append(ctypes.byref(desc), int(kv_format), None if rope is None else ctypes.byref(rope),
+                                 _dptr(inv_freq), _dptr(positions), qp, qs, kp, ks, vp, vs, _dptr(slot_mapping), n,
+                                 _dptr(q_out), _dptr(k_cache), _dptr(v_cache), _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_rope_append")
+
+
+def kv_read(desc: AttnDesc, slots, k_cache, v_cache, k_out, v_out, kv_format: int = KV_BF16, stream=None) -> None:
+    """The rows that ``slots`` store, as bf16 (``fnpu_kv_read``)."""
+    rc = load().fnpu_kv_read(ctypes.byref(desc), int(kv_format), _dptr(slots), int(slots.shape[0]), _dptr(k_cache),
+                             _dptr(v_cache), _dptr(k_out), _dptr(v_out), _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_kv_read")
+
+
+def kv8_block_bytes(desc: AttnDesc, kv_format: int) -> int:
+    """Bytes of one block of each pool in an 8-bit block format."""
+    out = ctypes.c_int64()
+    rc = load().fnpu_kv8_block_bytes(ctypes.byref(desc), int(kv_format), ctypes.byref(out))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_kv8_block_bytes")
+    return out.value
+
+
+def kv8_attn_plan(desc: AttnDesc, kv_format: int, query_len, context_len, phase, block_table,
+                  opts: Optional[PlanOpts] = None, stream=None) -> Plan:
+    """A plan over an 8-bit block cache (``fnpu_kv8_attn_plan``)."""
+    arrays, addr = _step_meta(query_len, context_len, phase, block_table)
+    ql = arrays[0]
+    out = ctypes.c_void_p()
+    rc = load().fnpu_kv8_attn_plan(ctypes.byref(desc), int(kv_format), ql.shape[0], *addr,
+                                   None if opts is None else ctypes.byref(opts), _stream(stream), ctypes.byref(out))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_kv8_attn_plan")
+    return Plan(out.value, desc, int(ql.sum()))

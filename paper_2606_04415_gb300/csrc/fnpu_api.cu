@@ -31,6 +31,8 @@ struct fnpu_plan {
     int32_t bt_width = 0;
     int32_t num_sms = 0;
     int32_t flags = 0;
+    int32_t kv_format = FNPU_KV_BF16;  // 8-bit block formats: fnpu_kv8_attn_plan
+    bool kv8_wide = false;             // ... some sequence has more rows a kv head than the narrow kernel takes
     bool use_tc = false;
     bool use_dt = false;
     bool use_mla = false;  // latent attention: one work list for both phases
@@ -56,7 +58,8 @@ struct fnpu_plan {
     fnpu::DecodeItem *d_ditems = nullptr;
     // FP8 cache with tcgen05 prefill: the prefill sequences' blocks dequantised
     // to f16 (num_jobs blocks, block table of tbt_width columns) and the
-    // queries in f16, staged before the prefill kernel
+    // queries in f16, staged before the prefill kernel (8-bit block formats: the
+    // blocks in bf16, the queries as they are)
     int32_t num_jobs = 0, tbt_width = 1, num_tblocks = 0;
     fnpu::Fp8StageJob *d_jobs = nullptr;
     int32_t *d_tbt = nullptr;
@@ -181,6 +184,12 @@ constexpr double kTileSec = 1.5e-6;
 constexpr double kDecodeSmBps = 69e9;
 constexpr double kDecodeSmBpsFp8 = 50e9;  // (bytes of the FP8 cache: the conversion bounds it)
 constexpr double kDecodeAllBps = 4.0e12;
+
+// 8-bit block cache: sequences of up to this many rows a kv head (query tokens x
+// G) go to the decode kernel, 8 or 16 rows an item, which reads the codes once for
+// each; beyond, the staged copy of the prefill (one byte read, two written and read
+// again a value) costs less.
+constexpr int64_t kKv8DecodeRows = 64;
 
 // Two packed Q tiles of one kv head (the tcgen05 prefill unit) before its key
 // range is split.
@@ -615,6 +624,18 @@ namespace {
 int launch_prefill(const fnpu_plan *pl, const AttnParams &p, void *stream, int ctas, void *started,
                    bool pdl = false) {
     if (p.num_pitems == 0) return FNPU_OK;  // (nothing to stage either)
+    if (pl->kv_format != FNPU_KV_BF16) {
+        const int st = launch_kv8_stage(pl->kv_format, &pl->desc, p.k_cache, p.v_cache, pl->d_jobs, pl->num_jobs, pl->d_tk,
+                                        pl->d_tv, stream, pdl);
+        if (st != FNPU_OK) return st;
+        AttnParams pp = p;
+        pp.k_cache = pl->d_tk;
+        pp.v_cache = pl->d_tv;
+        pp.block_table = pl->d_tbt;
+        pp.bt_stride = pl->tbt_width;
+        pp.num_blocks = pl->num_tblocks;
+        return launch_prefill_tc(pp, stream, ctas, started, false, pdl && !started);
+    }
     if (!pl->desc.kv_fp8) return launch_prefill_tc(p, stream, ctas, started, false, pdl);
     const int rc = launch_fp8_stage(p.k_cache, p.v_cache, pl->d_jobs, pl->num_jobs, pl->d_tk, pl->d_tv, p.q, pl->d_tq,
                                     p.num_tokens * p.num_q_heads * p.head_dim_qk, stream, pdl);
@@ -705,9 +726,10 @@ struct StepMeta {
 // Host checks of a plan's arguments: nothing is launched or allocated.
 int validate_meta(const fnpu_attn_desc *desc, int32_t num_seqs, const int32_t *query_len,
                   const int32_t *context_len, const uint8_t *phase, const int32_t *block_table,
-                  int32_t block_table_stride, const fnpu_plan_opts &o, StepMeta *m) {
+                  int32_t block_table_stride, const fnpu_plan_opts &o, StepMeta *m, int32_t kv_format = FNPU_KV_BF16) {
     int st;
     if (!shape_ok(desc, &st)) return st;
+    if (kv_format < FNPU_KV_BF16 || kv_format > FNPU_KV_E4M3_BLOCK) return FNPU_EINVAL;
     if (num_seqs < 0) return FNPU_EINVAL;
     if (num_seqs > 0 && (!query_len || !context_len || !phase || !block_table)) return FNPU_EINVAL;
     if (o.decode_split_keys < 0 || o.decode_share_pct < 0 || o.decode_share_pct > 100 || o.num_sms < 0)
@@ -736,7 +758,13 @@ int validate_meta(const fnpu_attn_desc *desc, int32_t num_seqs, const int32_t *q
     }
     if (r.T > INT32_MAX) return FNPU_EINVAL;
     if (num_seqs > 0) {
-        const int ks = kernel_support(desc, r.has_decode, r.has_prefill);
+        // (8-bit blocks: every shape has its decode kernel; the staged prefill is
+        // the tcgen05 kernel alone)
+        const bool kv8_ok = kv8_supported(desc) && !(o.flags & FNPU_PLAN_NO_TCGEN05) &&
+                            prefill_tc_supported(desc->head_dim_qk, desc->head_dim_v, desc->block_size,
+                                                 desc->num_q_heads / desc->num_kv_heads);
+        const int ks = kv_format != FNPU_KV_BF16 ? (kv8_ok ? FNPU_OK : FNPU_EUNSUPPORTED)
+                                                 : kernel_support(desc, r.has_decode, r.has_prefill);
         if (ks != FNPU_OK) return ks;
     }
     *m = r;
@@ -776,8 +804,9 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     pl->use_mla = desc->v_in_k_latent != 0;
     pl->use_mla_tc = pl->use_mla && !(o.flags & FNPU_PLAN_NO_TCGEN05) &&
                      mla_tc_supported(desc->head_dim_qk, desc->head_dim_v, desc->num_q_heads, desc->num_kv_heads, bs);
-    pl->use_dt = !pl->use_mla && decode_tma_supported(desc->head_dim_qk, desc->head_dim_v,
-                                                      desc->num_q_heads / desc->num_kv_heads, bs);
+    const bool kv8 = pl->kv_format != FNPU_KV_BF16;
+    pl->use_dt = kv8 || (!pl->use_mla && decode_tma_supported(desc->head_dim_qk, desc->head_dim_v,
+                                                              desc->num_q_heads / desc->num_kv_heads, bs));
     pl->use_tc = !pl->use_mla && !(o.flags & FNPU_PLAN_NO_TCGEN05) &&
                  prefill_tc_supported(desc->head_dim_qk, desc->head_dim_v, bs,
                                       desc->num_q_heads / desc->num_kv_heads);
@@ -805,22 +834,27 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     // takes 61 us with 512-key items (322 items), 65 us with 256 and 68 us
     // with 128. The per-head kernel aims at about 3 waves of 2 CTAs per SM.
     // the queue a sequence's work enters: decode items for one-token decodes
-    auto decode_queue = [&](int32_t s) { return phase[s] == 1 && query_len[s] == 1; };
+    // (8-bit blocks: whatever has few rows a kv head, of either phase -- see kKv8DecodeRows)
+    auto decode_queue = [&](int32_t s) {
+        return kv8 ? static_cast<int64_t>(query_len[s]) * G <= kKv8DecodeRows : phase[s] == 1 && query_len[s] == 1;
+    };
     // a decode item with its sequence's fields and its first four block ids
     auto decode_item = [&](int32_t s, int32_t kvh, int32_t kb, int32_t ke, int32_t sp, int32_t ns, int32_t base,
                            int32_t grp) {
-        DecodeItem it{s, kvh, kb, ke, sp, ns, base, grp, seqs[s].q_start, seqs[s].bt_row, 0, 0, {0, 0, 0, 0}};
+        DecodeItem it{s, kvh, kb, ke, sp, ns, base, grp, seqs[s].q_start, seqs[s].bt_row, 0, query_len[s], {0, 0, 0, 0}};
         for (int32_t i = 0; i < 4 && kb / bs + i <= (ke - 1) / bs; ++i)
             it.blk[i] = block_table[static_cast<int64_t>(s) * block_table_stride + kb / bs + i];
         return it;
     };
     int64_t dec_keys = 0, num_dec = 0;
+    pl->kv8_wide = false;
     for (int32_t s = 0; s < num_seqs; ++s)
         if (decode_queue(s)) {
             dec_keys += context_len[s];
             ++num_dec;
+            pl->kv8_wide |= kv8 && query_len[s] * G > kv8_rows_per_item(false);
         }
-    if (pl->use_dt && desc->num_kv_heads <= 2 && desc->head_dim_qk == 64 && o.decode_share_pct == 0 &&
+    if (pl->use_dt && !kv8 && desc->num_kv_heads <= 2 && desc->head_dim_qk == 64 && o.decode_share_pct == 0 &&
         !(o.flags & FNPU_PLAN_GREEN_CONTEXTS)) {
         // One or two 64-wide kv heads leave three or two of the TMA kernel's four
         // compute warps idle. It is the faster one while a step is light (20 of
@@ -833,7 +867,7 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
                                              : num_dec < 2LL * sms || dec_keys < 256 * num_dec;
     }
     // items per key range: one per group of kv heads (TMA kernel), one per kv head
-    const int32_t hpi = pl->use_dt ? decode_tma_heads_per_item() : 1;
+    const int32_t hpi = kv8 ? kv8_heads_per_item(desc->num_kv_heads) : pl->use_dt ? decode_tma_heads_per_item() : 1;
     const int32_t hgroups = (desc->num_kv_heads + hpi - 1) / hpi;
     dec_keys *= hgroups;
     int32_t split = std::min(o.decode_split_keys, 1 << 30);  // (room to round up)
@@ -966,6 +1000,24 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
                                                  qs + i, c, s});
                 }
             }
+        } else if (decode_queue(s) && kv8) {
+            // as below; each split has a partial for every key part of the CTA (with
+            // fewer than four kv heads an item), each token its merge, and the rows of a
+            // kv head beyond the kernel's go to items of their own beside each other
+            const int32_t rows = q * G, per = kv8_rows_per_item(pl->kv8_wide), kparts = 4 / hpi;
+            const int32_t sk = std::max((split + 15) / 16 * 16, (c + 256 / kparts * 64 - 1) / (256 / kparts * 64) * 64);
+            const int32_t ns = (c + sk - 1) / sk * kparts;
+            const int32_t base = ns > 1 ? parts : 0;
+            for (int32_t i = 0; i < q && ns > 1; ++i) {
+                mgroups.push_back(MergeGroup{qs + i, ns, parts, 0});
+                parts += ns;
+            }
+            for (int32_t sp = 0; sp * sk < c; ++sp)
+                for (int32_t hg = 0; hg < hgroups; ++hg)
+                    for (int32_t r0 = 0; r0 < rows; r0 += per) {
+                        ditems.push_back(decode_item(s, hg * hpi, sp * sk, std::min(c, (sp + 1) * sk), sp * kparts, ns, base, c));
+                        ditems.back().row_begin = r0;
+                    }
         } else if (decode_queue(s) && pl->use_dt) {
             // items over groups of kv heads, cut at whole 16-key stages; a
             // split sequence is merged by the merge kernel (at most 256
@@ -1030,7 +1082,8 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
         for (const TcUnit &u : tc_units) item_tiles.push_back(u.ntiles + kTcItemCost);
         for (const DecodeItem &it : ditems)
             dec_bytes += static_cast<int64_t>(it.key_end - it.key_begin) * std::min(hpi, desc->num_kv_heads - it.kvh) *
-                         (desc->kv_fp8 ? desc->head_dim_qk + desc->head_dim_v + 8
+                         (kv8            ? desc->head_dim_qk + desc->head_dim_v
+                          : desc->kv_fp8 ? desc->head_dim_qk + desc->head_dim_v + 8
                                        : (desc->head_dim_qk + desc->head_dim_v) * 2);
     }
     if (pl->coloc && desc->num_kv_heads != 4 && o.decode_share_pct == 0 && !(o.flags & FNPU_PLAN_GREEN_CONTEXTS)) {
@@ -1064,7 +1117,7 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
             // 112 -> 99, 111 -> 97.5 125 -> 113.5; but 60 -> 54 measured 79.6 -> 83.5
             // and 85.5 -> 81 97 -> 100. (No schedule is shorter than the work
             // of both phases over all SMs, which rules most steps out.)
-            const double sm_bps = desc->kv_fp8 ? kDecodeSmBpsFp8 : kDecodeSmBps;
+            const double sm_bps = desc->kv_fp8 || kv8 ? kDecodeSmBpsFp8 : kDecodeSmBps;
             const DecodeShare whole = choose_decode_sms(item_tiles, nullptr, tile_scale, dec_bytes, sm_bps, sms);
             k = whole.k;
             int64_t work = 0;
@@ -1145,7 +1198,7 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     // copy (its own block-table row over the staged blocks)
     std::vector<Fp8StageJob> jobs;
     std::vector<int32_t> tbt;
-    if (desc->kv_fp8 && pl->use_tc && !tc_units.empty()) {
+    if ((desc->kv_fp8 || kv8) && pl->use_tc && !tc_units.empty()) {
         std::vector<char> pre(num_seqs, 0);
         for (const TcUnit &u : tc_units) pre[u.seq] = 1;
         int32_t tw = 1;
@@ -1249,7 +1302,7 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     const size_t o_tk = off; off = align_up(off + (pl->num_jobs ? stage_blk * pl->num_tblocks : 0), 256);
     const size_t o_tv = off; off = align_up(off + (pl->num_jobs ? stage_blk * pl->num_tblocks : 0), 256);
     const size_t o_tq = off;
-    off = align_up(off + (pl->num_jobs ? static_cast<size_t>(T) * desc->num_q_heads * desc->head_dim_qk * 2 : 0), 256);
+    off = align_up(off + (pl->num_jobs && !kv8 ? static_cast<size_t>(T) * desc->num_q_heads * desc->head_dim_qk * 2 : 0), 256);
     pl->ws_bytes = off;
 
     // device workspace: allocated once, grown only when a re-plan needs more
@@ -1361,25 +1414,22 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     return FNPU_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-int fnpu_mixed_attn_plan_ex(const fnpu_attn_desc *desc, int32_t num_seqs, const int32_t *query_len,
-                            const int32_t *context_len, const uint8_t *phase,
-                            const int32_t *block_table, int32_t block_table_stride,
-                            const fnpu_plan_opts *opts, void *stream, fnpu_plan **out) {
+// A new plan for a validated step.
+int plan_new(const fnpu_attn_desc *desc, int32_t kv_format, int32_t num_seqs, const int32_t *query_len, const int32_t *context_len,
+             const uint8_t *phase, const int32_t *block_table, int32_t block_table_stride, const fnpu_plan_opts *opts, void *stream,
+             fnpu_plan **out) {
     if (!out) return FNPU_EINVAL;
     fnpu_plan_opts o = {};
     if (opts) o = *opts;
     StepMeta m;
-    int rc = validate_meta(desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, &m);
+    int rc = validate_meta(desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, &m, kv_format);
     if (rc != FNPU_OK) return rc;
     int sms = 0;
     rc = plan_sms(o, &sms);
     if (rc != FNPU_OK) return rc;
     fnpu_plan *pl = new (std::nothrow) fnpu_plan();
     if (!pl) return FNPU_ENOMEM;
+    pl->kv_format = kv_format;
     rc = plan_fill(pl, desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, m, sms,
                    stream);
     if (rc != FNPU_OK) {
@@ -1391,6 +1441,24 @@ int fnpu_mixed_attn_plan_ex(const fnpu_attn_desc *desc, int32_t num_seqs, const 
     return FNPU_OK;
 }
 
+}  // namespace
+
+extern "C" {
+
+int fnpu_mixed_attn_plan_ex(const fnpu_attn_desc *desc, int32_t num_seqs, const int32_t *query_len,
+                            const int32_t *context_len, const uint8_t *phase,
+                            const int32_t *block_table, int32_t block_table_stride,
+                            const fnpu_plan_opts *opts, void *stream, fnpu_plan **out) {
+    return plan_new(desc, FNPU_KV_BF16, num_seqs, query_len, context_len, phase, block_table, block_table_stride, opts, stream, out);
+}
+
+int fnpu_kv8_attn_plan(const fnpu_attn_desc *desc, int32_t kv_format, int32_t num_seqs, const int32_t *query_len,
+                       const int32_t *context_len, const uint8_t *phase, const int32_t *block_table,
+                       int32_t block_table_stride, const fnpu_plan_opts *opts, void *stream, fnpu_plan **out) {
+    if (kv_format != FNPU_KV_INT8_BLOCK && kv_format != FNPU_KV_E4M3_BLOCK) return FNPU_EINVAL;
+    return plan_new(desc, kv_format, num_seqs, query_len, context_len, phase, block_table, block_table_stride, opts, stream, out);
+}
+
 int fnpu_mixed_attn_replan(fnpu_plan *pl, int32_t num_seqs, const int32_t *query_len, const int32_t *context_len,
                            const uint8_t *phase, const int32_t *block_table, int32_t block_table_stride,
                            const fnpu_plan_opts *opts, void *stream) {
@@ -1399,7 +1467,7 @@ int fnpu_mixed_attn_replan(fnpu_plan *pl, int32_t num_seqs, const int32_t *query
     if (opts) o = *opts;
     StepMeta m;
     int rc = validate_meta(&pl->desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o,
-                           &m);
+                           &m, pl->kv_format);
     if (rc != FNPU_OK) return rc;  // the plan is unchanged
     int sms = 0;
     rc = plan_sms(o, &sms);
@@ -1471,6 +1539,7 @@ bool run_pointers_ok(const fnpu_plan *pl, const void *q, const void *k_cache, co
 
 // The decode kernel of a plan and its merge, on `stream`.
 int launch_decode(const fnpu_plan *pl, const AttnParams &p, void *stream, int ctas) {
+    if (pl->kv_format != FNPU_KV_BF16) return launch_decode_kv8(pl->kv_format, p, pl->kv8_wide, stream, ctas, false);
     return pl->desc.kv_fp8 ? launch_decode_fp8(p, stream, ctas, false) : launch_decode_tma(p, stream, ctas, false);
 }
 
@@ -1563,7 +1632,9 @@ int fnpu_mixed_attn_run(const fnpu_plan *pl, const void *q, const void *k_cache,
     const AttnParams p = run_params(pl, q, k_cache, v_cache, out, lse);
     if (pl->use_mla) return pl->use_mla_tc ? launch_mla_tc(p, stream, pl->num_sms) : launch_mla(p, stream);
     if (pl->coloc) return run_colocated(pl, p, stream);
-    int rc = pl->desc.kv_fp8 ? launch_decode_fp8(p, stream, 3 * pl->num_sms, true)
+    int rc = pl->kv_format != FNPU_KV_BF16
+                 ? launch_decode_kv8(pl->kv_format, p, pl->kv8_wide, stream, 3 * pl->num_sms, true)
+             : pl->desc.kv_fp8 ? launch_decode_fp8(p, stream, 3 * pl->num_sms, true)
              : pl->use_dt    ? launch_decode_tma(p, stream, 3 * pl->num_sms, true)
                              : launch_decode_mma(p, stream);
     if (rc != FNPU_OK) return rc;
@@ -1586,9 +1657,13 @@ int fnpu_mixed_step(const fnpu_plan *pl, const void *k_new, const void *v_new, c
     // the prefill is the tcgen05 kernel over a bf16 cache (green-context
     // plans keep the two calls)
     const bool fused = (pl->flags & FNPU_PLAN_FUSED_APPEND) && pl->use_tc && !pl->use_mla && !pl->desc.kv_fp8 &&
-                       pl->num_ftok > 0 && !pl->g_pre;
+                       pl->num_ftok > 0 && !pl->g_pre && pl->kv_format == FNPU_KV_BF16;
     if (!fused) {
-        const int rc = fnpu_kv_append(&pl->desc, k_new, v_new, slot_mapping, n, k_cache, v_cache, stream);
+        const int64_t row = static_cast<int64_t>(pl->desc.num_kv_heads) * pl->desc.head_dim_qk;
+        const int rc = pl->kv_format != FNPU_KV_BF16
+                           ? fnpu_rope_append(&pl->desc, pl->kv_format, nullptr, nullptr, nullptr, nullptr, 0, k_new, row, v_new,
+                                              row, slot_mapping, n, nullptr, k_cache, v_cache, stream)
+                           : fnpu_kv_append(&pl->desc, k_new, v_new, slot_mapping, n, k_cache, v_cache, stream);
         if (rc != FNPU_OK) return rc;
         return fnpu_mixed_attn_run(pl, q, k_cache, v_cache, out, lse, stream);
     }

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -16,10 +17,14 @@ namespace fnpu {
 // to scratch rows part_base + split. The item also carries its sequence's
 // query token and block-table row and the ids of its first four blocks, so
 // that a kernel can issue its first copies after one load.
+// 8-bit block kernel: the item is rows [row_begin, row_begin + rows a kernel takes)
+// of the q_len x G rows (token, query head of the kv head) of the sequence, `group`
+// is its context length and `split` its first partial of each token (one for each
+// of the CTA's key parts).
 struct DecodeItem {
     int32_t seq, kvh, key_begin, key_end;
     int32_t split, num_splits, part_base, group;
-    int32_t q_start, bt_row, pad0, pad1;
+    int32_t q_start, bt_row, row_begin, q_len;  // (the last two: 8-bit block kernel, see below)
     int32_t blk[4];  // block_table[bt_row][key_begin / bs + i], 0 past the item
 };
 static_assert(sizeof(DecodeItem) == 64, "DecodeItem layout");
@@ -128,6 +133,32 @@ struct AttnParams {
     int32_t na_num_seqs, na_max_ctx, na_split, na_max_splits;
 };
 
+// Rotation of column pairs: pair i of a row turns by positions[axis[i]][t] *
+// inv_freq[i]; sign -1 turns back.
+constexpr int kRopeMaxAxes = 4;
+constexpr int kRopeMaxPairs = 128;
+struct RopeArgs {
+    const float *inv_freq;     // [pairs]
+    const int32_t *positions;  // [axes, n]
+    int64_t n;                 // tokens
+    int32_t pairs, offset, interleaved, axes;
+    float sign;
+    uint8_t axis[kRopeMaxPairs];
+};
+
+// Rows of an append: queries and keys may turn (RopeArgs), keys and values go to
+// their slots. Strides in elements between tokens; q null: no queries.
+struct RopeAppendArgs {
+    const __nv_bfloat16 *q, *k_new, *v_new;
+    int64_t q_stride, k_stride, v_stride;
+    const int64_t *slots;
+    __nv_bfloat16 *q_out;
+    void *k_cache, *v_cache;  // v_new, v_cache null: a latent cache
+    int64_t num_slots;
+    int32_t q_heads, kv_heads, d, d_v, block_size;
+    int *err;                 // the library-wide error flag
+};
+
 // cuTensorMapEncodeTiled, looked up once through the runtime's driver entry
 // point (the library does not link the driver library); null if unavailable.
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -175,6 +206,27 @@ struct Fp8StageJob {
 };
 int launch_fp8_stage(const void *k_pool, const void *v_pool, const Fp8StageJob *jobs, int32_t num_jobs, void *k_f16,
                      void *v_f16, const void *q_bf16, void *q_f16, int64_t q_values, void *stream, bool pdl);
+// Rotary positions. vector: rows may be read in 16-byte chunks of eight pairs.
+int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, int d, void *out, int64_t out_stride,
+                bool vector, void *stream);
+int rope_heads_per_warp(int64_t n, int heads, int pairs);
+int launch_rope_append(const RopeArgs &r, const RopeAppendArgs &p, void *stream);
+// 8-bit cache with a scale for each (block, kv head), format FNPU_KV_INT8_BLOCK or
+// FNPU_KV_E4M3_BLOCK: append (turning rows where r.pairs > 0), rows read back as
+// bf16, staging of listed blocks as bf16 blocks for the tcgen05 prefill, and the
+// split-KV attention of few rows a sequence
+bool kv8_supported(const fnpu_attn_desc *d);
+int64_t kv8_block_bytes(int hkv, int block_size, int d);
+int launch_kv8_append(int format, const RopeArgs &r, const RopeAppendArgs &p, void *stream);
+int launch_kv8_read(int format, const fnpu_attn_desc *d, const int64_t *slots, int32_t n, const void *k_pool,
+                    const void *v_pool, void *k_out, void *v_out, int *err, void *stream);
+int launch_kv_read_bf16(const fnpu_attn_desc *d, const int64_t *slots, int32_t n, const void *k_cache, const void *v_cache,
+                        void *k_out, void *v_out, int *err, void *stream);
+int launch_kv8_stage(int format, const fnpu_attn_desc *d, const void *k_pool, const void *v_pool, const Fp8StageJob *jobs,
+                     int32_t num_jobs, void *k_bf16, void *v_bf16, void *stream, bool pdl);
+int launch_decode_kv8(int format, const AttnParams &p, bool wide, void *stream, int max_ctas, bool alone);
+int kv8_heads_per_item(int hkv);  // kv heads of an item; 4 / this key parts
+int kv8_rows_per_item(bool wide);
 bool decode_fp8_supported(int d_qk, int d_v, int hkv, int group, int block_size);
 int launch_decode_mma(const AttnParams &p, void *stream);
 int launch_decode_tma(const AttnParams &p, void *stream, int max_ctas, bool alone);

@@ -1,0 +1,357 @@
+// Writing to and reading from the 8-bit cache with a scale per block and kv head.
+#include "kv8.cuh"
+#include "rope.cuh"
+
+namespace fnpu {
+namespace {
+
+// ------------------------------------------------------------------ append
+//
+// The rows that a call stores in one block are a run: consecutive tokens at
+// consecutive slots of it. They and the rows before them share one scale per kv
+// head, so a run is one piece of work per kv head and side (K or V): take the
+// largest magnitude of its rows, and where that asks for a larger exponent than the
+// block has, store the rows before the run anew. A block whose slot 0 is in the
+// run is a fresh one; what it held and its scale are dead.
+//
+// A warp has 16 rows of the block (a run of a 64-slot block is four warps' work): 16
+// columns a lane, the eight pairs that a lane turns among them, so that K rows are
+// turned and stored in one pass through registers. Every (token, kv head, side)
+// has a place in the grid and those that do not begin a run leave at once: no list
+// of runs to build, and a decode step, whose rows are all runs of one, has a warp
+// for each. The queries are turned by further CTAs of the same launch.
+constexpr int kRowsPerWarp = 16;
+
+template <int kFormat, int kD>
+__device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendArgs &p, int64_t t, int64_t slot, int n, int head,
+                                           bool is_v, int part, int parts, int lane, uint32_t *amax_sh) {
+    constexpr int kLanesPerRow = kD / 16, kPass = 32 / kLanesPerRow, kPasses = kRowsPerWarp / kPass;
+    const int bs = p.block_size;
+    const int off = static_cast<int>(slot % bs);
+    uint8_t *blk = static_cast<uint8_t *>(is_v ? p.v_cache : p.k_cache) + slot / bs * kv8::block_bytes(p.kv_heads, bs, kD);
+    uint8_t *rows = blk + static_cast<int64_t>(head) * bs * kD;
+    float *scale = reinterpret_cast<float *>(blk + static_cast<int64_t>(p.kv_heads) * bs * kD) + head;
+    const int e_old = off > 0 ? kv8::scale_exp(*scale) : kv8::kMinExp;
+    const __nv_bfloat16 *src = is_v ? p.v_new : p.k_new;
+    const int64_t stride = is_v ? p.v_stride : p.k_stride;
+    const int c = lane % kLanesPerRow, lr = lane / kLanesPerRow;
+    const int cp = is_v ? 0 : r.pairs >> 3;
+    int ca, cb;
+    if (c < cp) {
+        rope_columns(r, c, ca, cb);
+    } else {  // 16 columns that do not turn
+        ca = 16 * (c - cp);
+        if (cp > 0 && ca >= r.offset) ca += 2 * r.pairs;
+        cb = ca + 8;
+    }
+    float a[kPasses][8], b[kPasses][8];
+    uint4 ra[kPasses], rb[kPasses];
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int o = part * kRowsPerWarp + i * kPass + lr;
+        ra[i] = rb[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (o >= off && o < off + n) {
+            const __nv_bfloat16 *row = src + (t + o - off) * stride + static_cast<int64_t>(head) * kD;
+            ra[i] = __ldg(reinterpret_cast<const uint4 *>(row + ca));
+            rb[i] = __ldg(reinterpret_cast<const uint4 *>(row + cb));
+        }
+    }
+    float amax = 0.f;
+    bool odd = false;  // a value that is not finite
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int o = part * kRowsPerWarp + i * kPass + lr;
+        bf16x8_to_f32(ra[i], a[i]);
+        bf16x8_to_f32(rb[i], b[i]);
+        if (c < cp && o >= off && o < off + n) {
+            float cs[8], sn[8];
+            rope_angles8(r, t + o - off, c, cs, sn);
+            rope_rotate8(r.interleaved != 0, cs, sn, a[i], b[i]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = fabsf(a[i][j]), y = fabsf(b[i][j]);
+            odd |= !(x < INFINITY) | !(y < INFINITY);
+            amax = fmaxf(amax, fmaxf(x, y));
+        }
+    }
+    if (odd) {  // NaN is stored as zero, an infinity as the largest magnitude that the others allow
+        amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (a[i][j] != a[i][j]) a[i][j] = 0.f;
+                if (b[i][j] != b[i][j]) b[i][j] = 0.f;
+                if (fabsf(a[i][j]) < INFINITY) amax = fmaxf(amax, fabsf(a[i][j]));
+                if (fabsf(b[i][j]) < INFINITY) amax = fmaxf(amax, fabsf(b[i][j]));
+            }
+        atomicOr(p.err, 8);
+    }
+    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));  // (non-negative floats order as integers)
+    if (parts > 1) {
+        if (lane == 0) amax_sh[part] = top;
+        __syncthreads();  // (every warp of the CTA has the same run; all have read the old scale)
+        for (int i = 0; i < parts; ++i) top = max(top, amax_sh[i]);
+        __syncthreads();
+    }
+    int e = max(e_old, kv8::required_exp<kFormat>(__uint_as_float(top)));
+    if (e > kv8::kMaxExp) {
+        e = kv8::kMaxExp;
+        if (lane == 0) atomicOr(p.err, 8);
+    }
+    const float inv = kv8::pow2(-e);
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int o = part * kRowsPerWarp + i * kPass + lr;
+        if (o >= off && o < off + n) {
+            *reinterpret_cast<uint2 *>(rows + o * kD + ca) = kv8::encode8<kFormat>(a[i], inv);
+            *reinterpret_cast<uint2 *>(rows + o * kD + cb) = kv8::encode8<kFormat>(b[i], inv);
+        } else if (o < off && e > e_old) {  // a row that the block held before, over the grown scale
+            const float down = kv8::pow2(e_old - e);
+            for (int s = 0; s < 2; ++s) {
+                uint2 *at = reinterpret_cast<uint2 *>(rows + o * kD + (s ? cb : ca));
+                const uint2 w = *at;
+                float x[4], y[4];
+                kv8::decode4<kFormat>(w.x, x);
+                kv8::decode4<kFormat>(w.y, y);
+                const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                *at = kv8::encode8<kFormat>(f, down);
+            }
+        }
+    }
+    if (part == 0 && lane == 0 && (off == 0 || e > e_old)) *scale = kv8::pow2(e);
+}
+
+template <int kFormat, int kD>
+__global__ void __launch_bounds__(256)
+    kv8_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int kv_ctas, int parts,
+                      int q_groups, int q_heads_per_warp) {
+    __shared__ uint32_t amax_sh[kRowsPerWarp];
+    pdl_trigger();
+    pdl_wait();  // writers of the rows, earlier readers of the blocks
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    if (static_cast<int>(blockIdx.x) >= kv_ctas) {
+        const int64_t w = static_cast<int64_t>(blockIdx.x - kv_ctas) * warps + warp, t = w / q_groups;
+        if (t >= r.n) return;
+        const int h0 = static_cast<int>(w - t * q_groups) * q_heads_per_warp;
+        rope_heads(r, t, h0, min(p.q_heads, h0 + q_heads_per_warp), kD, lane,
+                   [&](int h) { return p.q + t * p.q_stride + static_cast<int64_t>(h) * kD; },
+                   [&](int h) { return p.q_out + (t * p.q_heads + h) * kD; });
+        return;
+    }
+    // units (token, side, head), warps / parts of them a CTA at a time
+    const int per = 2 * p.kv_heads, units = warps / parts, sub = warp / parts, part = warp - sub * parts;
+    const int64_t total = r.n * per;
+    for (int64_t u0 = static_cast<int64_t>(blockIdx.x) * units; u0 < total; u0 += static_cast<int64_t>(kv_ctas) * units) {
+        const int64_t u = u0 + sub;  // (with several parts a CTA has one unit: all its warps take the same branches)
+        if (u >= total) continue;
+        const int64_t t = u / per;
+        const int j = static_cast<int>(u - t * per);
+        const int64_t slot = __ldg(p.slots + t), before = t > 0 ? __ldg(p.slots + t - 1) : -1;
+        if (slot < 0) continue;
+        if (slot >= p.num_slots) {
+            if (j == 0 && part == 0 && lane == 0) atomicOr(p.err, 1);
+            continue;
+        }
+        const int off = static_cast<int>(slot % p.block_size);
+        if (off > 0 && before == slot - 1) continue;  // inside a run
+        int n = 1;  // rows of the run: tokens t + i at slot + i, within the block
+        for (int i0 = 1; i0 < p.block_size - off; i0 += 32) {
+            const int i = i0 + lane;
+            const bool more = i < p.block_size - off && t + i < r.n && __ldg(p.slots + t + i) == slot + i;
+            const uint32_t miss = ~__ballot_sync(0xffffffffu, more);
+            n += miss ? __ffs(miss) - 1 : 32;
+            if (miss) break;
+        }
+        append_run<kFormat, kD>(r, p, t, slot, n, j % p.kv_heads, j >= p.kv_heads, part, parts, lane, amax_sh);
+    }
+}
+
+// -------------------------------------------------------------------- read
+
+// 16 codes, scaled, as two 16-byte chunks of bf16 (exact)
+template <int kFormat>
+__device__ __forceinline__ void codes_to_bf16(const uint4 &w, float scale, uint4 &lo, uint4 &hi) {
+    const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+    uint32_t out[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float f[4];
+        kv8::decode4<kFormat>(in[i], f);
+        out[2 * i] = pack_bf16x2(f[0] * scale, f[1] * scale);
+        out[2 * i + 1] = pack_bf16x2(f[2] * scale, f[3] * scale);
+    }
+    lo = make_uint4(out[0], out[1], out[2], out[3]);
+    hi = make_uint4(out[4], out[5], out[6], out[7]);
+}
+
+// A thread per 16 values of a row: K rows' first, then V's.
+template <int kFormat>
+__global__ void __launch_bounds__(256)
+    kv8_read_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool, const int64_t *__restrict__ slots,
+                    int64_t n, int64_t num_slots, int hkv, int bs, int d, uint4 *__restrict__ k_out, uint4 *__restrict__ v_out,
+                    int *err) {
+    pdl_trigger();
+    pdl_wait();
+    const int per_row = d >> 4, per = hkv * per_row;
+    const int64_t bytes = kv8::block_bytes(hkv, bs, d), total = 2 * n * per;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+        const bool v = i >= n * per;
+        const int64_t k = v ? i - n * per : i, row = k / per;
+        const int j = static_cast<int>(k - row * per), h = j / per_row, c = j - h * per_row;
+        const int64_t slot = __ldg(slots + row);
+        uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+        if (slot >= num_slots) {
+            if (k == row * per && !v) atomicOr(err, 1);
+        } else if (slot >= 0) {
+            const uint8_t *blk = (v ? v_pool : k_pool) + slot / bs * bytes;
+            const int o = static_cast<int>(slot % bs);
+            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(blk + (static_cast<int64_t>(h) * bs + o) * d) + c);
+            const float scale = __ldg(reinterpret_cast<const float *>(blk + static_cast<int64_t>(hkv) * bs * d) + h);
+            codes_to_bf16<kFormat>(w, scale, lo, hi);
+        }
+        uint4 *to = (v ? v_out : k_out) + 2 * k;
+        to[0] = lo;
+        to[1] = hi;
+    }
+}
+
+__global__ void __launch_bounds__(256)
+    kv_read_bf16_kernel(const uint4 *__restrict__ k_cache, const uint4 *__restrict__ v_cache, const int64_t *__restrict__ slots,
+                        int64_t n, int64_t num_slots, int k_chunks, int v_chunks, uint4 *__restrict__ k_out,
+                        uint4 *__restrict__ v_out, int *err) {
+    pdl_trigger();
+    pdl_wait();
+    const int per = k_chunks + v_chunks;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n * per; i += gridDim.x * 256ll) {
+        const int64_t row = i / per;
+        const int c = static_cast<int>(i - row * per);
+        const int64_t slot = __ldg(slots + row);
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (slot >= num_slots) {
+            if (c == 0) atomicOr(err, 1);
+        } else if (slot >= 0) {
+            w = c < k_chunks ? __ldg(k_cache + slot * k_chunks + c) : __ldg(v_cache + slot * v_chunks + c - k_chunks);
+        }
+        if (c < k_chunks) k_out[row * k_chunks + c] = w;
+        else v_out[row * v_chunks + c - k_chunks] = w;
+    }
+}
+
+// ----------------------------------------------------------------- staging
+//
+// The tcgen05 prefill takes bf16 operands, which hold the stored values exactly.
+// A CTA writes one kv head of a source block, K and V, as bf16 rows [slots][kv
+// heads][d] of block `dst`; rows past `valid` are zero.
+template <int kFormat>
+__global__ void __launch_bounds__(128)
+    kv8_stage_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool, const Fp8StageJob *__restrict__ jobs,
+                     int hkv, int bs, int d, uint4 *__restrict__ k_out, uint4 *__restrict__ v_out) {
+    pdl_trigger();
+    pdl_wait();  // the codes of the kernel before (the step's append)
+    const Fp8StageJob jb = jobs[blockIdx.x / hkv];
+    const int h = blockIdx.x % hkv;
+    const int per_row = d >> 4, per = bs * per_row;
+    const int64_t src = jb.src * kv8::block_bytes(hkv, bs, d), codes = static_cast<int64_t>(hkv) * bs * d;
+    const float ks = __ldg(reinterpret_cast<const float *>(k_pool + src + codes) + h);
+    const float vs = __ldg(reinterpret_cast<const float *>(v_pool + src + codes) + h);
+    for (int i = threadIdx.x; i < per; i += 128) {
+        const int o = i / per_row, c = i - o * per_row;
+        const int64_t from = src + (static_cast<int64_t>(h) * bs + o) * d;
+        const uint4 kw = __ldg(reinterpret_cast<const uint4 *>(k_pool + from) + c);
+        const uint4 vw = __ldg(reinterpret_cast<const uint4 *>(v_pool + from) + c);
+        const int64_t to = (((static_cast<int64_t>(jb.dst) * bs + o) * hkv + h) * per_row + c) * 2;
+        uint4 z = make_uint4(0u, 0u, 0u, 0u), klo = z, khi = z, vlo = z, vhi = z;
+        if (o < jb.valid) {
+            codes_to_bf16<kFormat>(kw, ks, klo, khi);
+            codes_to_bf16<kFormat>(vw, vs, vlo, vhi);
+        }
+        k_out[to] = klo;
+        k_out[to + 1] = khi;
+        v_out[to] = vlo;
+        v_out[to + 1] = vhi;
+    }
+}
+
+int sm_count() {
+    int dev = 0, sms = 152;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    return sms;
+}
+
+template <int kFormat, int kD>
+int launch_append(const RopeArgs &r, const RopeAppendArgs &p, cudaStream_t st) {
+    const int parts = p.block_size / kRowsPerWarp;
+    const int warps = 8, units = parts > 1 ? 1 : warps;
+    const int threads = 32 * (parts > 1 ? parts : warps);
+    const int64_t total = r.n * 2 * p.kv_heads, want = (total + units - 1) / units;
+    const int64_t cap = 16ll * sm_count() * (parts > 1 ? 2 : 1);
+    const int kv_ctas = static_cast<int>(want < cap ? want : cap);
+    int groups = 1, hpw = 1;
+    int64_t q_ctas = 0;
+    if (p.q && p.q_heads > 0) {
+        hpw = rope_heads_per_warp(r.n, p.q_heads, r.pairs);
+        groups = (p.q_heads + hpw - 1) / hpw;
+        q_ctas = (r.n * groups + threads / 32 - 1) / (threads / 32);
+    }
+    if (kv_ctas + q_ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
+    FNPU_CUDA_TRY(launch_ex(kv8_append_kernel<kFormat, kD>, static_cast<int>(kv_ctas + q_ctas), threads, 0, st, true, nullptr, r, p,
+                            kv_ctas, parts, groups, hpw));
+    return FNPU_OK;
+}
+
+}  // namespace
+
+bool kv8_supported(const fnpu_attn_desc *d) {
+    return !d->v_in_k_latent && d->kv_fp8 == 0 && d->head_dim_qk == d->head_dim_v && (d->head_dim_qk == 64 || d->head_dim_qk == 128) &&
+           (d->block_size == 16 || d->block_size == 32 || d->block_size == 64);
+}
+
+int64_t kv8_block_bytes(int hkv, int block_size, int d) { return kv8::block_bytes(hkv, block_size, d); }
+
+int launch_kv8_append(int format, const RopeArgs &r, const RopeAppendArgs &p, void *stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (format == FNPU_KV_INT8_BLOCK)
+        return p.d == 64 ? launch_append<FNPU_KV_INT8_BLOCK, 64>(r, p, st) : launch_append<FNPU_KV_INT8_BLOCK, 128>(r, p, st);
+    return p.d == 64 ? launch_append<FNPU_KV_E4M3_BLOCK, 64>(r, p, st) : launch_append<FNPU_KV_E4M3_BLOCK, 128>(r, p, st);
+}
+
+int launch_kv8_read(int format, const fnpu_attn_desc *d, const int64_t *slots, int32_t n, const void *k_pool, const void *v_pool,
+                    void *k_out, void *v_out, int *err, void *stream) {
+    const int64_t want = (2ll * n * d->num_kv_heads * (d->head_dim_qk / 16) + 255) / 256, cap = 32ll * sm_count();
+    const int grid = static_cast<int>(want < cap ? want : cap);
+    auto kernel = format == FNPU_KV_INT8_BLOCK ? kv8_read_kernel<FNPU_KV_INT8_BLOCK> : kv8_read_kernel<FNPU_KV_E4M3_BLOCK>;
+    FNPU_CUDA_TRY(launch_ex(kernel, grid, 256, 0, static_cast<cudaStream_t>(stream), true, nullptr,
+                            static_cast<const uint8_t *>(k_pool), static_cast<const uint8_t *>(v_pool), slots, static_cast<int64_t>(n),
+                            static_cast<int64_t>(d->num_blocks) * d->block_size, static_cast<int>(d->num_kv_heads),
+                            static_cast<int>(d->block_size), static_cast<int>(d->head_dim_qk), static_cast<uint4 *>(k_out),
+                            static_cast<uint4 *>(v_out), err));
+    return FNPU_OK;
+}
+
+int launch_kv_read_bf16(const fnpu_attn_desc *d, const int64_t *slots, int32_t n, const void *k_cache, const void *v_cache,
+                        void *k_out, void *v_out, int *err, void *stream) {
+    const int kc = d->num_kv_heads * d->head_dim_qk / 8, vc = d->v_in_k_latent ? 0 : d->num_kv_heads * d->head_dim_v / 8;
+    const int64_t want = (static_cast<int64_t>(n) * (kc + vc) + 255) / 256, cap = 32ll * sm_count();
+    const int grid = static_cast<int>(want < cap ? want : cap);
+    FNPU_CUDA_TRY(launch_ex(kv_read_bf16_kernel, grid, 256, 0, static_cast<cudaStream_t>(stream), true, nullptr,
+                            static_cast<const uint4 *>(k_cache), static_cast<const uint4 *>(v_cache), slots, static_cast<int64_t>(n),
+                            static_cast<int64_t>(d->num_blocks) * d->block_size, kc, vc, static_cast<uint4 *>(k_out),
+                            static_cast<uint4 *>(v_out), err));
+    return FNPU_OK;
+}
+
+int launch_kv8_stage(int format, const fnpu_attn_desc *d, const void *k_pool, const void *v_pool, const Fp8StageJob *jobs,
+                     int32_t num_jobs, void *k_bf16, void *v_bf16, void *stream, bool pdl) {
+    if (num_jobs == 0) return FNPU_OK;
+    auto kernel = format == FNPU_KV_INT8_BLOCK ? kv8_stage_kernel<FNPU_KV_INT8_BLOCK> : kv8_stage_kernel<FNPU_KV_E4M3_BLOCK>;
+    FNPU_CUDA_TRY(launch_ex(kernel, num_jobs * d->num_kv_heads, 128, 0, static_cast<cudaStream_t>(stream), pdl, nullptr,
+                            static_cast<const uint8_t *>(k_pool), static_cast<const uint8_t *>(v_pool), jobs,
+                            static_cast<int>(d->num_kv_heads), static_cast<int>(d->block_size), static_cast<int>(d->head_dim_qk),
+                            static_cast<uint4 *>(k_bf16), static_cast<uint4 *>(v_bf16)));
+    return FNPU_OK;
+}
+
+}  // namespace fnpu

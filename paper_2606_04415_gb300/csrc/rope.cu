@@ -1,0 +1,143 @@
+// Rotary positions on one to four axes, by themselves and on the way into a
+// bf16 paged cache.
+//
+// y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin for each pair of columns, with the
+// angle position[axis(pair)] * inv_freq[pair]; the inverse turns back, which
+// is also the gradient (the rotation is orthogonal). Bound by HBM: 4 bytes a
+// value against some 5 operations, and an angle costs about 40 instructions but
+// serves every head of its token.
+#include "rope.cuh"
+
+namespace fnpu {
+namespace {
+
+constexpr int kWarpsPerCta = 8;
+
+// A warp per token and group of heads_per_warp heads.
+__global__ void __launch_bounds__(32 * kWarpsPerCta)
+    rope_kernel(const __grid_constant__ RopeArgs r, const __nv_bfloat16 *x, int64_t x_stride, int heads, int d,
+                __nv_bfloat16 *out, int64_t out_stride, int groups, int heads_per_warp) {
+    pdl_trigger();
+    pdl_wait();  // writers of x, earlier readers of out
+    const int lane = threadIdx.x & 31;
+    const int64_t w = blockIdx.x * static_cast<int64_t>(kWarpsPerCta) + (threadIdx.x >> 5);
+    const int64_t t = w / groups;
+    if (t >= r.n) return;
+    const int h0 = static_cast<int>(w - t * groups) * heads_per_warp;
+    rope_heads(r, t, h0, min(heads, h0 + heads_per_warp), d, lane,
+               [&](int h) { return x + t * x_stride + static_cast<int64_t>(h) * d; },
+               [&](int h) { return out + t * out_stride + static_cast<int64_t>(h) * d; });
+}
+
+// Any even rotary width, offset, stride and alignment: a thread per pair of a
+// row, then per column that does not turn.
+__global__ void __launch_bounds__(256)
+    rope_any_kernel(const __grid_constant__ RopeArgs r, const __nv_bfloat16 *x, int64_t x_stride, int heads, int d,
+                    __nv_bfloat16 *out, int64_t out_stride) {
+    pdl_trigger();
+    pdl_wait();
+    const int per = d - r.pairs;  // pairs, then plain columns
+    const int64_t total = r.n * heads * per;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+        const int64_t row = i / per, t = row / heads;
+        const int j = static_cast<int>(i - row * per), h = static_cast<int>(row - t * heads);
+        const __nv_bfloat16 *from = x + t * x_stride + static_cast<int64_t>(h) * d;
+        __nv_bfloat16 *to = out + t * out_stride + static_cast<int64_t>(h) * d;
+        if (j < r.pairs) {
+            float s, c;
+            sincospif(2.f * rope_turns(r.positions[r.axis[j] * r.n + t], r.inv_freq[j]), &s, &c);
+            s *= r.sign;
+            const int a = r.offset + (r.interleaved ? 2 * j : j), b = r.interleaved ? a + 1 : a + r.pairs;
+            const float u = __bfloat162float(from[a]), v = __bfloat162float(from[b]);
+            to[a] = __float2bfloat16_rn(u * c - v * s);
+            to[b] = __float2bfloat16_rn(v * c + u * s);
+        } else {
+            const int col = j - r.pairs < r.offset ? j - r.pairs : j + r.pairs;
+            if (to != from) to[col] = from[col];
+        }
+    }
+}
+
+// The append: the query heads and then the key heads of a token are the heads
+// that turn, into q_out and into the token's cache slot; value rows are copied,
+// shared out among the token's warps.
+__global__ void __launch_bounds__(32 * kWarpsPerCta)
+    rope_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int groups,
+                       int heads_per_warp) {
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t w = blockIdx.x * static_cast<int64_t>(kWarpsPerCta) + (threadIdx.x >> 5);
+    const int64_t t = w / groups;
+    if (t >= r.n) return;
+    const int g = static_cast<int>(w - t * groups);
+    const int64_t slot = __ldg(p.slots + t);
+    const bool stored = slot >= 0 && slot < p.num_slots;
+    if (slot >= p.num_slots && g == 0 && lane == 0) atomicOr(p.err, 1);
+    // value rows first: their loads are in flight while the angles are worked out
+    if (stored && p.v_new) {
+        const uint4 *from = reinterpret_cast<const uint4 *>(p.v_new + t * p.v_stride);
+        uint4 *to = reinterpret_cast<uint4 *>(p.v_cache) + slot * (static_cast<int64_t>(p.kv_heads) * p.d_v / 8);
+        for (int i = g * 32 + lane; i < p.kv_heads * p.d_v / 8; i += groups * 32) to[i] = __ldg(from + i);
+    }
+    const int h0 = g * heads_per_warp;
+    rope_heads(r, t, h0, min(p.q_heads + p.kv_heads, h0 + heads_per_warp), p.d, lane,
+               [&](int h) -> const __nv_bfloat16 * {
+                   return h < p.q_heads ? p.q + t * p.q_stride + static_cast<int64_t>(h) * p.d
+                                        : p.k_new + t * p.k_stride + static_cast<int64_t>(h - p.q_heads) * p.d;
+               },
+               [&](int h) -> __nv_bfloat16 * {
+                   if (h < p.q_heads) return p.q_out + (t * p.q_heads + h) * p.d;
+                   return stored ? static_cast<__nv_bfloat16 *>(p.k_cache) + (slot * p.kv_heads + h - p.q_heads) * p.d : nullptr;
+               });
+}
+
+int sm_count() {
+    int dev = 0, sms = 152;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    return sms;
+}
+
+}  // namespace
+
+int rope_heads_per_warp(int64_t n, int heads, int pairs) {
+    // Angles are worked out once per warp, so a warp should have many heads; but
+    // a call of few tokens is its longest chain, and there each warp has one pass.
+    const int hp = 32 / (pairs / 8);
+    const int64_t want = 16ll * sm_count();
+    for (int passes = 8; passes > 1; passes /= 2)
+        if (n * ((heads + hp * passes - 1) / (hp * passes)) >= want) return hp * passes;
+    return hp;
+}
+
+int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, int d, void *out, int64_t out_stride,
+                bool vector, void *stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const __nv_bfloat16 *xp = static_cast<const __nv_bfloat16 *>(x);
+    __nv_bfloat16 *op = static_cast<__nv_bfloat16 *>(out);
+    if (!vector) {
+        const int64_t want = (r.n * heads * (d - r.pairs) + 255) / 256;
+        const int grid = static_cast<int>(want < 64ll * sm_count() ? want : 64ll * sm_count());
+        FNPU_CUDA_TRY(launch_ex(rope_any_kernel, grid, 256, 0, st, true, nullptr, r, xp, x_stride, heads, d, op, out_stride));
+        return FNPU_OK;
+    }
+    const int hpw = rope_heads_per_warp(r.n, heads, r.pairs), groups = (heads + hpw - 1) / hpw;
+    const int64_t ctas = (r.n * groups + kWarpsPerCta - 1) / kWarpsPerCta;
+    if (ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
+    FNPU_CUDA_TRY(launch_ex(rope_kernel, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, st, true, nullptr, r, xp, x_stride, heads, d, op,
+                            out_stride, groups, hpw));
+    return FNPU_OK;
+}
+
+int launch_rope_append(const RopeArgs &r, const RopeAppendArgs &p, void *stream) {
+    const int heads = p.q_heads + p.kv_heads;
+    const int hpw = rope_heads_per_warp(r.n, heads, r.pairs), groups = (heads + hpw - 1) / hpw;
+    const int64_t ctas = (r.n * groups + kWarpsPerCta - 1) / kWarpsPerCta;
+    if (ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
+    FNPU_CUDA_TRY(launch_ex(rope_append_kernel, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, static_cast<cudaStream_t>(stream), true,
+                            nullptr, r, p, groups, hpw));
+    return FNPU_OK;
+}
+
+}  // namespace fnpu

@@ -1,0 +1,137 @@
+// Rotary positions: angles, and the rotation of eight column pairs of a bf16
+// row held in two 16-byte chunks.
+#pragma once
+
+#include "common.cuh"
+
+namespace fnpu {
+
+// Angles. angle = position * inv_freq wants more than 32 bits: at position
+// 100000 the rounded product alone is up to 0.004 rad off. In turns (angle / 2 pi)
+// only the fraction counts, so inv_freq / 2 pi is kept as a sum of two fp32 values
+// (48 bits), the position is cut into two parts that fp32 holds exactly, and each
+// product's whole turns are dropped before anything small is added. What is left is
+// good to 2^-24 turns for positions below 2^20 and goes to sincospif.
+__device__ __forceinline__ float rope_turns(int32_t position, float inv_freq) {
+    constexpr float kHi = 0.15915494f, kLo = 6.4206382e-09f;  // kHi + kLo = 1 / (2 pi) to 2^-53
+    const float f = inv_freq * kHi;
+    const float g = __fmaf_rn(inv_freq, kHi, -f) + inv_freq * kLo;
+    const float a = static_cast<float>(position & ~4095), b = static_cast<float>(position & 4095);
+    const float pa = a * f, pb = b * f;
+    const float lo = (__fmaf_rn(a, f, -pa) + a * g) + (__fmaf_rn(b, f, -pb) + b * g);
+    return ((pa - rintf(pa)) + (pb - rintf(pb))) + lo;
+}
+
+// cosine and sine of pairs 8 c .. 8 c + 7 at token t (inv_freq is 16-byte aligned)
+__device__ __forceinline__ void rope_angles8(const RopeArgs &r, int64_t t, int c, float (&cs)[8], float (&sn)[8]) {
+    int32_t pos[kRopeMaxAxes];
+#pragma unroll
+    for (int a = 0; a < kRopeMaxAxes; ++a) pos[a] = a < r.axes ? __ldg(r.positions + a * r.n + t) : 0;
+    const float4 f0 = __ldg(reinterpret_cast<const float4 *>(r.inv_freq) + 2 * c);
+    const float4 f1 = __ldg(reinterpret_cast<const float4 *>(r.inv_freq) + 2 * c + 1);
+    const float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        int32_t p = pos[0];
+        if (r.axes > 1) {
+            const int a = r.axis[8 * c + i];
+            p = a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : pos[3];
+        }
+        sincospif(2.f * rope_turns(p, f[i]), &sn[i], &cs[i]);
+        sn[i] *= r.sign;
+    }
+}
+
+__device__ __forceinline__ void bf16x8_to_f32(const uint4 &v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ uint4 f32_to_bf16x8(const float (&f)[8]) {
+    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+
+// Where pairs 8 c .. 8 c + 7 lie: columns col_a .. + 7 and col_b .. + 7.
+__device__ __forceinline__ void rope_columns(const RopeArgs &r, int c, int &col_a, int &col_b) {
+    col_a = r.offset + (r.interleaved ? 16 * c : 8 * c);
+    col_b = r.interleaved ? col_a + 8 : col_a + r.pairs;
+}
+
+// The two chunks rotated: y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin in fp32.
+// Half-split pairs have x1 in a and x2 in b; interleaved pairs are neighbours.
+__device__ __forceinline__ void rope_rotate8(bool interleaved, const float (&cs)[8], const float (&sn)[8], float (&a)[8],
+                                             float (&b)[8]) {
+    if (interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = a[2 * i], y = a[2 * i + 1], z = b[2 * i], w = b[2 * i + 1];
+            a[2 * i] = x * cs[i] - y * sn[i];
+            a[2 * i + 1] = y * cs[i] + x * sn[i];
+            b[2 * i] = z * cs[i + 4] - w * sn[i + 4];
+            b[2 * i + 1] = w * cs[i + 4] + z * sn[i + 4];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = a[i], y = b[i];
+            a[i] = x * cs[i] - y * sn[i];
+            b[i] = y * cs[i] + x * sn[i];
+        }
+    }
+}
+
+// One warp rotates heads [h0, h1) of token t: src(h) and dst(h) give the rows
+// (dst null: the head is left out). A lane owns eight pairs, whose angles it
+// works out once for all its heads; the pairs / 8 lanes of a head lie side by
+// side, 32 / (pairs / 8) heads go at a time and kRopeUnroll of them are in flight
+// per lane. Columns that do not turn are copied unless the rows are the same.
+constexpr int kRopeUnroll = 4;
+template <class Src, class Dst>
+__device__ __forceinline__ void rope_heads(const RopeArgs &r, int64_t t, int h0, int h1, int d, int lane, Src src, Dst dst) {
+    const int cp = r.pairs >> 3, hp = 32 / cp;
+    const int lh = lane / cp, c = lane - lh * cp;
+    int ca, cb;
+    rope_columns(r, c, ca, cb);
+    if (lh < hp) {
+        float cs[8], sn[8];
+        uint4 a[kRopeUnroll], b[kRopeUnroll];
+        auto load = [&](int h) {
+#pragma unroll
+            for (int u = 0; u < kRopeUnroll; ++u)
+                if (h + u * hp < h1) {
+                    const __nv_bfloat16 *row = src(h + u * hp);
+                    a[u] = *reinterpret_cast<const uint4 *>(row + ca);
+                    b[u] = *reinterpret_cast<const uint4 *>(row + cb);
+                }
+        };
+        load(h0 + lh);  // in flight while the angles are worked out
+        rope_angles8(r, t, c, cs, sn);
+        for (int h = h0 + lh; h < h1; h += kRopeUnroll * hp) {
+            if (h != h0 + lh) load(h);
+#pragma unroll
+            for (int u = 0; u < kRopeUnroll; ++u)
+                if (h + u * hp < h1) {
+                    __nv_bfloat16 *row = dst(h + u * hp);
+                    if (!row) continue;
+                    float x[8], y[8];
+                    bf16x8_to_f32(a[u], x);
+                    bf16x8_to_f32(b[u], y);
+                    rope_rotate8(r.interleaved != 0, cs, sn, x, y);
+                    *reinterpret_cast<uint4 *>(row + ca) = f32_to_bf16x8(x);
+                    *reinterpret_cast<uint4 *>(row + cb) = f32_to_bf16x8(y);
+                }
+        }
+    }
+    const int pc = (d - 2 * r.pairs) >> 3;  // chunks of a head that do not turn
+    for (int i = lane; i < (h1 - h0) * pc; i += 32) {
+        const int h = h0 + i / pc, j = i % pc, col = 8 * j < r.offset ? 8 * j : 8 * j + 2 * r.pairs;
+        const __nv_bfloat16 *from = src(h);
+        __nv_bfloat16 *to = dst(h);
+        if (to && to != from) *reinterpret_cast<uint4 *>(to + col) = *reinterpret_cast<const uint4 *>(from + col);
+    }
+}
+
+}  // namespace fnpu
