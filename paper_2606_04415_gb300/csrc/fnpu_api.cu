@@ -32,7 +32,7 @@ struct fnpu_plan {
     int32_t num_sms = 0;
     int32_t flags = 0;
     int32_t kv_format = FNPU_KV_BF16;  // 8-bit block formats: fnpu_kv8_attn_plan
-    bool kv8_wide = false;             // ... some sequence has more rows a kv head than the narrow kernel takes
+    int32_t kv8_rows = 8;              // ... rows (query token x query head of a kv head) of a decode item
     bool use_tc = false;
     bool use_dt = false;
     bool use_mla = false;  // latent attention: one work list for both phases
@@ -425,6 +425,47 @@ bool remainder_histogram(const WaveUnits &w, int32_t m, int32_t n, std::vector<i
         hist[static_cast<size_t>(q + kTcItemCost + kTcMergeCost)] += n - r;
     }
     return true;
+}
+
+// Keys of a range of the 8-bit decode, over `slots` CTAs at a time, longest first:
+// the length with the shortest schedule, where an item costs its 16-key tiles and
+// kKv8ItemTiles for its start and end (its CTA's first loads, the meeting of its
+// warps, the partial result). `each(add)` gives add(keys, items) of every
+// sequence. One wave of equal items is best where there is one (64 decodes of
+// 512..4096 keys, 4 kv heads: 592 items 34.0 us, 772 38.7, 1140 35.9); beyond,
+// what the last items last weighs against the starts (128 of 128..8192: 4096-key
+// ranges 112 us, 2048 99.8, 1024 104; 256 of 500..8000, 8 kv heads: 323, 328, 347).
+constexpr int32_t kKv8ItemTiles = 14;
+template <typename Each>
+int32_t kv8_split(Each each, int32_t slots) {
+    std::vector<int32_t> hist;
+    // the shortest that makes one wave
+    int32_t one_wave = kKv8MaxItemKeys;
+    for (int32_t lo = 4, hi = kKv8MaxItemKeys / 64; lo < hi;) {
+        const int32_t mid = (lo + hi) / 2;
+        int64_t n = 0;
+        each([&](int32_t keys, int64_t items) { n += (keys + 64 * mid - 1) / (64 * mid) * items; });
+        if (n <= slots) hi = mid;
+        else lo = mid + 1;
+        one_wave = 64 * hi;
+    }
+    int32_t best_keys = one_wave;
+    int64_t best = INT64_MAX;
+    for (int32_t sk : {one_wave, 256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
+        hist.assign(kKv8MaxItemKeys / 16 + kKv8ItemTiles + 1, 0);
+        each([&](int32_t keys, int64_t items) {
+            const int32_t n = (keys + sk - 1) / sk, tiles = (keys + 15) / 16;
+            const int64_t all = n * items;
+            if (all > INT32_MAX / 2) return;
+            hist[static_cast<size_t>((tiles + n - 1) / n + kKv8ItemTiles)] += static_cast<int32_t>(all);
+        });
+        const int64_t span = lpt_makespan(hist, slots, best);
+        if (span < best) {
+            best = span;
+            best_keys = sk;
+        }
+    }
+    return best_keys;
 }
 
 // Number of key splits per unit. A persistent CTA per SM takes items longest
@@ -847,13 +888,14 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
         return it;
     };
     int64_t dec_keys = 0, num_dec = 0;
-    pl->kv8_wide = false;
+    int64_t kv8_rows = 1;
     for (int32_t s = 0; s < num_seqs; ++s)
         if (decode_queue(s)) {
             dec_keys += context_len[s];
             ++num_dec;
-            pl->kv8_wide |= kv8 && query_len[s] * G > kv8_rows_per_item(false);
+            kv8_rows = std::max(kv8_rows, static_cast<int64_t>(query_len[s]) * G);
         }
+    pl->kv8_rows = kv8_rows_per_item(kv8_rows);
     if (pl->use_dt && !kv8 && desc->num_kv_heads <= 2 && desc->head_dim_qk == 64 && o.decode_share_pct == 0 &&
         !(o.flags & FNPU_PLAN_GREEN_CONTEXTS)) {
         // One or two 64-wide kv heads leave three or two of the TMA kernel's four
@@ -867,11 +909,18 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
                                              : num_dec < 2LL * sms || dec_keys < 256 * num_dec;
     }
     // items per key range: one per group of kv heads (TMA kernel), one per kv head
-    const int32_t hpi = kv8 ? kv8_heads_per_item(desc->num_kv_heads) : pl->use_dt ? decode_tma_heads_per_item() : 1;
+    const int32_t hpi = pl->use_dt && !kv8 ? decode_tma_heads_per_item() : 1;
     const int32_t hgroups = (desc->num_kv_heads + hpi - 1) / hpi;
     dec_keys *= hgroups;
     int32_t split = std::min(o.decode_split_keys, 1 << 30);  // (room to round up)
-    if (split == 0) {
+    if (kv8 && split == 0) {
+        split = kv8_split([&](auto add) {
+            for (int32_t s = 0; s < num_seqs; ++s)
+                if (decode_queue(s))
+                    add(context_len[s], static_cast<int64_t>(desc->num_kv_heads) *
+                                            ((static_cast<int64_t>(query_len[s]) * G + pl->kv8_rows - 1) / pl->kv8_rows));
+        }, sms * (pl->kv8_rows == 8 ? 4 : pl->kv8_rows == 16 ? 3 : 2));
+    } else if (split == 0) {
         const int64_t target = (pl->use_dt ? 2LL : 6LL) * sms;
         int64_t sk = (dec_keys + target - 1) / std::max<int64_t>(target, 1);
         sk = (sk + 63) / 64 * 64;
@@ -1001,23 +1050,25 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
                 }
             }
         } else if (decode_queue(s) && kv8) {
-            // as below; each split has a partial for every key part of the CTA (with
-            // fewer than four kv heads an item), each token its merge, and the rows of a
-            // kv head beyond the kernel's go to items of their own beside each other
-            const int32_t rows = q * G, per = kv8_rows_per_item(pl->kv8_wide), kparts = 4 / hpi;
-            const int32_t sk = std::max((split + 15) / 16 * 16, (c + 256 / kparts * 64 - 1) / (256 / kparts * 64) * 64);
-            const int32_t ns = (c + sk - 1) / sk * kparts;
-            const int32_t base = ns > 1 ? parts : 0;
-            for (int32_t i = 0; i < q && ns > 1; ++i) {
-                mgroups.push_back(MergeGroup{qs + i, ns, parts, 0});
-                parts += ns;
-            }
-            for (int32_t sp = 0; sp * sk < c; ++sp)
-                for (int32_t hg = 0; hg < hgroups; ++hg)
-                    for (int32_t r0 = 0; r0 < rows; r0 += per) {
-                        ditems.push_back(decode_item(s, hg * hpi, sp * sk, std::min(c, (sp + 1) * sk), sp * kparts, ns, base, c));
-                        ditems.back().row_begin = r0;
+            // an item for each key range, kv head and kv8_rows rows; the last CTA
+            // of a split group merges it
+            const int32_t rows = q * G, most = std::min((split + 15) / 16 * 16, kKv8MaxItemKeys), want = (c + most - 1) / most;
+            const int32_t sk = ((c + want - 1) / want + 15) / 16 * 16, ns = (c + sk - 1) / sk;  // even pieces, of whole tiles
+            for (int32_t kvh = 0; kvh < desc->num_kv_heads; ++kvh)
+                for (int32_t r0 = 0; r0 < rows; r0 += pl->kv8_rows) {
+                    const int32_t base = ns > 1 ? parts : 0, grp = ns > 1 ? groups : 0;
+                    const int32_t merged = ns > kKv8MergeAtOnce ? (ns + kKv8MergeGroup - 1) / kKv8MergeGroup : 0;
+                    if (ns > 1) {
+                        parts += ns + merged;
+                        groups += 1 + merged;
                     }
+                    for (int32_t sp = 0; sp < ns; ++sp) {
+                        DecodeItem it = decode_item(s, kvh, sp * sk, std::min(c, (sp + 1) * sk), sp, ns, base, grp);
+                        it.row_begin = r0;
+                        it.blk[0] = c;
+                        ditems.push_back(it);
+                    }
+                }
         } else if (decode_queue(s) && pl->use_dt) {
             // items over groups of kv heads, cut at whole 16-key stages; a
             // split sequence is merged by the merge kernel (at most 256
@@ -1289,9 +1340,10 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     const size_t o_ftok = off; off = align_up(off + sizeof(int32_t) * std::max<size_t>(ftok.size(), 1), 256);
     const size_t o_dtok = off; off = align_up(off + sizeof(int32_t) * std::max<size_t>(dtok.size(), 1), 256);
     const size_t meta_bytes = off;
-    // query heads per partial
+    // query heads (8-bit blocks: rows) per partial
     const int32_t part_rows = pl->use_mla_tc ? desc->num_q_heads
                               : pl->use_mla  ? mla_heads_per_item()
+                              : kv8          ? pl->kv8_rows
                                              : (pl->use_dt ? desc->num_q_heads : G);
     const size_t o_plse = off; off = align_up(off + sizeof(float) * static_cast<size_t>(std::max(parts, 1)) * part_rows, 256);
     const size_t o_po = off; off = align_up(off + sizeof(float) * static_cast<size_t>(std::max(parts, 1)) * part_rows * desc->head_dim_v, 256);
@@ -1539,7 +1591,7 @@ bool run_pointers_ok(const fnpu_plan *pl, const void *q, const void *k_cache, co
 
 // The decode kernel of a plan and its merge, on `stream`.
 int launch_decode(const fnpu_plan *pl, const AttnParams &p, void *stream, int ctas) {
-    if (pl->kv_format != FNPU_KV_BF16) return launch_decode_kv8(pl->kv_format, p, pl->kv8_wide, stream, ctas, false);
+    if (pl->kv_format != FNPU_KV_BF16) return launch_decode_kv8(pl->kv_format, p, pl->kv8_rows, stream, false);
     return pl->desc.kv_fp8 ? launch_decode_fp8(p, stream, ctas, false) : launch_decode_tma(p, stream, ctas, false);
 }
 
@@ -1633,7 +1685,7 @@ int fnpu_mixed_attn_run(const fnpu_plan *pl, const void *q, const void *k_cache,
     if (pl->use_mla) return pl->use_mla_tc ? launch_mla_tc(p, stream, pl->num_sms) : launch_mla(p, stream);
     if (pl->coloc) return run_colocated(pl, p, stream);
     int rc = pl->kv_format != FNPU_KV_BF16
-                 ? launch_decode_kv8(pl->kv_format, p, pl->kv8_wide, stream, 3 * pl->num_sms, true)
+                 ? launch_decode_kv8(pl->kv_format, p, pl->kv8_rows, stream, true)
              : pl->desc.kv_fp8 ? launch_decode_fp8(p, stream, 3 * pl->num_sms, true)
              : pl->use_dt    ? launch_decode_tma(p, stream, 3 * pl->num_sms, true)
                              : launch_decode_mma(p, stream);

@@ -17,10 +17,9 @@ namespace fnpu {
 // to scratch rows part_base + split. The item also carries its sequence's
 // query token and block-table row and the ids of its first four blocks, so
 // that a kernel can issue its first copies after one load.
-// 8-bit block kernel: the item is rows [row_begin, row_begin + rows a kernel takes)
-// of the q_len x G rows (token, query head of the kv head) of the sequence, `group`
-// is its context length and `split` its first partial of each token (one for each
-// of the CTA's key parts).
+// 8-bit block kernel: the item is rows [row_begin, row_begin + the rows that the
+// kernel takes) of the q_len x G rows (token, query head of the kv head) of the
+// sequence, at most kKv8MaxItemKeys keys; blk[0] is the sequence's context length.
 struct DecodeItem {
     int32_t seq, kvh, key_begin, key_end;
     int32_t split, num_splits, part_base, group;
@@ -224,9 +223,13 @@ int launch_kv_read_bf16(const fnpu_attn_desc *d, const int64_t *slots, int32_t n
                         void *k_out, void *v_out, int *err, void *stream);
 int launch_kv8_stage(int format, const fnpu_attn_desc *d, const void *k_pool, const void *v_pool, const Fp8StageJob *jobs,
                      int32_t num_jobs, void *k_bf16, void *v_bf16, void *stream, bool pdl);
-int launch_decode_kv8(int format, const AttnParams &p, bool wide, void *stream, int max_ctas, bool alone);
-int kv8_heads_per_item(int hkv);  // kv heads of an item; 4 / this key parts
-int kv8_rows_per_item(bool wide);
+// (rows: of an item, from kv8_rows_per_item of the largest sequence's)
+int launch_decode_kv8(int format, const AttnParams &p, int rows, void *stream, bool alone);
+int kv8_rows_per_item(int64_t rows);
+constexpr int kKv8MaxItemKeys = 4096;
+// Ranges of a sequence that one CTA merges; more are merged in groups first, which
+// have a counter each behind the sequence's and a partial result each behind its ranges'.
+constexpr int kKv8MergeAtOnce = 12, kKv8MergeGroup = 8;
 bool decode_fp8_supported(int d_qk, int d_v, int hkv, int group, int block_size);
 int launch_decode_mma(const AttnParams &p, void *stream);
 int launch_decode_tma(const AttnParams &p, void *stream, int max_ctas, bool alone);

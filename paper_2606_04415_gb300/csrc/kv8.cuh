@@ -76,20 +76,21 @@ __device__ __forceinline__ void decode4(uint32_t w, float (&f)[4]) {
     }
 }
 
-// Two codes (bytes i and j of w) as f16, exactly. INT8: 1024 + code is the f16 with
-// the code as its low byte; less 1152.
-template <int kFormat, int kI, int kJ>
-__device__ __forceinline__ uint32_t codes_f16x2(uint32_t w) {
+// Four codes as f16, exactly: neighbouring bytes in pairs (0, 1) and (2, 3), or with
+// kAcross bytes (0, 2) and (1, 3). INT8: 1024 + code is the f16 with the code as its
+// low byte; less 1152.
+template <int kFormat, bool kAcross>
+__device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t &a, uint32_t &b) {
     if constexpr (kFormat == FNPU_KV_INT8_BLOCK) {
-        const uint32_t h = __byte_perm(w, 0x64646464u, 0x4040 | kI | kJ << 8);
+        const uint32_t x = __byte_perm(w, 0x64646464u, kAcross ? 0x4240 : 0x4140);
+        const uint32_t y = __byte_perm(w, 0x64646464u, kAcross ? 0x4341 : 0x4342);
         const uint32_t k = 0x64806480u;
-        const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&h), *reinterpret_cast<const __half2 *>(&k));
-        return *reinterpret_cast<const uint32_t *>(&v);
+        const __half2 u = __hsub2(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&k));
+        const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&y), *reinterpret_cast<const __half2 *>(&k));
+        a = *reinterpret_cast<const uint32_t *>(&u);
+        b = *reinterpret_cast<const uint32_t *>(&v);
     } else {
-        uint32_t r;
-        const uint16_t two = static_cast<uint16_t>(__byte_perm(w, 0, kI | kJ << 4));
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(r) : "h"(two));
-        return r;
+        e4m3x4_to_f16x2x2(kAcross ? __byte_perm(w, 0, 0x3120) : w, a, b);
     }
 }
 
