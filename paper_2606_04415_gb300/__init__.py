@@ -157,6 +157,11 @@ def status_str(code: int) -> str:
 
 def _dptr(x) -> Optional[int]:
     """Device address of a CUDA tensor / raw int / None."""
+    try:  # a tensor as it should be, first
+        if x.is_cuda and x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:
+        pass
     if x is None:
         return None
     if isinstance(x, int):
@@ -171,17 +176,20 @@ def _dptr(x) -> Optional[int]:
 
 
 _raw_stream = None  # (device index) -> raw handle of torch's current stream
+_current_device = None  # () -> index of the current device
 
 
 def _current_stream() -> int:
     """Raw handle of torch's current stream on the current device, without
     building a Stream object for it (3.1 us a call, against 0.6)."""
-    global _raw_stream
-    import torch
+    global _raw_stream, _current_device
     if _raw_stream is None:
+        import torch
+        torch.cuda.current_device()  # (torch's own start, before its inner functions are called)
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _raw_stream = get or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(_current_device())
 
 
 def _stream(stream) -> Optional[int]:
@@ -402,14 +410,16 @@ def _types():
     return _dtypes
 
 
-def _rows(x):
-    """Address and token stride of bf16 rows [n, heads, d] whose tokens may lie
-    apart (a slice of a fused projection's output)."""
+def _rows(x, tokens: int):
+    """Address and token stride of bf16 rows [tokens, heads, d] whose tokens may
+    lie apart (a slice of a fused projection's output)."""
     if not x.is_cuda:
         raise ValueError("expected a CUDA tensor")
     if x.dtype is not _types()[0]:
         raise TypeError("rows are bf16")
     n, h, d = x.shape
+    if n != tokens:
+        raise ValueError("rows, positions and slots have the same number of tokens")
     s, t, u = x.stride()
     if (u != 1 and d > 1) or (t != d and h > 1):
         raise ValueError("the heads and columns of a token must be contiguous")
@@ -431,7 +441,7 @@ def rope(desc: RopeDesc, inv_freq, positions, x, out=None, stream=None) -> None:
     if tuple(out.shape) != (n, h, d):
         raise ValueError("out has the shape of x")
     _check_positions(desc, inv_freq, positions, n)
-    (xp, xs), (op, os_) = _rows(x), _rows(out)
+    (xp, xs), (op, os_) = _rows(x, n), _rows(out, n)
     rc = load().fnpu_rope(ctypes.byref(desc), _dptr(inv_freq), _dptr(positions), xp, xs, h, d, n, op, os_, _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_rope")
@@ -442,13 +452,13 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
     """Rotate the step's queries into ``q_out`` and its keys into their cache
     slots, and store its values (``fnpu_rope_append``); q, k_new and v_new are
     [n, heads, d], their tokens possibly apart. ``rope`` None: rows as they are."""
-    n = int(slot_mapping.shape[0])
-    if any(x is not None and int(x.shape[0]) != n for x in (q, k_new, v_new)):
-        raise ValueError("q, k_new, v_new and slot_mapping have the same number of tokens")
+    n = slot_mapping.numel()
     if rope is not None:
         _check_positions(rope, inv_freq, positions, n)
-    (qp, qs), (kp, ks), (vp, vs) = ((None, 0) if x is None else _rows(x) for x in (q, k_new, v_new))
-    rc = load().fnpu_rope_append(ctypes.byref(desc), int(kv_format), None if rope is None else ctypes.byref(rope),
+    qp, qs = (None, 0) if q is None else _rows(q, n)
+    kp, ks = _rows(k_new, n)
+    vp, vs = (None, 0) if v_new is None else _rows(v_new, n)
+    rc = (_lib or load()).fnpu_rope_append(ctypes.byref(desc), int(kv_format), None if rope is None else ctypes.byref(rope),
                                  _dptr(inv_freq), _dptr(positions), qp, qs, kp, ks, vp, vs, _dptr(slot_mapping), n,
                                  _dptr(q_out), _dptr(k_cache), _dptr(v_cache), _stream(stream))
     if rc != FNPU_OK:

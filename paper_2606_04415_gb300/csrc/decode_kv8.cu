@@ -147,20 +147,26 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, kN>::kCtas) decode_kv8_kernel
     uint32_t qb[kN == 4 ? 1 : kN][D / 16][2];
     uint8_t *q_sh = smem + C::kQOff;  // [row tile][column pair c][lane]: 16 bytes, columns 32 c + 4 t4 .. + 3 and + 16
     float o[kN][D / 16][4], m[kN][2], l[kN][2], qs[kN][2];
-#pragma unroll
-    for (int n = 0; n < kN; ++n) {
+    auto query = [&](int n, uint32_t(&to)[D / 16][2]) -> float {  // row tile n: operands, and the scale of this lane's row
         const int row = it.row_begin + 8 * n + g8;
         const __nv_bfloat16 *src = q + (static_cast<int64_t>(it.q_start + row / G) * Hq + it.kvh * G + row % G) * D;
-        const float down = load_q<D>(src, row < rows, t4, qb[kN == 4 ? 0 : n]);
-        if (kN == 4 && warp == 0) {
+        return load_q<D>(src, row < rows, t4, to) * p.scale_log2;
+    };
+    if constexpr (kN == 4) {  // a row tile each for the four warps, through shared memory
+        const float down = query(warp, qb[0]);
+        if (t4 == 0) m_sh[8 * warp + g8] = down;
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c)
-                *reinterpret_cast<uint4 *>(q_sh + ((n * (D / 32) + c) * 32 + lane) * 16) =
-                    make_uint4(qb[0][2 * c][0], qb[0][2 * c][1], qb[0][2 * c + 1][0], qb[0][2 * c + 1][1]);
-        }
+        for (int c = 0; c < D / 32; ++c)
+            *reinterpret_cast<uint4 *>(q_sh + ((warp * (D / 32) + c) * 32 + lane) * 16) =
+                make_uint4(qb[0][2 * c][0], qb[0][2 * c][1], qb[0][2 * c + 1][0], qb[0][2 * c + 1][1]);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+        const float down = kN == 4 ? 0.f : query(n, qb[kN == 4 ? 0 : n]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            qs[n][e] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e)) * p.scale_log2;
+            qs[n][e] = kN == 4 ? m_sh[8 * n + 2 * t4 + e] : __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e));
             m[n][e] = mine > 0 ? 0.f : kNoMax;  // (a warp without a tile: nothing)
             l[n][e] = 0.f;
         }

@@ -427,45 +427,56 @@ bool remainder_histogram(const WaveUnits &w, int32_t m, int32_t n, std::vector<i
     return true;
 }
 
-// Keys of a range of the 8-bit decode, over `slots` CTAs at a time, longest first:
-// the length with the shortest schedule, where an item costs its 16-key tiles and
-// kKv8ItemTiles for its start and end (its CTA's first loads, the meeting of its
-// warps, the partial result). `each(add)` gives add(keys, items) of every
-// sequence. One wave of equal items is best where there is one (64 decodes of
-// 512..4096 keys, 4 kv heads: 592 items 34.0 us, 772 38.7, 1140 35.9); beyond,
-// what the last items last weighs against the starts (128 of 128..8192: 4096-key
-// ranges 112 us, 2048 99.8, 1024 104; 256 of 500..8000, 8 kv heads: 323, 328, 347).
+// Ranges of the 8-bit decode. An item costs its 16-key tiles and kKv8ItemTiles for
+// its start and end (its CTA's first loads, the meeting of its warps, the partial
+// result); the schedule is longest first on the CTAs that fit the device. One wave of
+// equal items is best where there is one (64 decodes of 512..4096 keys, 4 kv heads:
+// 592 items 34.0 us, 772 38.7, 1140 35.9); beyond, what the last items last weighs
+// against the starts (128 of 128..8192: 4096-key ranges 112 us, 2048 99.8, 1024
+// 104; 256 of 500..8000, 8 kv heads: 323, 328, 347).
+// The rows of a kv head (query token x query head) may go to items of 8, 16 or 32:
+// wide items read the codes once for more rows, narrow ones have a shorter chain a
+// tile (kKv8TileCost, in 1/20 of the narrow one's) and more CTAs an SM. (16 sequences
+// of 4 x 7 rows on 2000..30000 keys: 75 us in 32, 96 in 16; 3 of 9 x 7 on 200: 12.0 and
+// 8.1. 32 of 2 x 7 on 700..5000: 28.7 in 16, 31.7 in 8; 4 of them 15.0 and 13.2.)
 constexpr int32_t kKv8ItemTiles = 14;
+struct Kv8Split {
+    int32_t rows, keys;
+};
+// `each(add)` gives add(keys, kv heads, rows a kv head) of every sequence, the most
+// rows being max_rows.
 template <typename Each>
-int32_t kv8_split(Each each, int32_t slots) {
-    std::vector<int32_t> hist;
-    // the shortest that makes one wave
-    int32_t one_wave = kKv8MaxItemKeys;
-    for (int32_t lo = 4, hi = kKv8MaxItemKeys / 64; lo < hi;) {
-        const int32_t mid = (lo + hi) / 2;
-        int64_t n = 0;
-        each([&](int32_t keys, int64_t items) { n += (keys + 64 * mid - 1) / (64 * mid) * items; });
-        if (n <= slots) hi = mid;
-        else lo = mid + 1;
-        one_wave = 64 * hi;
-    }
-    int32_t best_keys = one_wave;
-    int64_t best = INT64_MAX;
-    for (int32_t sk : {one_wave, 256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
-        hist.assign(kKv8MaxItemKeys / 16 + kKv8ItemTiles + 1, 0);
-        each([&](int32_t keys, int64_t items) {
-            const int32_t n = (keys + sk - 1) / sk, tiles = (keys + 15) / 16;
-            const int64_t all = n * items;
-            if (all > INT32_MAX / 2) return;
-            hist[static_cast<size_t>((tiles + n - 1) / n + kKv8ItemTiles)] += static_cast<int32_t>(all);
-        });
-        const int64_t span = lpt_makespan(hist, slots, best);
-        if (span < best) {
-            best = span;
-            best_keys = sk;
+Kv8Split kv8_split(Each each, int64_t max_rows, int32_t sms) {
+    thread_local std::vector<int32_t> hist;
+    Kv8Split best{kv8_rows_per_item(max_rows), kKv8MaxItemKeys};
+    int64_t least = INT64_MAX;
+    for (int32_t rows = 8; rows <= kv8_rows_per_item(max_rows); rows *= 2) {
+        const int32_t slots = sms * (rows == 8 ? 4 : rows == 16 ? 3 : 2), cost = rows == 8 ? 20 : rows == 16 ? 24 : 29;
+        int32_t one_wave = kKv8MaxItemKeys;  // the shortest ranges that make one wave
+        for (int32_t lo = 4, hi = kKv8MaxItemKeys / 64; lo < hi;) {
+            const int32_t mid = (lo + hi) / 2;
+            int64_t n = 0;
+            each([&](int32_t keys, int64_t heads, int64_t r) { n += (keys + 64 * mid - 1) / (64 * mid) * heads * ((r + rows - 1) / rows); });
+            if (n <= slots) hi = mid;
+            else lo = mid + 1;
+            one_wave = 64 * hi;
+        }
+        for (int32_t sk : {one_wave, 256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
+            hist.assign(kKv8MaxItemKeys / 16 + kKv8ItemTiles + 1, 0);
+            each([&](int32_t keys, int64_t heads, int64_t r) {
+                const int32_t n = (keys + sk - 1) / sk, tiles = (keys + 15) / 16;
+                const int64_t items = n * heads * ((r + rows - 1) / rows);
+                int32_t &h = hist[static_cast<size_t>((tiles + n - 1) / n + kKv8ItemTiles)];
+                h = static_cast<int32_t>(std::min<int64_t>(h + items, INT32_MAX));
+            });
+            const int64_t span = lpt_makespan(hist, slots, (least - 1) / cost + 1);
+            if (span * cost < least) {
+                least = span * cost;
+                best = {rows, sk};
+            }
         }
     }
-    return best_keys;
+    return best;
 }
 
 // Number of key splits per unit. A persistent CTA per SM takes items longest
@@ -895,7 +906,6 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
             ++num_dec;
             kv8_rows = std::max(kv8_rows, static_cast<int64_t>(query_len[s]) * G);
         }
-    pl->kv8_rows = kv8_rows_per_item(kv8_rows);
     if (pl->use_dt && !kv8 && desc->num_kv_heads <= 2 && desc->head_dim_qk == 64 && o.decode_share_pct == 0 &&
         !(o.flags & FNPU_PLAN_GREEN_CONTEXTS)) {
         // One or two 64-wide kv heads leave three or two of the TMA kernel's four
@@ -913,13 +923,15 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     const int32_t hgroups = (desc->num_kv_heads + hpi - 1) / hpi;
     dec_keys *= hgroups;
     int32_t split = std::min(o.decode_split_keys, 1 << 30);  // (room to round up)
-    if (kv8 && split == 0) {
-        split = kv8_split([&](auto add) {
+    Kv8Split kv8_plan{8, 0};
+    if (kv8)
+        kv8_plan = kv8_split([&](auto add) {
             for (int32_t s = 0; s < num_seqs; ++s)
-                if (decode_queue(s))
-                    add(context_len[s], static_cast<int64_t>(desc->num_kv_heads) *
-                                            ((static_cast<int64_t>(query_len[s]) * G + pl->kv8_rows - 1) / pl->kv8_rows));
-        }, sms * (pl->kv8_rows == 8 ? 4 : pl->kv8_rows == 16 ? 3 : 2));
+                if (decode_queue(s)) add(context_len[s], desc->num_kv_heads, static_cast<int64_t>(query_len[s]) * G);
+        }, kv8_rows, sms);
+    pl->kv8_rows = kv8_plan.rows;
+    if (kv8 && split == 0) {
+        split = kv8_plan.keys;
     } else if (split == 0) {
         const int64_t target = (pl->use_dt ? 2LL : 6LL) * sms;
         int64_t sk = (dec_keys + target - 1) / std::max<int64_t>(target, 1);

@@ -208,7 +208,7 @@ int launch_fp8_stage(const void *k_pool, const void *v_pool, const Fp8StageJob *
 // Rotary positions. vector: rows may be read in 16-byte chunks of eight pairs.
 int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, int d, void *out, int64_t out_stride,
                 bool vector, void *stream);
-int rope_heads_per_warp(int64_t n, int heads, int pairs);
+int rope_heads_per_warp(int64_t n, int heads, int pairs, int d);
 int launch_rope_append(const RopeArgs &r, const RopeAppendArgs &p, void *stream);
 // 8-bit cache with a scale for each (block, kv head), format FNPU_KV_INT8_BLOCK or
 // FNPU_KV_E4M3_BLOCK: append (turning rows where r.pairs > 0), rows read back as

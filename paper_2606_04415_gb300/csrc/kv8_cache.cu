@@ -14,27 +14,24 @@ namespace {
 // block has, store the rows before the run anew. A block whose slot 0 is in the
 // run is a fresh one; what it held and its scale are dead.
 //
-// A warp has 16 rows of the block (a run of a 64-slot block is four warps' work): 16
-// columns a lane, the eight pairs that a lane turns among them, so that K rows are
-// turned and stored in one pass through registers. Every (token, kv head, side)
-// has a place in the grid and those that do not begin a run leave at once: no list
-// of runs to build, and a decode step, whose rows are all runs of one, has a warp
-// for each. The queries are turned by further CTAs of the same launch.
-constexpr int kRowsPerWarp = 16;
-
+// A CTA has a warp for each 512 values of a block and kv head, 16 columns a lane (the
+// eight pairs that a lane turns among them), so that rows are loaded, turned and
+// stored in one pass through few registers; its warps meet once, for the largest
+// magnitude. It looks for runs that begin in a window of tokens, one token while the
+// grid is one wave: no list of runs to build, and a decode step, whose rows are all
+// runs of one, has a CTA for each. The queries are turned by further CTAs of the
+// same launch.
 template <int kFormat, int kD>
 __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendArgs &p, int64_t t, int64_t slot, int n, int head,
-                                           bool is_v, int part, int parts, int lane, uint32_t *amax_sh) {
-    constexpr int kLanesPerRow = kD / 16, kPass = 32 / kLanesPerRow, kPasses = kRowsPerWarp / kPass;
+                                           bool is_v, uint32_t *amax_sh) {
+    constexpr int kLanesPerRow = kD / 16, kRows = 32 / kLanesPerRow;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int bs = p.block_size;
-    const int off = static_cast<int>(slot % bs);
+    const int off = static_cast<int>(slot & (bs - 1));
     uint8_t *blk = static_cast<uint8_t *>(is_v ? p.v_cache : p.k_cache) + slot / bs * kv8::block_bytes(p.kv_heads, bs, kD);
-    uint8_t *rows = blk + static_cast<int64_t>(head) * bs * kD;
     float *scale = reinterpret_cast<float *>(blk + static_cast<int64_t>(p.kv_heads) * bs * kD) + head;
     const int e_old = off > 0 ? kv8::scale_exp(*scale) : kv8::kMinExp;
-    const __nv_bfloat16 *src = is_v ? p.v_new : p.k_new;
-    const int64_t stride = is_v ? p.v_stride : p.k_stride;
-    const int c = lane % kLanesPerRow, lr = lane / kLanesPerRow;
+    const int o = warp * kRows + lane / kLanesPerRow, c = lane % kLanesPerRow;  // this lane's row and columns
     const int cp = is_v ? 0 : r.pairs >> 3;
     int ca, cb;
     if (c < cp) {
@@ -44,95 +41,80 @@ __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendAr
         if (cp > 0 && ca >= r.offset) ca += 2 * r.pairs;
         cb = ca + 8;
     }
-    float a[kPasses][8], b[kPasses][8];
-    uint4 ra[kPasses], rb[kPasses];
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        const int o = part * kRowsPerWarp + i * kPass + lr;
-        ra[i] = rb[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (o >= off && o < off + n) {
-            const __nv_bfloat16 *row = src + (t + o - off) * stride + static_cast<int64_t>(head) * kD;
-            ra[i] = __ldg(reinterpret_cast<const uint4 *>(row + ca));
-            rb[i] = __ldg(reinterpret_cast<const uint4 *>(row + cb));
+    uint8_t *row = blk + (static_cast<int64_t>(head) * bs + o) * kD;
+    const bool fresh = o >= off && o < off + n;
+    float a[8], b[8];
+    {
+        uint4 ra = make_uint4(0u, 0u, 0u, 0u), rb = ra;
+        if (fresh) {
+            const __nv_bfloat16 *src = (is_v ? p.v_new : p.k_new) + (t + o - off) * (is_v ? p.v_stride : p.k_stride) +
+                                       static_cast<int64_t>(head) * kD;
+            ra = __ldg(reinterpret_cast<const uint4 *>(src + ca));
+            rb = __ldg(reinterpret_cast<const uint4 *>(src + cb));
         }
+        float cs[8], sn[8];
+        if (fresh && c < cp) rope_angles8(r, t + o - off, c, cs, sn);  // while the row comes
+        bf16x8_to_f32(ra, a);
+        bf16x8_to_f32(rb, b);
+        if (fresh && c < cp) rope_rotate8(r.interleaved != 0, cs, sn, a, b);
     }
     float amax = 0.f;
     bool odd = false;  // a value that is not finite
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        const int o = part * kRowsPerWarp + i * kPass + lr;
-        bf16x8_to_f32(ra[i], a[i]);
-        bf16x8_to_f32(rb[i], b[i]);
-        if (c < cp && o >= off && o < off + n) {
-            float cs[8], sn[8];
-            rope_angles8(r, t + o - off, c, cs, sn);
-            rope_rotate8(r.interleaved != 0, cs, sn, a[i], b[i]);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = fabsf(a[i][j]), y = fabsf(b[i][j]);
-            odd |= !(x < INFINITY) | !(y < INFINITY);
-            amax = fmaxf(amax, fmaxf(x, y));
-        }
+    for (int j = 0; j < 8; ++j) {
+        const float x = fabsf(a[j]), y = fabsf(b[j]);
+        odd |= !(x < INFINITY) | !(y < INFINITY);
+        amax = fmaxf(amax, fmaxf(x, y));
     }
     if (odd) {  // NaN is stored as zero, an infinity as the largest magnitude that the others allow
         amax = 0.f;
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (a[i][j] != a[i][j]) a[i][j] = 0.f;
-                if (b[i][j] != b[i][j]) b[i][j] = 0.f;
-                if (fabsf(a[i][j]) < INFINITY) amax = fmaxf(amax, fabsf(a[i][j]));
-                if (fabsf(b[i][j]) < INFINITY) amax = fmaxf(amax, fabsf(b[i][j]));
-            }
+        for (int j = 0; j < 8; ++j) {
+            if (a[j] != a[j]) a[j] = 0.f;
+            if (b[j] != b[j]) b[j] = 0.f;
+            if (fabsf(a[j]) < INFINITY) amax = fmaxf(amax, fabsf(a[j]));
+            if (fabsf(b[j]) < INFINITY) amax = fmaxf(amax, fabsf(b[j]));
+        }
         atomicOr(p.err, 8);
     }
     uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));  // (non-negative floats order as integers)
-    if (parts > 1) {
-        if (lane == 0) amax_sh[part] = top;
-        __syncthreads();  // (every warp of the CTA has the same run; all have read the old scale)
-        for (int i = 0; i < parts; ++i) top = max(top, amax_sh[i]);
-        __syncthreads();
-    }
+    if (lane == 0) amax_sh[warp] = top;
+    __syncthreads();  // (also: every warp has the old scale)
+    for (int i = 0; i < warps; ++i) top = max(top, amax_sh[i]);
     int e = max(e_old, kv8::required_exp<kFormat>(__uint_as_float(top)));
     if (e > kv8::kMaxExp) {
         e = kv8::kMaxExp;
         if (lane == 0) atomicOr(p.err, 8);
     }
-    const float inv = kv8::pow2(-e);
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-        const int o = part * kRowsPerWarp + i * kPass + lr;
-        if (o >= off && o < off + n) {
-            *reinterpret_cast<uint2 *>(rows + o * kD + ca) = kv8::encode8<kFormat>(a[i], inv);
-            *reinterpret_cast<uint2 *>(rows + o * kD + cb) = kv8::encode8<kFormat>(b[i], inv);
-        } else if (o < off && e > e_old) {  // a row that the block held before, over the grown scale
-            const float down = kv8::pow2(e_old - e);
-            for (int s = 0; s < 2; ++s) {
-                uint2 *at = reinterpret_cast<uint2 *>(rows + o * kD + (s ? cb : ca));
-                const uint2 w = *at;
-                float x[4], y[4];
-                kv8::decode4<kFormat>(w.x, x);
-                kv8::decode4<kFormat>(w.y, y);
-                const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-                *at = kv8::encode8<kFormat>(f, down);
-            }
+    if (fresh) {
+        const float inv = kv8::pow2(-e);
+        *reinterpret_cast<uint2 *>(row + ca) = kv8::encode8<kFormat>(a, inv);
+        *reinterpret_cast<uint2 *>(row + cb) = kv8::encode8<kFormat>(b, inv);
+    } else if (o < off && e > e_old) {  // a row that the block held before, over the grown scale
+        const float down = kv8::pow2(e_old - e);
+        for (int s = 0; s < 2; ++s) {
+            uint2 *at = reinterpret_cast<uint2 *>(row + (s ? cb : ca));
+            const uint2 w = *at;
+            float x[4], y[4];
+            kv8::decode4<kFormat>(w.x, x);
+            kv8::decode4<kFormat>(w.y, y);
+            const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            *at = kv8::encode8<kFormat>(f, down);
         }
     }
-    if (part == 0 && lane == 0 && (off == 0 || e > e_old)) *scale = kv8::pow2(e);
+    if (threadIdx.x == 0 && (off == 0 || e > e_old)) *scale = kv8::pow2(e);
 }
 
 template <int kFormat, int kD>
-__global__ void __launch_bounds__(256)
-    kv8_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int kv_ctas, int parts,
+__global__ void __launch_bounds__(512)
+    kv8_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int kv_ctas, int window,
                       int q_groups, int q_heads_per_warp) {
-    __shared__ uint32_t amax_sh[kRowsPerWarp];
+    __shared__ uint32_t amax_sh[16];
     pdl_trigger();
     pdl_wait();  // writers of the rows, earlier readers of the blocks
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int lane = threadIdx.x & 31;
     if (static_cast<int>(blockIdx.x) >= kv_ctas) {
-        const int64_t w = static_cast<int64_t>(blockIdx.x - kv_ctas) * warps + warp, t = w / q_groups;
+        const int64_t w = static_cast<int64_t>(blockIdx.x - kv_ctas) * (blockDim.x >> 5) + (threadIdx.x >> 5), t = w / q_groups;
         if (t >= r.n) return;
         const int h0 = static_cast<int>(w - t * q_groups) * q_heads_per_warp;
         rope_heads(r, t, h0, min(p.q_heads, h0 + q_heads_per_warp), kD, lane,
@@ -140,31 +122,36 @@ __global__ void __launch_bounds__(256)
                    [&](int h) { return p.q_out + (t * p.q_heads + h) * kD; });
         return;
     }
-    // units (token, side, head), warps / parts of them a CTA at a time
-    const int per = 2 * p.kv_heads, units = warps / parts, sub = warp / parts, part = warp - sub * parts;
-    const int64_t total = r.n * per;
-    for (int64_t u0 = static_cast<int64_t>(blockIdx.x) * units; u0 < total; u0 += static_cast<int64_t>(kv_ctas) * units) {
-        const int64_t u = u0 + sub;  // (with several parts a CTA has one unit: all its warps take the same branches)
-        if (u >= total) continue;
-        const int64_t t = u / per;
-        const int j = static_cast<int>(u - t * per);
-        const int64_t slot = __ldg(p.slots + t), before = t > 0 ? __ldg(p.slots + t - 1) : -1;
-        if (slot < 0) continue;
+    // tokens t0 .. t0 + window - 1 of one kv head and side; every warp does the same here
+    const int per = 2 * p.kv_heads, w = blockIdx.x / per, j = blockIdx.x - w * per;
+    const int64_t t0 = static_cast<int64_t>(w) * window;
+    int64_t slot = -1;
+    bool begins = false;
+    if (lane < window && t0 + lane < r.n) {
+        const int64_t t = t0 + lane, before = t > 0 ? __ldg(p.slots + t - 1) : -1;
+        slot = __ldg(p.slots + t);
         if (slot >= p.num_slots) {
-            if (j == 0 && part == 0 && lane == 0) atomicOr(p.err, 1);
-            continue;
+            if (j == 0) atomicOr(p.err, 1);
+            slot = -1;
         }
-        const int off = static_cast<int>(slot % p.block_size);
-        if (off > 0 && before == slot - 1) continue;  // inside a run
-        int n = 1;  // rows of the run: tokens t + i at slot + i, within the block
-        for (int i0 = 1; i0 < p.block_size - off; i0 += 32) {
+        begins = slot >= 0 && ((slot & (p.block_size - 1)) == 0 || before != slot - 1);
+    }
+    uint32_t todo = __ballot_sync(0xffffffffu, begins);
+    while (todo) {
+        const int at = __ffs(todo) - 1;
+        todo &= todo - 1;
+        const int64_t t = t0 + at, s = __shfl_sync(0xffffffffu, slot, at);
+        const int room = p.block_size - static_cast<int>(s & (p.block_size - 1));
+        int n = 1;  // rows of the run: tokens t + i at slot s + i, within the block
+        for (int i0 = 1; i0 < room; i0 += 32) {
             const int i = i0 + lane;
-            const bool more = i < p.block_size - off && t + i < r.n && __ldg(p.slots + t + i) == slot + i;
+            const bool more = i < room && t + i < r.n && __ldg(p.slots + t + i) == s + i;
             const uint32_t miss = ~__ballot_sync(0xffffffffu, more);
             n += miss ? __ffs(miss) - 1 : 32;
             if (miss) break;
         }
-        append_run<kFormat, kD>(r, p, t, slot, n, j % p.kv_heads, j >= p.kv_heads, part, parts, lane, amax_sh);
+        append_run<kFormat, kD>(r, p, t, s, n, j >= p.kv_heads ? j - p.kv_heads : j, j >= p.kv_heads, amax_sh);
+        __syncthreads();  // before the next run writes the magnitudes
     }
 }
 
@@ -186,7 +173,7 @@ __device__ __forceinline__ void codes_to_bf16(const uint4 &w, float scale, uint4
     hi = make_uint4(out[4], out[5], out[6], out[7]);
 }
 
-// A thread per 16 values of a row: K rows' first, then V's.
+// A warp per row and side, 16 values a lane.
 template <int kFormat>
 __global__ void __launch_bounds__(256)
     kv8_read_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool, const int64_t *__restrict__ slots,
@@ -194,26 +181,28 @@ __global__ void __launch_bounds__(256)
                     int *err) {
     pdl_trigger();
     pdl_wait();
-    const int per_row = d >> 4, per = hkv * per_row;
-    const int64_t bytes = kv8::block_bytes(hkv, bs, d), total = 2 * n * per;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-        const bool v = i >= n * per;
-        const int64_t k = v ? i - n * per : i, row = k / per;
-        const int j = static_cast<int>(k - row * per), h = j / per_row, c = j - h * per_row;
+    const int lane = threadIdx.x & 31, sh = d == 64 ? 2 : 3, per = hkv << sh;  // chunks of a row: 4 or 8 a kv head
+    const int64_t bytes = kv8::block_bytes(hkv, bs, d), step = gridDim.x * 8ll;
+    for (int64_t w = blockIdx.x * 8ll + (threadIdx.x >> 5); w < 2 * n; w += step) {
+        const int64_t row = w >> 1;
+        const bool v = (w & 1) != 0;
         const int64_t slot = __ldg(slots + row);
-        uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-        if (slot >= num_slots) {
-            if (k == row * per && !v) atomicOr(err, 1);
-        } else if (slot >= 0) {
-            const uint8_t *blk = (v ? v_pool : k_pool) + slot / bs * bytes;
-            const int o = static_cast<int>(slot % bs);
-            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(blk + (static_cast<int64_t>(h) * bs + o) * d) + c);
-            const float scale = __ldg(reinterpret_cast<const float *>(blk + static_cast<int64_t>(hkv) * bs * d) + h);
-            codes_to_bf16<kFormat>(w, scale, lo, hi);
+        const bool in = slot >= 0 && slot < num_slots;
+        if (slot >= num_slots && !v && lane == 0) atomicOr(err, 1);
+        const uint8_t *blk = (v ? v_pool : k_pool) + (in ? slot / bs : 0) * bytes;
+        const int o = static_cast<int>(slot & (bs - 1));
+        uint4 *to = (v ? v_out : k_out) + 2 * row * per;
+        for (int i = lane; i < per; i += 32) {
+            const int h = i >> sh, c = i & ((1 << sh) - 1);
+            uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+            if (in) {
+                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(blk + (static_cast<int64_t>(h) * bs + o) * d) + c);
+                const float scale = __ldg(reinterpret_cast<const float *>(blk + static_cast<int64_t>(hkv) * bs * d) + h);
+                codes_to_bf16<kFormat>(x, scale, lo, hi);
+            }
+            to[2 * i] = lo;
+            to[2 * i + 1] = hi;
         }
-        uint4 *to = (v ? v_out : k_out) + 2 * k;
-        to[0] = lo;
-        to[1] = hi;
     }
 }
 
@@ -283,22 +272,21 @@ int sm_count() {
 
 template <int kFormat, int kD>
 int launch_append(const RopeArgs &r, const RopeAppendArgs &p, cudaStream_t st) {
-    const int parts = p.block_size / kRowsPerWarp;
-    const int warps = 8, units = parts > 1 ? 1 : warps;
-    const int threads = 32 * (parts > 1 ? parts : warps);
-    const int64_t total = r.n * 2 * p.kv_heads, want = (total + units - 1) / units;
-    const int64_t cap = 16ll * sm_count() * (parts > 1 ? 2 : 1);
-    const int kv_ctas = static_cast<int>(want < cap ? want : cap);
+    const int warps = p.block_size * kD / 512, per = 2 * p.kv_heads;
+    // one token a CTA in one wave of 32 warps an SM
+    const int64_t wave = 32ll * sm_count() / warps, all = r.n * per;
+    const int window = static_cast<int>(all <= wave ? 1 : all >= 32 * wave ? 32 : (all + wave - 1) / wave);
+    const int64_t kv_ctas = (r.n + window - 1) / window * per;
     int groups = 1, hpw = 1;
     int64_t q_ctas = 0;
     if (p.q && p.q_heads > 0) {
-        hpw = rope_heads_per_warp(r.n, p.q_heads, r.pairs);
+        hpw = rope_heads_per_warp(r.n, p.q_heads, r.pairs, p.d);
         groups = (p.q_heads + hpw - 1) / hpw;
-        q_ctas = (r.n * groups + threads / 32 - 1) / (threads / 32);
+        q_ctas = (r.n * groups + warps - 1) / warps;
     }
     if (kv_ctas + q_ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
-    FNPU_CUDA_TRY(launch_ex(kv8_append_kernel<kFormat, kD>, static_cast<int>(kv_ctas + q_ctas), threads, 0, st, true, nullptr, r, p,
-                            kv_ctas, parts, groups, hpw));
+    FNPU_CUDA_TRY(launch_ex(kv8_append_kernel<kFormat, kD>, static_cast<int>(kv_ctas + q_ctas), 32 * warps, 0, st, true, nullptr, r, p,
+                            static_cast<int>(kv_ctas), window, groups, hpw));
     return FNPU_OK;
 }
 
@@ -320,7 +308,7 @@ int launch_kv8_append(int format, const RopeArgs &r, const RopeAppendArgs &p, vo
 
 int launch_kv8_read(int format, const fnpu_attn_desc *d, const int64_t *slots, int32_t n, const void *k_pool, const void *v_pool,
                     void *k_out, void *v_out, int *err, void *stream) {
-    const int64_t want = (2ll * n * d->num_kv_heads * (d->head_dim_qk / 16) + 255) / 256, cap = 32ll * sm_count();
+    const int64_t want = (2ll * n + 7) / 8, cap = 32ll * sm_count();
     const int grid = static_cast<int>(want < cap ? want : cap);
     auto kernel = format == FNPU_KV_INT8_BLOCK ? kv8_read_kernel<FNPU_KV_INT8_BLOCK> : kv8_read_kernel<FNPU_KV_E4M3_BLOCK>;
     FNPU_CUDA_TRY(launch_ex(kernel, grid, 256, 0, static_cast<cudaStream_t>(stream), true, nullptr,

@@ -11,10 +11,12 @@
 namespace fnpu {
 namespace {
 
-constexpr int kWarpsPerCta = 8;
+constexpr int kWarpsPerCta = 4, kCtasPerSm = 8;  // latency is hidden by warps: 64 registers, 32 warps an SM
+constexpr int kMaxPasses = 8;                    // over the heads, of one warp
+constexpr int kValues = 2;  // chunks of value rows that a lane of the append holds
 
 // A warp per token and group of heads_per_warp heads.
-__global__ void __launch_bounds__(32 * kWarpsPerCta)
+__global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm)
     rope_kernel(const __grid_constant__ RopeArgs r, const __nv_bfloat16 *x, int64_t x_stride, int heads, int d,
                 __nv_bfloat16 *out, int64_t out_stride, int groups, int heads_per_warp) {
     pdl_trigger();
@@ -45,7 +47,7 @@ __global__ void __launch_bounds__(256)
         __nv_bfloat16 *to = out + t * out_stride + static_cast<int64_t>(h) * d;
         if (j < r.pairs) {
             float s, c;
-            sincospif(2.f * rope_turns(r.positions[r.axis[j] * r.n + t], r.inv_freq[j]), &s, &c);
+            rope_cos_sin(rope_turns(r.positions[r.axis[j] * r.n + t], r.inv_freq[j]), c, s);
             s *= r.sign;
             const int a = r.offset + (r.interleaved ? 2 * j : j), b = r.interleaved ? a + 1 : a + r.pairs;
             const float u = __bfloat162float(from[a]), v = __bfloat162float(from[b]);
@@ -61,7 +63,7 @@ __global__ void __launch_bounds__(256)
 // The append: the query heads and then the key heads of a token are the heads
 // that turn, into q_out and into the token's cache slot; value rows are copied,
 // shared out among the token's warps.
-__global__ void __launch_bounds__(32 * kWarpsPerCta)
+__global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm)
     rope_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int groups,
                        int heads_per_warp) {
     pdl_trigger();
@@ -74,11 +76,14 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta)
     const int64_t slot = __ldg(p.slots + t);
     const bool stored = slot >= 0 && slot < p.num_slots;
     if (slot >= p.num_slots && g == 0 && lane == 0) atomicOr(p.err, 1);
-    // value rows first: their loads are in flight while the angles are worked out
-    if (stored && p.v_new) {
-        const uint4 *from = reinterpret_cast<const uint4 *>(p.v_new + t * p.v_stride);
-        uint4 *to = reinterpret_cast<uint4 *>(p.v_cache) + slot * (static_cast<int64_t>(p.kv_heads) * p.d_v / 8);
-        for (int i = g * 32 + lane; i < p.kv_heads * p.d_v / 8; i += groups * 32) to[i] = __ldg(from + i);
+    // value rows, this warp's share: the first loads are in flight while heads turn
+    const int v_chunks = p.v_new ? p.kv_heads * p.d_v / 8 : 0, v_step = 32 * groups;
+    const uint4 *v_from = reinterpret_cast<const uint4 *>(p.v_new + t * p.v_stride);
+    uint4 v[kValues];
+#pragma unroll
+    for (int u = 0; u < kValues; ++u) {
+        const int i = g * 32 + lane + u * v_step;
+        if (i < v_chunks) v[u] = __ldg(v_from + i);
     }
     const int h0 = g * heads_per_warp;
     rope_heads(r, t, h0, min(p.q_heads + p.kv_heads, h0 + heads_per_warp), p.d, lane,
@@ -90,6 +95,14 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta)
                    if (h < p.q_heads) return p.q_out + (t * p.q_heads + h) * p.d;
                    return stored ? static_cast<__nv_bfloat16 *>(p.k_cache) + (slot * p.kv_heads + h - p.q_heads) * p.d : nullptr;
                });
+    if (!stored) return;
+    uint4 *v_to = reinterpret_cast<uint4 *>(p.v_cache) + slot * v_chunks;
+#pragma unroll
+    for (int u = 0; u < kValues; ++u) {
+        const int i = g * 32 + lane + u * v_step;
+        if (i < v_chunks) v_to[i] = v[u];
+    }
+    for (int i = g * 32 + lane + kValues * v_step; i < v_chunks; i += v_step) v_to[i] = __ldg(v_from + i);
 }
 
 int sm_count() {
@@ -101,14 +114,15 @@ int sm_count() {
 
 }  // namespace
 
-int rope_heads_per_warp(int64_t n, int heads, int pairs) {
+int rope_heads_per_warp(int64_t n, int heads, int pairs, int d) {
     // Angles are worked out once per warp, so a warp should have many heads; but
     // a call of few tokens is its longest chain, and there each warp has one pass.
-    const int hp = 32 / (pairs / 8);
-    const int64_t want = 16ll * sm_count();
-    for (int passes = 8; passes > 1; passes /= 2)
-        if (n * ((heads + hp * passes - 1) / (hp * passes)) >= want) return hp * passes;
-    return hp;
+    // The passes are shared out evenly.
+    const int hp = 32 / rope_lanes(pairs, d), passes = (heads + hp - 1) / hp;
+    const int64_t want = 32ll * sm_count();
+    int64_t groups = (want + n - 1) / n;
+    groups = groups < (passes + kMaxPasses - 1) / kMaxPasses ? (passes + kMaxPasses - 1) / kMaxPasses : groups > passes ? passes : groups;
+    return hp * static_cast<int>((passes + groups - 1) / groups);
 }
 
 int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, int d, void *out, int64_t out_stride,
@@ -122,7 +136,7 @@ int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, i
         FNPU_CUDA_TRY(launch_ex(rope_any_kernel, grid, 256, 0, st, true, nullptr, r, xp, x_stride, heads, d, op, out_stride));
         return FNPU_OK;
     }
-    const int hpw = rope_heads_per_warp(r.n, heads, r.pairs), groups = (heads + hpw - 1) / hpw;
+    const int hpw = rope_heads_per_warp(r.n, heads, r.pairs, d), groups = (heads + hpw - 1) / hpw;
     const int64_t ctas = (r.n * groups + kWarpsPerCta - 1) / kWarpsPerCta;
     if (ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
     FNPU_CUDA_TRY(launch_ex(rope_kernel, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, st, true, nullptr, r, xp, x_stride, heads, d, op,
@@ -132,7 +146,7 @@ int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, i
 
 int launch_rope_append(const RopeArgs &r, const RopeAppendArgs &p, void *stream) {
     const int heads = p.q_heads + p.kv_heads;
-    const int hpw = rope_heads_per_warp(r.n, heads, r.pairs), groups = (heads + hpw - 1) / hpw;
+    const int hpw = rope_heads_per_warp(r.n, heads, r.pairs, p.d), groups = (heads + hpw - 1) / hpw;
     const int64_t ctas = (r.n * groups + kWarpsPerCta - 1) / kWarpsPerCta;
     if (ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
     FNPU_CUDA_TRY(launch_ex(rope_append_kernel, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, static_cast<cudaStream_t>(stream), true,

@@ -9,17 +9,27 @@ namespace fnpu {
 // Angles. angle = position * inv_freq wants more than 32 bits: at position
 // 100000 the rounded product alone is up to 0.004 rad off. In turns (angle / 2 pi)
 // only the fraction counts, so inv_freq / 2 pi is kept as a sum of two fp32 values
-// (48 bits), the position is cut into two parts that fp32 holds exactly, and each
-// product's whole turns are dropped before anything small is added. What is left is
-// good to 2^-24 turns for positions below 2^20 and goes to sincospif.
+// (48 bits) and the product's whole turns are dropped before anything small is
+// added. What is left is good to 2^-24 turns for positions below 2^20. (A position
+// beyond 2^24 is cut into two parts that fp32 holds exactly.)
 __device__ __forceinline__ float rope_turns(int32_t position, float inv_freq) {
     constexpr float kHi = 0.15915494f, kLo = 6.4206382e-09f;  // kHi + kLo = 1 / (2 pi) to 2^-53
     const float f = inv_freq * kHi;
     const float g = __fmaf_rn(inv_freq, kHi, -f) + inv_freq * kLo;
-    const float a = static_cast<float>(position & ~4095), b = static_cast<float>(position & 4095);
-    const float pa = a * f, pb = b * f;
-    const float lo = (__fmaf_rn(a, f, -pa) + a * g) + (__fmaf_rn(b, f, -pb) + b * g);
-    return ((pa - rintf(pa)) + (pb - rintf(pb))) + lo;
+    auto part = [&](float p) {
+        const float t = p * f;
+        return (t - rintf(t)) + (__fmaf_rn(p, f, -t) + p * g);
+    };
+    if (__builtin_expect(position > 1 << 24 || position < -(1 << 24), 0))
+        return part(static_cast<float>(position & ~4095)) + part(static_cast<float>(position & 4095));
+    return part(static_cast<float>(position));
+}
+// cosine and sine of a turn's fraction (below 1.1): the hardware functions, whose
+// error of some 2^-20 is far below a bf16 result's
+__device__ __forceinline__ void rope_cos_sin(float turns, float &c, float &s) {
+    const float a = turns * 6.2831853f;
+    c = __cosf(a);
+    s = __sinf(a);
 }
 
 // cosine and sine of pairs 8 c .. 8 c + 7 at token t (inv_freq is 16-byte aligned)
@@ -37,7 +47,7 @@ __device__ __forceinline__ void rope_angles8(const RopeArgs &r, int64_t t, int c
             const int a = r.axis[8 * c + i];
             p = a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : pos[3];
         }
-        sincospif(2.f * rope_turns(p, f[i]), &sn[i], &cs[i]);
+        rope_cos_sin(rope_turns(p, f[i]), cs[i], sn[i]);
         sn[i] *= r.sign;
     }
 }
@@ -85,49 +95,67 @@ __device__ __forceinline__ void rope_rotate8(bool interleaved, const float (&cs)
 
 // One warp rotates heads [h0, h1) of token t: src(h) and dst(h) give the rows
 // (dst null: the head is left out). A lane owns eight pairs, whose angles it
-// works out once for all its heads; the pairs / 8 lanes of a head lie side by
-// side, 32 / (pairs / 8) heads go at a time and kRopeUnroll of them are in flight
-// per lane. Columns that do not turn are copied unless the rows are the same.
-constexpr int kRopeUnroll = 4;
+// works out once for all its heads, or two chunks that do not turn; the lanes of a
+// head lie side by side, and kRopeUnroll passes over the heads are in flight per
+// lane. (Rows with more chunks than a warp has lanes, a latent cache's, have those
+// that do not turn copied afterwards.)
+constexpr int kRopeUnroll = 3;
+__host__ __device__ __forceinline__ int rope_lanes(int pairs, int d) {  // lanes of a head
+    const int turn = pairs >> 3, rest = ((d - 2 * pairs) / 8 + 1) >> 1;
+    return turn + rest <= 32 ? turn + rest : turn;
+}
 template <class Src, class Dst>
 __device__ __forceinline__ void rope_heads(const RopeArgs &r, int64_t t, int h0, int h1, int d, int lane, Src src, Dst dst) {
-    const int cp = r.pairs >> 3, hp = 32 / cp;
-    const int lh = lane / cp, c = lane - lh * cp;
+    const int turn = r.pairs >> 3, chunks = (d - 2 * r.pairs) >> 3, per = rope_lanes(r.pairs, d), hp = 32 / per;
+    const int lh = lane / per, c = lane - lh * per;
+    const bool turns = c < turn;
+    auto plain = [&](int j) { return 8 * j < r.offset ? 8 * j : 8 * j + 2 * r.pairs; };
     int ca, cb;
-    rope_columns(r, c, ca, cb);
+    if (turns) {
+        rope_columns(r, c, ca, cb);
+    } else {
+        ca = plain(2 * (c - turn));
+        cb = 2 * (c - turn) + 1 < chunks ? plain(2 * (c - turn) + 1) : ca;
+    }
+    uint4 a[kRopeUnroll], b[kRopeUnroll];
+    auto load = [&](int u, int h) {
+        if (h >= h1) return;
+        const __nv_bfloat16 *row = src(h);
+        a[u] = *reinterpret_cast<const uint4 *>(row + ca);
+        b[u] = *reinterpret_cast<const uint4 *>(row + cb);
+    };
+    if (lh < hp) {
+#pragma unroll
+        for (int u = 0; u < kRopeUnroll; ++u) load(u, h0 + lh + u * hp);
+    }
     if (lh < hp) {
         float cs[8], sn[8];
-        uint4 a[kRopeUnroll], b[kRopeUnroll];
-        auto load = [&](int h) {
-#pragma unroll
-            for (int u = 0; u < kRopeUnroll; ++u)
-                if (h + u * hp < h1) {
-                    const __nv_bfloat16 *row = src(h + u * hp);
-                    a[u] = *reinterpret_cast<const uint4 *>(row + ca);
-                    b[u] = *reinterpret_cast<const uint4 *>(row + cb);
-                }
-        };
-        load(h0 + lh);  // in flight while the angles are worked out
-        rope_angles8(r, t, c, cs, sn);
+        if (turns) rope_angles8(r, t, c, cs, sn);
         for (int h = h0 + lh; h < h1; h += kRopeUnroll * hp) {
-            if (h != h0 + lh) load(h);
 #pragma unroll
-            for (int u = 0; u < kRopeUnroll; ++u)
-                if (h + u * hp < h1) {
-                    __nv_bfloat16 *row = dst(h + u * hp);
-                    if (!row) continue;
+            for (int u = 0; u < kRopeUnroll; ++u) {
+                if (h + u * hp >= h1) break;
+                __nv_bfloat16 *row = dst(h + u * hp);
+                if (turns) {
                     float x[8], y[8];
                     bf16x8_to_f32(a[u], x);
                     bf16x8_to_f32(b[u], y);
                     rope_rotate8(r.interleaved != 0, cs, sn, x, y);
-                    *reinterpret_cast<uint4 *>(row + ca) = f32_to_bf16x8(x);
-                    *reinterpret_cast<uint4 *>(row + cb) = f32_to_bf16x8(y);
+                    a[u] = f32_to_bf16x8(x);
+                    b[u] = f32_to_bf16x8(y);
                 }
+                if (row && (turns || row != src(h + u * hp))) {
+                    *reinterpret_cast<uint4 *>(row + ca) = a[u];
+                    *reinterpret_cast<uint4 *>(row + cb) = b[u];
+                }
+                load(u, h + (u + kRopeUnroll) * hp);  // in flight over the next ones
+            }
         }
     }
-    const int pc = (d - 2 * r.pairs) >> 3;  // chunks of a head that do not turn
-    for (int i = lane; i < (h1 - h0) * pc; i += 32) {
-        const int h = h0 + i / pc, j = i % pc, col = 8 * j < r.offset ? 8 * j : 8 * j + 2 * r.pairs;
+    if (per > turn || chunks == 0) return;
+#pragma unroll 4
+    for (int i = lane; i < (h1 - h0) * chunks; i += 32) {
+        const int h = h0 + i / chunks, col = plain(i % chunks);
         const __nv_bfloat16 *from = src(h);
         __nv_bfloat16 *to = dst(h);
         if (to && to != from) *reinterpret_cast<uint4 *>(to + col) = *reinterpret_cast<const uint4 *>(from + col);
