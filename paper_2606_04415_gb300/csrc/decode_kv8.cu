@@ -355,13 +355,14 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, kN>::kCtas) decode_kv8_kernel
     // results are 32-byte loads of each thread, eight in flight: one CTA that merged all
     // 76 ranges of a 100000-key sequence took some 10 us.)
     auto is_last = [&](int counter, int count) -> bool {
-        __threadfence();  // this thread's partial results, before the count
+        // the barrier orders every thread's partial results before thread 0's count, and
+        // its acquire-release those of other CTAs before what this one reads next
         __syncthreads();
         if (tid == 0) {
-            const int n = atomicAdd(p.counters + counter, 1);
+            int n;
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;\n" : "=r"(n) : "l"(p.counters + counter) : "memory");
             *last_sh = n == count - 1;
             if (n == count - 1) p.counters[counter] = 0;  // zero for the next run
-            __threadfence();  // the others' counts, before their partial results
         }
         __syncthreads();
         return *last_sh != 0;

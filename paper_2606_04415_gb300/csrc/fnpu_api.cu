@@ -433,7 +433,8 @@ bool remainder_histogram(const WaveUnits &w, int32_t m, int32_t n, std::vector<i
 // equal items is best where there is one (64 decodes of 512..4096 keys, 4 kv heads:
 // 592 items 34.0 us, 772 38.7, 1140 35.9); beyond, what the last items last weighs
 // against the starts (128 of 128..8192: 4096-key ranges 112 us, 2048 99.8, 1024
-// 104; 256 of 500..8000, 8 kv heads: 323, 328, 347).
+// 104; 256 of 500..8000, 8 kv heads: 323, 328, 347). A light step ends sooner where no
+// SM has two items (20 of 300..4000, one kv head: 133 items 6.3, 161 7.3, 200 8.1).
 // The rows of a kv head (query token x query head) may go to items of 8, 16 or 32:
 // wide items read the codes once for more rows, narrow ones have a shorter chain a
 // tile (kKv8TileCost, in 1/20 of the narrow one's) and more CTAs an SM. (16 sequences
@@ -461,17 +462,20 @@ Kv8Split kv8_split(Each each, int64_t max_rows, int32_t sms) {
             else lo = mid + 1;
             one_wave = 64 * hi;
         }
-        for (int32_t sk : {one_wave, 256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
+        for (int32_t sk : {one_wave, 256, 320, 384, 448, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
             hist.assign(kKv8MaxItemKeys / 16 + kKv8ItemTiles + 1, 0);
+            int64_t all = 0;
             each([&](int32_t keys, int64_t heads, int64_t r) {
                 const int32_t n = (keys + sk - 1) / sk, tiles = (keys + 15) / 16;
                 const int64_t items = n * heads * ((r + rows - 1) / rows);
                 int32_t &h = hist[static_cast<size_t>((tiles + n - 1) / n + kKv8ItemTiles)];
                 h = static_cast<int32_t>(std::min<int64_t>(h + items, INT32_MAX));
+                all += items;
             });
-            const int64_t span = lpt_makespan(hist, slots, (least - 1) / cost + 1);
-            if (span * cost < least) {
-                least = span * cost;
+            const int32_t c = all <= sms ? cost * 3 / 4 : cost;  // a CTA with an SM to itself
+            const int64_t span = lpt_makespan(hist, slots, (least - 1) / c + 1);
+            if (span * c < least) {
+                least = span * c;
                 best = {rows, sk};
             }
         }
