@@ -237,7 +237,8 @@ int fnpu_plan_check(const fnpu_plan *plan, void *stream);
 
 /* Synchronise `stream`, then read and clear the library-wide device error
  * flag of the current device: FNPU_EDEVICE_RANGE (set by fnpu_kv_append and
- * fnpu_mla_expand on an out-of-range slot, and by fnpu_decode_attn_noalloc on a
+ * fnpu_mla_expand on an out-of-range slot, by fnpu_rope_append and fnpu_kv_read on one
+ * too and on values that an 8-bit cache cannot hold, and by fnpu_decode_attn_noalloc on a
  * context length or block id out of range), FNPU_EDEVICE_TIMEOUT (a bounded wait
  * of fnpu_mla_expand or fnpu_decode_attn_noalloc gave up: the rows of that call
  * are undefined), FNPU_OK or FNPU_ECUDA. */

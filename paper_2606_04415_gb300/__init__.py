@@ -421,7 +421,7 @@ def _rows(x, tokens: int):
     if n != tokens:
         raise ValueError("rows, positions and slots have the same number of tokens")
     s, t, u = x.stride()
-    if (u != 1 and d > 1) or (t != d and h > 1):
+    if ((u != 1 and d > 1) or (t != d and h > 1)) and n:
         raise ValueError("the heads and columns of a token must be contiguous")
     return x.data_ptr(), s if n > 1 else max(s, h * d)
 

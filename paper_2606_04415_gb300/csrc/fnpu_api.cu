@@ -464,15 +464,18 @@ Kv8Split kv8_split(Each each, int64_t max_rows, int32_t sms) {
         }
         for (int32_t sk : {one_wave, 256, 320, 384, 448, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
             hist.assign(kKv8MaxItemKeys / 16 + kKv8ItemTiles + 1, 0);
-            int64_t all = 0;
+            int64_t all = 0, work = 0, longest = 0;
             each([&](int32_t keys, int64_t heads, int64_t r) {
-                const int32_t n = (keys + sk - 1) / sk, tiles = (keys + 15) / 16;
+                const int32_t n = (keys + sk - 1) / sk, tiles = (keys + 15) / 16, len = (tiles + n - 1) / n + kKv8ItemTiles;
                 const int64_t items = n * heads * ((r + rows - 1) / rows);
-                int32_t &h = hist[static_cast<size_t>((tiles + n - 1) / n + kKv8ItemTiles)];
+                int32_t &h = hist[static_cast<size_t>(len)];
                 h = static_cast<int32_t>(std::min<int64_t>(h + items, INT32_MAX));
                 all += items;
+                work += items * len;
+                longest = std::max<int64_t>(longest, len);
             });
             const int32_t c = all <= sms ? cost * 3 / 4 : cost;  // a CTA with an SM to itself
+            if (std::max((work + slots - 1) / slots, longest) * c >= least) continue;  // (no schedule is shorter)
             const int64_t span = lpt_makespan(hist, slots, (least - 1) / c + 1);
             if (span * c < least) {
                 least = span * c;
@@ -1078,12 +1081,9 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
                         parts += ns + merged;
                         groups += 1 + merged;
                     }
-                    for (int32_t sp = 0; sp < ns; ++sp) {
-                        DecodeItem it = decode_item(s, kvh, sp * sk, std::min(c, (sp + 1) * sk), sp, ns, base, grp);
-                        it.row_begin = r0;
-                        it.blk[0] = c;
-                        ditems.push_back(it);
-                    }
+                    for (int32_t sp = 0; sp < ns; ++sp)
+                        ditems.push_back(DecodeItem{s, kvh, sp * sk, std::min(c, (sp + 1) * sk), sp, ns, base, grp, qs, s, r0, q,
+                                                    {c, 0, 0, 0}});
                 }
         } else if (decode_queue(s) && pl->use_dt) {
             // items over groups of kv heads, cut at whole 16-key stages; a

@@ -19,7 +19,8 @@ namespace fnpu {
 // slot, or the MLA expansion's gather one; bit 1: the allocation-free decode
 // met a context length or a block id out of range; bit 2: a bounded wait of the
 // MLA expansion or of the allocation-free decode gave up, or a kernel of theirs
-// found its shared memory misaligned.
+// found its shared memory misaligned; bit 3: an append met values that an 8-bit block
+// cache cannot hold (NaN, infinities, magnitudes past its largest scale).
 __device__ int g_device_error = 0;
 
 __global__ void __launch_bounds__(256) kv_append_kernel(

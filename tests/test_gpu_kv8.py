@@ -106,6 +106,23 @@ def test_append_bit_exact(fmt, hkv, d, bs):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("d,bs", [(64, 16), (128, 64)])
+def test_append_many(fmt, d, bs):
+    """More runs than one wave of the grid: thousands of single rows in blocks that
+    hold rows already, then one long chunk; and none (zero tokens)."""
+    n = 3000 if d == 64 else 1200
+    c = Cache([bs] * n, 2, 2, d, bs, fmt, seed=d)
+    first = np.concatenate([c.slots(s, 0, 3) for s in range(n)])
+    c.append(c.rows(3 * n), c.rows(3 * n), first, check=False)
+    c.append(c.rows(n, 4.0), c.rows(n, 4.0), np.array([c.slots(s, 3, 4)[0] for s in c.rng.permutation(n)]))
+    long = Cache([5000], 2, 2, d, bs, fmt, seed=d + 1)
+    long.fill([7])
+    long.append(long.rows(4993), long.rows(4993), long.slots(0, 7, 5000))
+    long.append(long.rows(0), long.rows(0), np.zeros(0, np.int64))
+    assert c.fnpu.check() == c.fnpu.FNPU_OK
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 def test_append_special_rows(fmt):
     """Zero rows, tiny and huge rows, exact largest values and ties, negative
     zeros; a block begun afresh forgets its scale; padding between runs."""
@@ -312,6 +329,88 @@ def test_decode_rising_and_falling_scores(fmt):
     q = torch.from_numpy(np.broadcast_to(u * 8, (2, 4, 64)) * np.array([1, 2, 4, 0.1])[None, :, None]).to(torch.bfloat16).cuda()
     _attend(c, [1, 1], q=q)
     _attend(c, [1, 1], q=q, opts=c.fnpu.PlanOpts(64, 0, 0, 0))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("ql", [1, 3, 9])
+def test_query_rows_do_not_mix(fmt, ql):
+    """A row of NaN, one with an infinity and one of zeros among others: theirs
+    alone are NaN (or plain means); every other row is what it would be."""
+    c = Cache([150, 40], 8, 2, 64, 16, fmt, seed=24)
+    c.fill(c.ctx)
+    T = 2 * ql
+    q = _bf16(c.rng, T, 8, 64)
+    clean = q.clone()
+    q[0, 1], q[ql, 6, 3], q[T - 1, 4] = float("nan"), float("inf"), 0
+    clean[T - 1, 4] = 0
+    plan, _, o, l = _attend(c, [ql, ql], q=clean.cuda())
+    o2, l2 = torch.empty_like(o), torch.empty_like(l)
+    c.fnpu.mixed_attn_run(plan, q.cuda(), *c.dev, o2, l2)
+    odd = torch.zeros((T, 8), dtype=torch.bool)
+    odd[0, 1] = odd[ql, 6] = True
+    assert torch.equal(o2.cpu()[~odd], o.cpu()[~odd]) and torch.equal(l2.cpu()[~odd], l.cpu()[~odd])
+    assert o2.cpu()[odd].isnan().all() and l2.cpu()[0, 1].isnan()
+
+
+def test_append_then_attend_across_streams_and_replays():
+    """A step captured with its append: replayed for the next token with new rows,
+    positions and slots in the same buffers; the append on one stream, the attention on
+    another after an event."""
+    import paper_2606_04415_gb300 as fnpu
+    fmt = K8.INT8
+    c = Cache([65, 30], 4, 2, 64, 16, fmt, seed=25)
+    c.ctx = c.ctx - 2
+    c.fill(c.ctx)
+    f = (1e4 ** (-np.arange(32) / 32)).astype(np.float32)
+    rd, fd = fnpu.make_rope(64), torch.from_numpy(f).cuda()
+    qkv = torch.zeros((2, 8, 64), dtype=torch.bfloat16, device="cuda")
+    pos, slots = torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+    q, out, lse = torch.empty((2, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((2, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((2, 4), device="cuda")
+    plan = fnpu.kv8_attn_plan(c.desc, fmt, [1, 1], c.ctx + 1, [1, 1], c.table)
+
+    def append():
+        fnpu.rope_append(c.desc, rd, fd, pos, qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], slots, q, *c.dev, kv_format=fmt)
+
+    def put():
+        x = _bf16(c.rng, 2, 8, 64)
+        qkv.copy_(x)
+        pos.copy_(torch.from_numpy(c.ctx[None]))
+        slots.copy_(torch.from_numpy(np.array([c.slots(s, int(n), int(n) + 1)[0] for s, n in enumerate(c.ctx)])))
+        return x
+
+    def check(x):
+        torch.cuda.synchronize()
+        assert fnpu.plan_check(plan) == fnpu.FNPU_OK and fnpu.check() == fnpu.FNPU_OK
+        sl = slots.cpu().numpy()
+        before = K8.views(c.pools[0], 2, 16, 64)[1].copy()
+        K8.append(c.pools[0], K8.rope(x[:, 4:6].double().numpy(), pos.cpu().numpy(), f), sl, 2, 16, 64, fmt)
+        K8.append(c.pools[1], x[:, 6:].double().numpy(), sl, 2, 16, 64, fmt)
+        got = c.dev[0].cpu().numpy()
+        assert np.abs(K8.read(got, sl, 2, 16, 64, fmt) - K8.read(c.pools[0], sl, 2, 16, 64, fmt)).max() <= before.max() * 2
+        c.pools[0][:] = got
+        c.same()
+        c.ctx = c.ctx + 1
+        _compare(c, [1, 1], q, out, lse)
+
+    x = put()
+    s1, s2, e = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.Event()
+    s1.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s1):
+        append()
+        e.record()
+    s2.wait_event(e)
+    with torch.cuda.stream(s2):
+        fnpu.mixed_attn_run(plan, q, *c.dev, out, lse)
+    check(x)
+    fnpu.mixed_attn_replan(plan, [1, 1], c.ctx + 1, [1, 1], c.table)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        append()
+        fnpu.mixed_attn_run(plan, q, *c.dev, out, lse)
+    x = put()
+    g.replay()
+    check(x)
 
 
 @pytest.mark.parametrize("fmt", FMTS)
