@@ -515,8 +515,9 @@ int fnpu_kv_read(const fnpu_attn_desc *desc, int32_t kv_format, const int64_t *s
  * byte pools), fnpu_mixed_step (whose append stores the rows unrotated),
  * fnpu_plan_check, _info, _destroy. Sequences with at most 64 rows a kv head
  * (query_len x Hq / Hkv: one-token decodes, speculative verification, short
- * chunks) attend over the codes directly, of either phase; longer chunks over a
- * bf16 copy of their blocks that each run makes in the plan's workspace.
+ * chunks) attend over the codes directly, of either phase, and so do those of up to
+ * 2048 rows where none has more and the planner's model finds it shorter; the
+ * others over a bf16 copy of their blocks that each run makes in the plan's workspace.
  * Errors: as fnpu_mixed_attn_plan_ex; FNPU_EINVAL for another kv_format;
  * FNPU_EUNSUPPORTED for shapes that the formats do not take and for
  * FNPU_PLAN_NO_TCGEN05.

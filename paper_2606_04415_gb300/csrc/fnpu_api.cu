@@ -186,9 +186,9 @@ constexpr double kDecodeSmBpsFp8 = 50e9;  // (bytes of the FP8 cache: the conver
 constexpr double kDecodeAllBps = 4.0e12;
 
 // 8-bit block cache: sequences of up to this many rows a kv head (query tokens x
-// G) go to the decode kernel, 8 or 16 rows an item, which reads the codes once for
-// each; beyond, the staged copy of the prefill (one byte read, two written and read
-// again a value) costs less.
+// G) always go to the decode kernel, which reads the codes once for each item's
+// rows (40 sequences of 9 x 7 rows on 700..3000 keys: 62 us, 82 staged; of 18 x 7: 116
+// and 82).
 constexpr int64_t kKv8DecodeRows = 64;
 
 // Two packed Q tiles of one kv head (the tcgen05 prefill unit) before its key
@@ -427,6 +427,40 @@ bool remainder_histogram(const WaveUnits &w, int32_t m, int32_t n, std::vector<i
     return true;
 }
 
+// The groups of `rows` rows (query token x query head) of a kv head of a sequence:
+// f(first row, keys that the last of them sees).
+template <typename F>
+void kv8_row_groups(int32_t q, int32_t ctx, int32_t G, int32_t rows, F f) {
+    for (int32_t r0 = 0; r0 < q * G; r0 += rows) f(r0, ctx - q + (std::min(r0 + rows, q * G) - 1) / G + 1);
+}
+
+// Whether all sequences of more than kKv8DecodeRows rows a kv head, up to
+// kKv8MostRows, attend over the codes directly too: where the modelled time of
+// their items (32 rows a tile of 16 keys and kv head, kKv8WideTileUs on one SM) is
+// below that of staging them for the prefill -- its launches and start, a byte of
+// code read, two written and read, and its products. (Staged and directly: two chunks
+// of 22 tokens x 4 rows on 92 keys, 8 kv heads, 11.0 and 4.5 us; three of 26 x 8 on
+// 4426, one kv head, 22.1 and 10.8; one of 888 x 2 beside 18 decodes 24.6 and 11.7;
+// three of 120 x 7 on up to 682 20.5 and 18.3.)
+constexpr int64_t kKv8MostRows = 2048;
+constexpr double kKv8WideTileUs = 0.174, kKv8StageStartUs = 9.0, kKv8StageBytesPerUs = 4.0e6, kKv8StageFlopPerUs = 1.0e9;
+bool kv8_direct(const fnpu_attn_desc *d, int32_t n, const int32_t *query_len, const int32_t *context_len, int32_t sms) {
+    const int32_t G = d->num_q_heads / d->num_kv_heads;
+    double direct = 0.0, staged = kKv8StageStartUs;
+    for (int32_t s = 0; s < n; ++s) {
+        const int64_t q = query_len[s], rows = q * G;
+        if (rows <= kKv8DecodeRows) continue;
+        if (rows > kKv8MostRows) return false;
+        int64_t tiles = 0;
+        kv8_row_groups(query_len[s], context_len[s], G, 32, [&](int32_t, int32_t keys) { tiles += (keys + 15) / 16; });
+        direct += static_cast<double>(tiles) * d->num_kv_heads * kKv8WideTileUs * d->head_dim_qk / 128.0 / sms;
+        const double pairs = static_cast<double>(q) * (context_len[s] - q) + 0.5 * static_cast<double>(q) * (q + 1);
+        staged += 10.0 * context_len[s] * d->num_kv_heads * d->head_dim_qk / kKv8StageBytesPerUs +
+                  4.0 * pairs * d->num_q_heads * d->head_dim_qk / kKv8StageFlopPerUs;
+    }
+    return direct < staged;
+}
+
 // Ranges of the 8-bit decode. An item costs its 16-key tiles and kKv8ItemTiles for
 // its start and end (its CTA's first loads, the meeting of its warps, the partial
 // result); the schedule is longest first on the CTAs that fit the device. One wave of
@@ -444,8 +478,8 @@ constexpr int32_t kKv8ItemTiles = 14;
 struct Kv8Split {
     int32_t rows, keys;
 };
-// `each(add)` gives add(keys, kv heads, rows a kv head) of every sequence, the most
-// rows being max_rows.
+// `each(rows, add)` gives add(keys, items) of every sequence's groups of `rows` rows,
+// the most rows of a sequence being max_rows.
 template <typename Each>
 Kv8Split kv8_split(Each each, int64_t max_rows, int32_t sms) {
     thread_local std::vector<int32_t> hist;
@@ -457,7 +491,7 @@ Kv8Split kv8_split(Each each, int64_t max_rows, int32_t sms) {
         for (int32_t lo = 4, hi = kKv8MaxItemKeys / 64; lo < hi;) {
             const int32_t mid = (lo + hi) / 2;
             int64_t n = 0;
-            each([&](int32_t keys, int64_t heads, int64_t r) { n += (keys + 64 * mid - 1) / (64 * mid) * heads * ((r + rows - 1) / rows); });
+            each(rows, [&](int32_t keys, int64_t items) { n += (keys + 64 * mid - 1) / (64 * mid) * items; });
             if (n <= slots) hi = mid;
             else lo = mid + 1;
             one_wave = 64 * hi;
@@ -465,9 +499,9 @@ Kv8Split kv8_split(Each each, int64_t max_rows, int32_t sms) {
         for (int32_t sk : {one_wave, 256, 320, 384, 448, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
             hist.assign(kKv8MaxItemKeys / 16 + kKv8ItemTiles + 1, 0);
             int64_t all = 0, work = 0, longest = 0;
-            each([&](int32_t keys, int64_t heads, int64_t r) {
+            each(rows, [&](int32_t keys, int64_t count) {
                 const int32_t n = (keys + sk - 1) / sk, tiles = (keys + 15) / 16, len = (tiles + n - 1) / n + kKv8ItemTiles;
-                const int64_t items = n * heads * ((r + rows - 1) / rows);
+                const int64_t items = n * count;
                 int32_t &h = hist[static_cast<size_t>(len)];
                 h = static_cast<int32_t>(std::min<int64_t>(h + items, INT32_MAX));
                 all += items;
@@ -894,8 +928,10 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     // with 128. The per-head kernel aims at about 3 waves of 2 CTAs per SM.
     // the queue a sequence's work enters: decode items for one-token decodes
     // (8-bit blocks: whatever has few rows a kv head, of either phase -- see kKv8DecodeRows)
+    const int64_t direct_rows =
+        kv8 && kv8_direct(desc, num_seqs, query_len, context_len, sms) ? kKv8MostRows : kKv8DecodeRows;
     auto decode_queue = [&](int32_t s) {
-        return kv8 ? static_cast<int64_t>(query_len[s]) * G <= kKv8DecodeRows : phase[s] == 1 && query_len[s] == 1;
+        return kv8 ? static_cast<int64_t>(query_len[s]) * G <= direct_rows : phase[s] == 1 && query_len[s] == 1;
     };
     // a decode item with its sequence's fields and its first four block ids
     auto decode_item = [&](int32_t s, int32_t kvh, int32_t kb, int32_t ke, int32_t sp, int32_t ns, int32_t base,
@@ -932,9 +968,10 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     int32_t split = std::min(o.decode_split_keys, 1 << 30);  // (room to round up)
     Kv8Split kv8_plan{8, 0};
     if (kv8)
-        kv8_plan = kv8_split([&](auto add) {
+        kv8_plan = kv8_split([&](int32_t rows, auto add) {
             for (int32_t s = 0; s < num_seqs; ++s)
-                if (decode_queue(s)) add(context_len[s], desc->num_kv_heads, static_cast<int64_t>(query_len[s]) * G);
+                if (decode_queue(s))
+                    kv8_row_groups(query_len[s], context_len[s], G, rows, [&](int32_t, int32_t keys) { add(keys, desc->num_kv_heads); });
         }, kv8_rows, sms);
     pl->kv8_rows = kv8_plan.rows;
     if (kv8 && split == 0) {
@@ -1071,10 +1108,11 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
         } else if (decode_queue(s) && kv8) {
             // an item for each key range, kv head and kv8_rows rows; the last CTA
             // of a split group merges it
-            const int32_t rows = q * G, most = std::min((split + 15) / 16 * 16, kKv8MaxItemKeys), want = (c + most - 1) / most;
-            const int32_t sk = ((c + want - 1) / want + 15) / 16 * 16, ns = (c + sk - 1) / sk;  // even pieces, of whole tiles
+            const int32_t most = std::min((split + 15) / 16 * 16, kKv8MaxItemKeys);
             for (int32_t kvh = 0; kvh < desc->num_kv_heads; ++kvh)
-                for (int32_t r0 = 0; r0 < rows; r0 += pl->kv8_rows) {
+                kv8_row_groups(q, c, G, pl->kv8_rows, [&](int32_t r0, int32_t keys) {
+                    const int32_t want = (keys + most - 1) / most;
+                    const int32_t sk = ((keys + want - 1) / want + 15) / 16 * 16, ns = (keys + sk - 1) / sk;  // even pieces, of whole tiles
                     const int32_t base = ns > 1 ? parts : 0, grp = ns > 1 ? groups : 0;
                     const int32_t merged = ns > kKv8MergeAtOnce ? (ns + kKv8MergeGroup - 1) / kKv8MergeGroup : 0;
                     if (ns > 1) {
@@ -1082,9 +1120,9 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
                         groups += 1 + merged;
                     }
                     for (int32_t sp = 0; sp < ns; ++sp)
-                        ditems.push_back(DecodeItem{s, kvh, sp * sk, std::min(c, (sp + 1) * sk), sp, ns, base, grp, qs, s, r0, q,
+                        ditems.push_back(DecodeItem{s, kvh, sp * sk, std::min(keys, (sp + 1) * sk), sp, ns, base, grp, qs, s, r0, q,
                                                     {c, 0, 0, 0}});
-                }
+                });
         } else if (decode_queue(s) && pl->use_dt) {
             // items over groups of kv heads, cut at whole 16-key stages; a
             // split sequence is merged by the merge kernel (at most 256

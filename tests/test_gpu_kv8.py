@@ -445,6 +445,38 @@ def test_mixed(fmt, hq, hkv, d, bs):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("hq,hkv,d,bs,n", [(28, 4, 128, 16, 1171), (4, 2, 64, 32, 4097), (32, 8, 128, 64, 2049), (8, 1, 64, 16, 1025)])
+def test_long_chunks(fmt, hq, hkv, d, bs, n):
+    """A chunk of more than 8192 rows a kv head, whose blocks are staged, beside a
+    middle one, a short one and a decode; alone; and on a long prefix."""
+    ctx, ql = [n + 77, 150, 40, 500], [n, 100, 2, 1]
+    c = Cache(ctx, hq, hkv, d, bs, fmt, seed=n)
+    c.fill(c.ctx)
+    rows = set(c.rng.permutation(sum(ql))[:20].tolist()) | {0, n - 1, n, n + 99, n + 100, n + 101, n + 102}
+    plan, *_ = _attend(c, ql, tokens=rows)
+    info = plan.info()
+    assert info["prefill_items"] > 0 and info["decode_items"] > 0
+    one = Cache([n + 900], hq, hkv, d, bs, fmt, seed=n + 1)
+    one.fill(one.ctx)
+    plan, *_ = _attend(one, [n], tokens={0, 1, n // 2, n - 2, n - 1})
+    assert plan.info()["prefill_items"] > 0 and plan.info()["decode_items"] == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("hq,hkv,d,q", [(8, 1, 64, 250), (4, 2, 64, 700), (28, 4, 128, 60), (40, 1, 128, 33)])
+def test_middle_chunks_directly(fmt, hq, hkv, d, q):
+    """Chunks of hundreds of rows a kv head over the codes: every row, with and
+    without a prefix (early rows see a part of a group's ranges only)."""
+    ctx = [q + 50, q, q + 333]
+    c = Cache(ctx, hq, hkv, d, 16, fmt, seed=q)
+    c.fill(c.ctx)
+    rows = set(c.rng.permutation(3 * q)[:60].tolist()) | {0, q - 1, q, q + 1, q + 15, q + 16, q + 17, 2 * q - 1, 2 * q, 3 * q - 1}
+    plan, *_ = _attend(c, [q, q, q], tokens=rows)
+    assert plan.info()["prefill_items"] == 0
+    _attend(c, [q, q, q], tokens=rows, opts=c.fnpu.PlanOpts(48, 0, 0, 0))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 def test_step_replan_stream_capture(fmt):
     """fnpu_mixed_step stores and attends; the plan is re-planned for the next step;
     runs on another stream and replayed from a graph give the same bits."""
