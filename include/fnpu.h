@@ -431,8 +431,8 @@ typedef struct {
  *   inv_freq   device fp32 [rotary_dim / 2], 16-byte aligned
  *   positions  device int32 [num_axes, num_tokens]
  * Rows whose rotary_dim is a multiple of 16 and whose offset, head_dim and strides
- * are multiples of 8, 16-byte aligned, are read and written in 16-byte chunks;
- * others a pair at a time.
+ * are multiples of 8, 16-byte aligned, are read and written in 16-byte chunks; of
+ * half of all that, in 8-byte chunks; others a pair at a time.
  * Errors: FNPU_EINVAL for NULL or misaligned pointers, a descriptor outside the
  * ranges above or head_dim, a stride below a row, negative num_tokens;
  * FNPU_EUNSUPPORTED for rotary_dim > 256; FNPU_ECUDA.

@@ -205,10 +205,11 @@ struct Fp8StageJob {
 };
 int launch_fp8_stage(const void *k_pool, const void *v_pool, const Fp8StageJob *jobs, int32_t num_jobs, void *k_f16,
                      void *v_f16, const void *q_bf16, void *q_f16, int64_t q_values, void *stream, bool pdl);
-// Rotary positions. vector: rows may be read in 16-byte chunks of eight pairs.
+// Rotary positions. width: the pairs that may be read together, in chunks of as many
+// columns (8: 16 bytes, 4: 8 bytes), or 1: one by one.
 int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, int d, void *out, int64_t out_stride,
-                bool vector, void *stream);
-int rope_heads_per_warp(int64_t n, int heads, int pairs, int d);
+                int width, void *stream);
+int rope_heads_per_warp(int64_t n, int heads, int width, int pairs, int d);
 int launch_rope_append(const RopeArgs &r, const RopeAppendArgs &p, void *stream);
 // 8-bit cache with a scale for each (block, kv head), format FNPU_KV_INT8_BLOCK or
 // FNPU_KV_E4M3_BLOCK: append (turning rows where r.pairs > 0), rows read back as

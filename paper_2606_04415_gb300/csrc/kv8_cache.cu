@@ -16,32 +16,40 @@ namespace {
 //
 // A CTA has a warp for each 512 values of a block and kv head, 16 columns a lane (the
 // eight pairs that a lane turns among them), so that rows are loaded, turned and
-// stored in one pass through few registers; its warps meet once, for the largest
-// magnitude. It looks for runs that begin in a window of tokens, one token while the
-// grid is one wave: no list of runs to build, and a decode step, whose rows are all
-// runs of one, has a CTA for each. The queries are turned by further CTAs of the
-// same launch.
+// stored in one pass through few registers. It looks for runs that begin in a window
+// of tokens, one token while the grid is one wave: no list of runs to build. A run of
+// no more rows than a warp has at once (a decode step's have one) is one warp's, and
+// the warps take such runs in turn; a longer one is the CTA's, whose warps meet for the
+// largest magnitude. (One run after the other by the whole CTA, 86 rows of 8 kv heads
+// into blocks of 32: SHORT1 us with their reading back, SHORT2 so.) The queries are
+// turned by further CTAs of the same launch.
+template <int kFormat, int kD>
+struct RunRows {
+    static constexpr int kLanesPerRow = kD / 16, kRows = 32 / kLanesPerRow;  // rows that a warp has at once
+};
+
+// whole: by all warps of the CTA, each its rows of the block; else by this warp alone.
 template <int kFormat, int kD>
 __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendArgs &p, int64_t t, int64_t slot, int n, int head,
-                                           bool is_v, uint32_t *amax_sh) {
-    constexpr int kLanesPerRow = kD / 16, kRows = 32 / kLanesPerRow;
+                                           bool is_v, bool whole, uint32_t *amax_sh) {
+    constexpr int kLanesPerRow = RunRows<kFormat, kD>::kLanesPerRow, kRows = RunRows<kFormat, kD>::kRows;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int bs = p.block_size;
     const int off = static_cast<int>(slot & (bs - 1));
     uint8_t *blk = static_cast<uint8_t *>(is_v ? p.v_cache : p.k_cache) + slot / bs * kv8::block_bytes(p.kv_heads, bs, kD);
+    uint8_t *rows = blk + static_cast<int64_t>(head) * bs * kD;
     float *scale = reinterpret_cast<float *>(blk + static_cast<int64_t>(p.kv_heads) * bs * kD) + head;
     const int e_old = off > 0 ? kv8::scale_exp(*scale) : kv8::kMinExp;
-    const int o = warp * kRows + lane / kLanesPerRow, c = lane % kLanesPerRow;  // this lane's row and columns
+    const int o = (whole ? warp * kRows : off) + lane / kLanesPerRow, c = lane % kLanesPerRow;  // this lane's row and columns
     const int cp = is_v ? 0 : r.pairs >> 3;
     int ca, cb;
     if (c < cp) {
-        rope_columns(r, c, ca, cb);
+        rope_columns<8>(r, c, ca, cb);
     } else {  // 16 columns that do not turn
         ca = 16 * (c - cp);
         if (cp > 0 && ca >= r.offset) ca += 2 * r.pairs;
         cb = ca + 8;
     }
-    uint8_t *row = blk + (static_cast<int64_t>(head) * bs + o) * kD;
     const bool fresh = o >= off && o < off + n;
     float a[8], b[8];
     {
@@ -53,10 +61,10 @@ __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendAr
             rb = __ldg(reinterpret_cast<const uint4 *>(src + cb));
         }
         float cs[8], sn[8];
-        if (fresh && c < cp) rope_angles8(r, t + o - off, c, cs, sn);  // while the row comes
-        bf16x8_to_f32(ra, a);
-        bf16x8_to_f32(rb, b);
-        if (fresh && c < cp) rope_rotate8(r.interleaved != 0, cs, sn, a, b);
+        if (fresh && c < cp) rope_angles<8>(r, t + o - off, c, cs, sn);  // while the row comes
+        bf16_to_f32<8>(ra, a);
+        bf16_to_f32<8>(rb, b);
+        if (fresh && c < cp) rope_rotate<8>(r.interleaved != 0, cs, sn, a, b);
     }
     float amax = 0.f;
     bool odd = false;  // a value that is not finite
@@ -77,10 +85,14 @@ __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendAr
         }
         atomicOr(p.err, 8);
     }
-    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));  // (non-negative floats order as integers)
-    if (lane == 0) amax_sh[warp] = top;
-    __syncthreads();  // (also: every warp has the old scale)
-    for (int i = 0; i < warps; ++i) top = max(top, amax_sh[i]);
+    // (non-negative floats order as integers)
+    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));
+    if (whole) {
+        if (lane == 0) amax_sh[warp] = top;
+        __syncthreads();  // (also: every warp has the old scale)
+        for (int i = 0; i < warps; ++i) top = max(top, amax_sh[i]);
+        __syncthreads();  // before another run's magnitudes
+    }
     int e = max(e_old, kv8::required_exp<kFormat>(__uint_as_float(top)));
     if (e > kv8::kMaxExp) {
         e = kv8::kMaxExp;
@@ -88,42 +100,47 @@ __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendAr
     }
     if (fresh) {
         const float inv = kv8::pow2(-e);
-        *reinterpret_cast<uint2 *>(row + ca) = kv8::encode8<kFormat>(a, inv);
-        *reinterpret_cast<uint2 *>(row + cb) = kv8::encode8<kFormat>(b, inv);
-    } else if (o < off && e > e_old) {  // a row that the block held before, over the grown scale
-        const float down = kv8::pow2(e_old - e);
-        for (int s = 0; s < 2; ++s) {
-            uint2 *at = reinterpret_cast<uint2 *>(row + (s ? cb : ca));
-            const uint2 w = *at;
-            float x[4], y[4];
-            kv8::decode4<kFormat>(w.x, x);
-            kv8::decode4<kFormat>(w.y, y);
-            const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-            *at = kv8::encode8<kFormat>(f, down);
-        }
+        *reinterpret_cast<uint2 *>(rows + o * kD + ca) = kv8::encode8<kFormat>(a, inv);
+        *reinterpret_cast<uint2 *>(rows + o * kD + cb) = kv8::encode8<kFormat>(b, inv);
     }
-    if (threadIdx.x == 0 && (off == 0 || e > e_old)) *scale = kv8::pow2(e);
+    if (e > e_old) {  // the rows that the block held before, over the grown scale
+        const float down = kv8::pow2(e_old - e);
+        for (int i = (whole ? warp * kRows : 0) + lane / kLanesPerRow; i < off; i += whole ? bs : kRows)
+            for (int s = 0; s < 2; ++s) {
+                uint2 *at = reinterpret_cast<uint2 *>(rows + i * kD + (s ? cb : ca));
+                const uint2 w = *at;
+                float x[4], y[4];
+                kv8::decode4<kFormat>(w.x, x);
+                kv8::decode4<kFormat>(w.y, y);
+                const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                *at = kv8::encode8<kFormat>(f, down);
+            }
+    }
+    if (lane == 0 && (!whole || warp == 0) && (off == 0 || e > e_old)) *scale = kv8::pow2(e);
 }
 
 template <int kFormat, int kD>
 __global__ void __launch_bounds__(512)
     kv8_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int kv_ctas, int window,
                       int q_groups, int q_heads_per_warp) {
+    constexpr int kRows = RunRows<kFormat, kD>::kRows;
     __shared__ uint32_t amax_sh[16];
     pdl_trigger();
     pdl_wait();  // writers of the rows, earlier readers of the blocks
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     if (static_cast<int>(blockIdx.x) >= kv_ctas) {
-        const int64_t w = static_cast<int64_t>(blockIdx.x - kv_ctas) * (blockDim.x >> 5) + (threadIdx.x >> 5), t = w / q_groups;
+        const int64_t w = static_cast<int64_t>(blockIdx.x - kv_ctas) * warps + warp, t = w / q_groups;
         if (t >= r.n) return;
         const int h0 = static_cast<int>(w - t * q_groups) * q_heads_per_warp;
-        rope_heads(r, t, h0, min(p.q_heads, h0 + q_heads_per_warp), kD, lane,
-                   [&](int h) { return p.q + t * p.q_stride + static_cast<int64_t>(h) * kD; },
-                   [&](int h) { return p.q_out + (t * p.q_heads + h) * kD; });
+        rope_heads<8>(r, t, h0, min(p.q_heads, h0 + q_heads_per_warp), kD, lane,
+                      [&](int h) { return p.q + t * p.q_stride + static_cast<int64_t>(h) * kD; },
+                      [&](int h) { return p.q_out + (t * p.q_heads + h) * kD; });
         return;
     }
-    // tokens t0 .. t0 + window - 1 of one kv head and side; every warp does the same here
+    // tokens t0 .. t0 + window - 1 of one kv head and side; every warp finds the same runs
     const int per = 2 * p.kv_heads, w = blockIdx.x / per, j = blockIdx.x - w * per;
+    const bool is_v = j >= p.kv_heads;
+    const int head = is_v ? j - p.kv_heads : j;
     const int64_t t0 = static_cast<int64_t>(w) * window;
     int64_t slot = -1;
     bool begins = false;
@@ -136,22 +153,29 @@ __global__ void __launch_bounds__(512)
         }
         begins = slot >= 0 && ((slot & (p.block_size - 1)) == 0 || before != slot - 1);
     }
-    uint32_t todo = __ballot_sync(0xffffffffu, begins);
-    while (todo) {
+    const uint32_t goes_on = __ballot_sync(0xffffffffu, slot >= 0 && !begins);
+    int turn = 0;  // of the short runs
+    for (uint32_t todo = __ballot_sync(0xffffffffu, begins); todo; todo &= todo - 1) {
         const int at = __ffs(todo) - 1;
-        todo &= todo - 1;
         const int64_t t = t0 + at, s = __shfl_sync(0xffffffffu, slot, at);
         const int room = p.block_size - static_cast<int>(s & (p.block_size - 1));
-        int n = 1;  // rows of the run: tokens t + i at slot s + i, within the block
-        for (int i0 = 1; i0 < room; i0 += 32) {
-            const int i = i0 + lane;
-            const bool more = i < room && t + i < r.n && __ldg(p.slots + t + i) == s + i;
-            const uint32_t miss = ~__ballot_sync(0xffffffffu, more);
-            n += miss ? __ffs(miss) - 1 : 32;
-            if (miss) break;
+        // rows of the run: tokens t + i at slot s + i, within the block; past the window, look
+        int n = at == 31 ? 1 : __ffs(~(goes_on >> (at + 1)));
+        if (at + n == window)
+            for (int i0 = n; i0 < room; i0 += 32) {
+                const int i = i0 + lane;
+                const bool more = i < room && t + i < r.n && __ldg(p.slots + t + i) == s + i;
+                const uint32_t miss = ~__ballot_sync(0xffffffffu, more);
+                n += miss ? __ffs(miss) - 1 : 32;
+                if (miss) break;
+            }
+        const bool whole = n > kRows;  // the CTA's, else the warp's whose turn it is
+        if (!whole) {
+            const bool mine = turn == warp;
+            turn = turn + 1 == warps ? 0 : turn + 1;
+            if (!mine) continue;
         }
-        append_run<kFormat, kD>(r, p, t, s, n, j >= p.kv_heads ? j - p.kv_heads : j, j >= p.kv_heads, amax_sh);
-        __syncthreads();  // before the next run writes the magnitudes
+        append_run<kFormat, kD>(r, p, t, s, n, head, is_v, whole, amax_sh);
     }
 }
 
@@ -280,7 +304,7 @@ int launch_append(const RopeArgs &r, const RopeAppendArgs &p, cudaStream_t st) {
     int groups = 1, hpw = 1;
     int64_t q_ctas = 0;
     if (p.q && p.q_heads > 0) {
-        hpw = rope_heads_per_warp(r.n, p.q_heads, r.pairs, p.d);
+        hpw = rope_heads_per_warp(r.n, p.q_heads, 8, r.pairs, p.d);
         groups = (p.q_heads + hpw - 1) / hpw;
         q_ctas = (r.n * groups + warps - 1) / warps;
     }

@@ -16,6 +16,7 @@ constexpr int kMaxPasses = 8;                    // over the heads, of one warp
 constexpr int kValues = 2;  // chunks of value rows that a lane of the append holds
 
 // A warp per token and group of heads_per_warp heads.
+template <int W>
 __global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm)
     rope_kernel(const __grid_constant__ RopeArgs r, const __nv_bfloat16 *x, int64_t x_stride, int heads, int d,
                 __nv_bfloat16 *out, int64_t out_stride, int groups, int heads_per_warp) {
@@ -26,9 +27,9 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm)
     const int64_t t = w / groups;
     if (t >= r.n) return;
     const int h0 = static_cast<int>(w - t * groups) * heads_per_warp;
-    rope_heads(r, t, h0, min(heads, h0 + heads_per_warp), d, lane,
-               [&](int h) { return x + t * x_stride + static_cast<int64_t>(h) * d; },
-               [&](int h) { return out + t * out_stride + static_cast<int64_t>(h) * d; });
+    rope_heads<W>(r, t, h0, min(heads, h0 + heads_per_warp), d, lane,
+                  [&](int h) { return x + t * x_stride + static_cast<int64_t>(h) * d; },
+                  [&](int h) { return out + t * out_stride + static_cast<int64_t>(h) * d; });
 }
 
 // Any even rotary width, offset, stride and alignment: a thread per pair of a
@@ -63,7 +64,7 @@ __global__ void __launch_bounds__(256)
 // The append: the query heads and then the key heads of a token are the heads
 // that turn, into q_out and into the token's cache slot; value rows are copied,
 // shared out among the token's warps.
-__global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm)
+__global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm - 1)
     rope_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int groups,
                        int heads_per_warp) {
     pdl_trigger();
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm)
         if (i < v_chunks) v[u] = __ldg(v_from + i);
     }
     const int h0 = g * heads_per_warp;
-    rope_heads(r, t, h0, min(p.q_heads + p.kv_heads, h0 + heads_per_warp), p.d, lane,
+    rope_heads<8>(r, t, h0, min(p.q_heads + p.kv_heads, h0 + heads_per_warp), p.d, lane,
                [&](int h) -> const __nv_bfloat16 * {
                    return h < p.q_heads ? p.q + t * p.q_stride + static_cast<int64_t>(h) * p.d
                                         : p.k_new + t * p.k_stride + static_cast<int64_t>(h - p.q_heads) * p.d;
@@ -114,11 +115,11 @@ int sm_count() {
 
 }  // namespace
 
-int rope_heads_per_warp(int64_t n, int heads, int pairs, int d) {
+int rope_heads_per_warp(int64_t n, int heads, int width, int pairs, int d) {
     // Angles are worked out once per warp, so a warp should have many heads; but
     // a call of few tokens is its longest chain, and there each warp has one pass.
     // The passes are shared out evenly.
-    const int hp = 32 / rope_lanes(pairs, d), passes = (heads + hp - 1) / hp;
+    const int hp = 32 / rope_lanes(width, pairs, d), passes = (heads + hp - 1) / hp;
     const int64_t want = 32ll * sm_count();
     int64_t groups = (want + n - 1) / n;
     groups = groups < (passes + kMaxPasses - 1) / kMaxPasses ? (passes + kMaxPasses - 1) / kMaxPasses : groups > passes ? passes : groups;
@@ -126,27 +127,27 @@ int rope_heads_per_warp(int64_t n, int heads, int pairs, int d) {
 }
 
 int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, int d, void *out, int64_t out_stride,
-                bool vector, void *stream) {
+                int width, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const __nv_bfloat16 *xp = static_cast<const __nv_bfloat16 *>(x);
     __nv_bfloat16 *op = static_cast<__nv_bfloat16 *>(out);
-    if (!vector) {
+    if (width == 1) {
         const int64_t want = (r.n * heads * (d - r.pairs) + 255) / 256;
         const int grid = static_cast<int>(want < 64ll * sm_count() ? want : 64ll * sm_count());
         FNPU_CUDA_TRY(launch_ex(rope_any_kernel, grid, 256, 0, st, true, nullptr, r, xp, x_stride, heads, d, op, out_stride));
         return FNPU_OK;
     }
-    const int hpw = rope_heads_per_warp(r.n, heads, r.pairs, d), groups = (heads + hpw - 1) / hpw;
+    const int hpw = rope_heads_per_warp(r.n, heads, width, r.pairs, d), groups = (heads + hpw - 1) / hpw;
     const int64_t ctas = (r.n * groups + kWarpsPerCta - 1) / kWarpsPerCta;
     if (ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
-    FNPU_CUDA_TRY(launch_ex(rope_kernel, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, st, true, nullptr, r, xp, x_stride, heads, d, op,
+    FNPU_CUDA_TRY(launch_ex(width == 8 ? rope_kernel<8> : rope_kernel<4>, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, st, true, nullptr, r, xp, x_stride, heads, d, op,
                             out_stride, groups, hpw));
     return FNPU_OK;
 }
 
 int launch_rope_append(const RopeArgs &r, const RopeAppendArgs &p, void *stream) {
     const int heads = p.q_heads + p.kv_heads;
-    const int hpw = rope_heads_per_warp(r.n, heads, r.pairs, p.d), groups = (heads + hpw - 1) / hpw;
+    const int hpw = rope_heads_per_warp(r.n, heads, 8, r.pairs, p.d), groups = (heads + hpw - 1) / hpw;
     const int64_t ctas = (r.n * groups + kWarpsPerCta - 1) / kWarpsPerCta;
     if (ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
     FNPU_CUDA_TRY(launch_ex(rope_append_kernel, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, static_cast<cudaStream_t>(stream), true,

@@ -32,19 +32,23 @@ __device__ __forceinline__ void rope_cos_sin(float turns, float &c, float &s) {
     s = __sinf(a);
 }
 
-// cosine and sine of pairs 8 c .. 8 c + 7 at token t (inv_freq is 16-byte aligned)
-__device__ __forceinline__ void rope_angles8(const RopeArgs &r, int64_t t, int c, float (&cs)[8], float (&sn)[8]) {
+// cosine and sine of pairs W c .. W c + W - 1 at token t (inv_freq is 16-byte aligned)
+template <int W>
+__device__ __forceinline__ void rope_angles(const RopeArgs &r, int64_t t, int c, float (&cs)[W], float (&sn)[W]) {
     int32_t pos[kRopeMaxAxes];
 #pragma unroll
     for (int a = 0; a < kRopeMaxAxes; ++a) pos[a] = a < r.axes ? __ldg(r.positions + a * r.n + t) : 0;
-    const float4 f0 = __ldg(reinterpret_cast<const float4 *>(r.inv_freq) + 2 * c);
-    const float4 f1 = __ldg(reinterpret_cast<const float4 *>(r.inv_freq) + 2 * c + 1);
-    const float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
+    float f[W];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < W / 4; ++i) {
+        const float4 v = __ldg(reinterpret_cast<const float4 *>(r.inv_freq) + W / 4 * c + i);
+        f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
         int32_t p = pos[0];
         if (r.axes > 1) {
-            const int a = r.axis[8 * c + i];
+            const int a = r.axis[W * c + i];
             p = a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : pos[3];
         }
         rope_cos_sin(rope_turns(p, f[i]), cs[i], sn[i]);
@@ -52,40 +56,59 @@ __device__ __forceinline__ void rope_angles8(const RopeArgs &r, int64_t t, int c
     }
 }
 
-__device__ __forceinline__ void bf16x8_to_f32(const uint4 &v, float (&f)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// W columns of a bf16 row: 16 bytes for eight, 8 for four.
+template <int W>
+struct RopeChunk;
+template <>
+struct RopeChunk<8> {
+    using Type = uint4;
+};
+template <>
+struct RopeChunk<4> {
+    using Type = uint2;
+};
+template <int W>
+__device__ __forceinline__ void bf16_to_f32(const typename RopeChunk<W>::Type &v, float (&f)[W]) {
+    const uint32_t *w = reinterpret_cast<const uint32_t *>(&v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < W / 2; ++i) {
         f[2 * i] = __uint_as_float(w[i] << 16);
         f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
 }
-__device__ __forceinline__ uint4 f32_to_bf16x8(const float (&f)[8]) {
-    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+template <int W>
+__device__ __forceinline__ typename RopeChunk<W>::Type f32_to_bf16(const float (&f)[W]) {
+    typename RopeChunk<W>::Type v;
+    uint32_t *w = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+    return v;
 }
 
-// Where pairs 8 c .. 8 c + 7 lie: columns col_a .. + 7 and col_b .. + 7.
+// Where pairs W c .. W c + W - 1 lie: columns col_a .. + W - 1 and col_b .. + W - 1.
+template <int W>
 __device__ __forceinline__ void rope_columns(const RopeArgs &r, int c, int &col_a, int &col_b) {
-    col_a = r.offset + (r.interleaved ? 16 * c : 8 * c);
-    col_b = r.interleaved ? col_a + 8 : col_a + r.pairs;
+    col_a = r.offset + (r.interleaved ? 2 * W * c : W * c);
+    col_b = r.interleaved ? col_a + W : col_a + r.pairs;
 }
 
 // The two chunks rotated: y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin in fp32.
 // Half-split pairs have x1 in a and x2 in b; interleaved pairs are neighbours.
-__device__ __forceinline__ void rope_rotate8(bool interleaved, const float (&cs)[8], const float (&sn)[8], float (&a)[8],
-                                             float (&b)[8]) {
+template <int W>
+__device__ __forceinline__ void rope_rotate(bool interleaved, const float (&cs)[W], const float (&sn)[W], float (&a)[W],
+                                            float (&b)[W]) {
     if (interleaved) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < W / 2; ++i) {
             const float x = a[2 * i], y = a[2 * i + 1], z = b[2 * i], w = b[2 * i + 1];
             a[2 * i] = x * cs[i] - y * sn[i];
             a[2 * i + 1] = y * cs[i] + x * sn[i];
-            b[2 * i] = z * cs[i + 4] - w * sn[i + 4];
-            b[2 * i + 1] = w * cs[i + 4] + z * sn[i + 4];
+            b[2 * i] = z * cs[i + W / 2] - w * sn[i + W / 2];
+            b[2 * i + 1] = w * cs[i + W / 2] + z * sn[i + W / 2];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < W; ++i) {
             const float x = a[i], y = b[i];
             a[i] = x * cs[i] - y * sn[i];
             b[i] = y * cs[i] + x * sn[i];
@@ -94,59 +117,58 @@ __device__ __forceinline__ void rope_rotate8(bool interleaved, const float (&cs)
 }
 
 // One warp rotates heads [h0, h1) of token t: src(h) and dst(h) give the rows
-// (dst null: the head is left out). A lane owns eight pairs, whose angles it
-// works out once for all its heads, or two chunks that do not turn; the lanes of a
-// head lie side by side, and kRopeUnroll passes over the heads are in flight per
-// lane. (Rows with more chunks than a warp has lanes, a latent cache's, have those
-// that do not turn copied afterwards.)
+// (dst null: the head is left out). A lane owns W pairs, whose angles it works out once
+// for all its heads, or two chunks that do not turn; the lanes of a head lie side by
+// side, and kRopeUnroll passes over the heads are in flight per lane. (Rows with more
+// chunks than a warp has lanes, a latent cache's, have those that do not turn copied
+// afterwards.)
 constexpr int kRopeUnroll = 3;
-__host__ __device__ __forceinline__ int rope_lanes(int pairs, int d) {  // lanes of a head
-    const int turn = pairs >> 3, rest = ((d - 2 * pairs) / 8 + 1) >> 1;
+__host__ __device__ __forceinline__ int rope_lanes(int width, int pairs, int d) {  // lanes of a head
+    const int turn = pairs / width, rest = ((d - 2 * pairs) / width + 1) >> 1;
     return turn + rest <= 32 ? turn + rest : turn;
 }
-template <class Src, class Dst>
+template <int W, class Src, class Dst>
 __device__ __forceinline__ void rope_heads(const RopeArgs &r, int64_t t, int h0, int h1, int d, int lane, Src src, Dst dst) {
-    const int turn = r.pairs >> 3, chunks = (d - 2 * r.pairs) >> 3, per = rope_lanes(r.pairs, d), hp = 32 / per;
+    using Chunk = typename RopeChunk<W>::Type;
+    const int turn = r.pairs / W, chunks = (d - 2 * r.pairs) / W, per = rope_lanes(W, r.pairs, d), hp = 32 / per;
     const int lh = lane / per, c = lane - lh * per;
     const bool turns = c < turn;
-    auto plain = [&](int j) { return 8 * j < r.offset ? 8 * j : 8 * j + 2 * r.pairs; };
+    auto plain = [&](int j) { return W * j < r.offset ? W * j : W * j + 2 * r.pairs; };
     int ca, cb;
     if (turns) {
-        rope_columns(r, c, ca, cb);
+        rope_columns<W>(r, c, ca, cb);
     } else {
         ca = plain(2 * (c - turn));
         cb = 2 * (c - turn) + 1 < chunks ? plain(2 * (c - turn) + 1) : ca;
     }
-    uint4 a[kRopeUnroll], b[kRopeUnroll];
+    Chunk a[kRopeUnroll], b[kRopeUnroll];
     auto load = [&](int u, int h) {
         if (h >= h1) return;
         const __nv_bfloat16 *row = src(h);
-        a[u] = *reinterpret_cast<const uint4 *>(row + ca);
-        b[u] = *reinterpret_cast<const uint4 *>(row + cb);
+        a[u] = *reinterpret_cast<const Chunk *>(row + ca);
+        b[u] = *reinterpret_cast<const Chunk *>(row + cb);
     };
     if (lh < hp) {
 #pragma unroll
         for (int u = 0; u < kRopeUnroll; ++u) load(u, h0 + lh + u * hp);
-    }
-    if (lh < hp) {
-        float cs[8], sn[8];
-        if (turns) rope_angles8(r, t, c, cs, sn);
+        float cs[W], sn[W];
+        if (turns) rope_angles<W>(r, t, c, cs, sn);
         for (int h = h0 + lh; h < h1; h += kRopeUnroll * hp) {
 #pragma unroll
             for (int u = 0; u < kRopeUnroll; ++u) {
                 if (h + u * hp >= h1) break;
                 __nv_bfloat16 *row = dst(h + u * hp);
                 if (turns) {
-                    float x[8], y[8];
-                    bf16x8_to_f32(a[u], x);
-                    bf16x8_to_f32(b[u], y);
-                    rope_rotate8(r.interleaved != 0, cs, sn, x, y);
-                    a[u] = f32_to_bf16x8(x);
-                    b[u] = f32_to_bf16x8(y);
+                    float x[W], y[W];
+                    bf16_to_f32<W>(a[u], x);
+                    bf16_to_f32<W>(b[u], y);
+                    rope_rotate<W>(r.interleaved != 0, cs, sn, x, y);
+                    a[u] = f32_to_bf16<W>(x);
+                    b[u] = f32_to_bf16<W>(y);
                 }
                 if (row && (turns || row != src(h + u * hp))) {
-                    *reinterpret_cast<uint4 *>(row + ca) = a[u];
-                    *reinterpret_cast<uint4 *>(row + cb) = b[u];
+                    *reinterpret_cast<Chunk *>(row + ca) = a[u];
+                    *reinterpret_cast<Chunk *>(row + cb) = b[u];
                 }
                 load(u, h + (u + kRopeUnroll) * hp);  // in flight over the next ones
             }
@@ -158,7 +180,7 @@ __device__ __forceinline__ void rope_heads(const RopeArgs &r, int64_t t, int h0,
         const int h = h0 + i / chunks, col = plain(i % chunks);
         const __nv_bfloat16 *from = src(h);
         __nv_bfloat16 *to = dst(h);
-        if (to && to != from) *reinterpret_cast<uint4 *>(to + col) = *reinterpret_cast<const uint4 *>(from + col);
+        if (to && to != from) *reinterpret_cast<Chunk *>(to + col) = *reinterpret_cast<const Chunk *>(from + col);
     }
 }
 

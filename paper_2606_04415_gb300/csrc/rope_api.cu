@@ -68,9 +68,11 @@ int fnpu_rope(const fnpu_rope_desc *rope, const float *inv_freq, const int32_t *
     const int64_t row = static_cast<int64_t>(num_heads) * head_dim;
     if (!x || !out || misaligned(x, 2) || misaligned(out, 2) || x_stride < row || out_stride < row) return FNPU_EINVAL;
     if (x == out && x_stride != out_stride) return FNPU_EINVAL;
-    const bool vector = r.pairs % 8 == 0 && r.offset % 8 == 0 && head_dim % 8 == 0 && x_stride % 8 == 0 && out_stride % 8 == 0 &&
-                        !misaligned(x, 16) && !misaligned(out, 16);
-    return launch_rope(r, x, x_stride, num_heads, head_dim, out, out_stride, vector, stream);
+    auto fits = [&](int w) {  // everything a multiple of w columns, and of its bytes
+        const uintptr_t at = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out);
+        return r.pairs % w == 0 && r.offset % w == 0 && head_dim % w == 0 && x_stride % w == 0 && out_stride % w == 0 && at % (2 * w) == 0;
+    };
+    return launch_rope(r, x, x_stride, num_heads, head_dim, out, out_stride, fits(8) ? 8 : fits(4) ? 4 : 1, stream);
 }
 
 int fnpu_rope_append(const fnpu_attn_desc *desc, int32_t kv_format, const fnpu_rope_desc *rope, const float *inv_freq,
