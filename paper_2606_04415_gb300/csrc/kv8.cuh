@@ -37,18 +37,19 @@ __device__ __forceinline__ int required_exp(float amax) {
     return max(kMinExp, x + ((bits & 0x7FFFFFu) > (top & 0x7FFFFFu) ? 1 : 0));
 }
 
-// Codes of eight values over 2^e: nearest, ties to even, saturating.
+// Codes of eight values over 2^e, of magnitude at most kLargest there: nearest, ties to
+// even.
 template <int kFormat>
 __device__ __forceinline__ uint2 encode8(const float (&f)[8], float inv) {
     uint32_t w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if constexpr (kFormat == FNPU_KV_INT8_BLOCK) {
-            // x + 1.5 * 2^23 + 128 is rounded to an integer whose low byte is x + 128
+            // x + 1.5 * 2^23 + 128 is rounded to an integer whose low byte is x + 128 (the
+            // product is exact)
             uint32_t c[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                c[j] = __float_as_uint(fminf(fmaxf(f[4 * i + j] * inv, -127.f), 127.f) + 12583040.f);
+            for (int j = 0; j < 4; ++j) c[j] = __float_as_uint(__fmaf_rn(f[4 * i + j], inv, 12583040.f));
             w[i] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
         } else {
             const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * i] * inv, f[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);

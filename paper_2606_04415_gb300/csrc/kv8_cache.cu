@@ -36,7 +36,7 @@ __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendAr
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int bs = p.block_size;
     const int off = static_cast<int>(slot & (bs - 1));
-    uint8_t *blk = static_cast<uint8_t *>(is_v ? p.v_cache : p.k_cache) + slot / bs * kv8::block_bytes(p.kv_heads, bs, kD);
+    uint8_t *blk = static_cast<uint8_t *>(is_v ? p.v_cache : p.k_cache) + (slot >> (__ffs(bs) - 1)) * kv8::block_bytes(p.kv_heads, bs, kD);
     uint8_t *rows = blk + static_cast<int64_t>(head) * bs * kD;
     float *scale = reinterpret_cast<float *>(blk + static_cast<int64_t>(p.kv_heads) * bs * kD) + head;
     const int e_old = off > 0 ? kv8::scale_exp(*scale) : kv8::kMinExp;
@@ -66,14 +66,14 @@ __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendAr
         bf16_to_f32<8>(rb, b);
         if (fresh && c < cp) rope_rotate<8>(r.interleaved != 0, cs, sn, a, b);
     }
-    float amax = 0.f;
-    bool odd = false;  // a value that is not finite
+    float amax = 0.f, zero = 0.f;  // (zero: NaN if a value is not finite)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float x = fabsf(a[j]), y = fabsf(b[j]);
-        odd |= !(x < INFINITY) | !(y < INFINITY);
-        amax = fmaxf(amax, fmaxf(x, y));
+        zero = __fmaf_rn(a[j], 0.f, zero);
+        zero = __fmaf_rn(b[j], 0.f, zero);
+        amax = fmax3(amax, fabsf(a[j]), fabsf(b[j]));
     }
+    const bool odd = zero != 0.f;
     if (odd) {  // NaN is stored as zero, an infinity as the largest magnitude that the others allow
         amax = 0.f;
 #pragma unroll
@@ -94,9 +94,18 @@ __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendAr
         __syncthreads();  // before another run's magnitudes
     }
     int e = max(e_old, kv8::required_exp<kFormat>(__uint_as_float(top)));
-    if (e > kv8::kMaxExp) {
+    const bool over = e > kv8::kMaxExp;
+    if (over) {
         e = kv8::kMaxExp;
         if (lane == 0) atomicOr(p.err, 8);
+    }
+    if (over || odd) {
+        const float most = kv8::kLargest<kFormat> * kv8::pow2(e);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            a[j] = fminf(fmaxf(a[j], -most), most);
+            b[j] = fminf(fmaxf(b[j], -most), most);
+        }
     }
     if (fresh) {
         const float inv = kv8::pow2(-e);
@@ -120,7 +129,7 @@ __device__ __forceinline__ void append_run(const RopeArgs &r, const RopeAppendAr
 }
 
 template <int kFormat, int kD>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(512, 2)
     kv8_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int kv_ctas, int window,
                       int q_groups, int q_heads_per_warp) {
     constexpr int kRows = RunRows<kFormat, kD>::kRows;
@@ -213,7 +222,7 @@ __global__ void __launch_bounds__(256)
         const int64_t slot = __ldg(slots + row);
         const bool in = slot >= 0 && slot < num_slots;
         if (slot >= num_slots && !v && lane == 0) atomicOr(err, 1);
-        const uint8_t *blk = (v ? v_pool : k_pool) + (in ? slot / bs : 0) * bytes;
+        const uint8_t *blk = (v ? v_pool : k_pool) + (in ? slot >> (__ffs(bs) - 1) : 0) * bytes;
         const int o = static_cast<int>(slot & (bs - 1));
         uint4 *to = (v ? v_out : k_out) + 2 * row * per;
         for (int i = lane; i < per; i += 32) {
@@ -265,12 +274,12 @@ __global__ void __launch_bounds__(128)
     pdl_wait();  // the codes of the kernel before (the step's append)
     const Fp8StageJob jb = jobs[blockIdx.x / hkv];
     const int h = blockIdx.x % hkv;
-    const int per_row = d >> 4, per = bs * per_row;
+    const int per_row = d >> 4, sh = d == 64 ? 2 : 3, per = bs * per_row;
     const int64_t src = jb.src * kv8::block_bytes(hkv, bs, d), codes = static_cast<int64_t>(hkv) * bs * d;
     const float ks = __ldg(reinterpret_cast<const float *>(k_pool + src + codes) + h);
     const float vs = __ldg(reinterpret_cast<const float *>(v_pool + src + codes) + h);
     for (int i = threadIdx.x; i < per; i += 128) {
-        const int o = i / per_row, c = i - o * per_row;
+        const int o = i >> sh, c = i & (per_row - 1);
         const int64_t from = src + (static_cast<int64_t>(h) * bs + o) * d;
         const uint4 kw = __ldg(reinterpret_cast<const uint4 *>(k_pool + from) + c);
         const uint4 vw = __ldg(reinterpret_cast<const uint4 *>(v_pool + from) + c);
