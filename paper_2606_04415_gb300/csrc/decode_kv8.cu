@@ -2,9 +2,13 @@
 // multi-token decodes) over the 8-bit cache with a scale per block and kv head;
 // d = 64 or 128, blocks of 16, 32 or 64 slots, any number of query heads a kv head.
 //
-// Bound by the cache bytes: two operations a byte and query row. A CTA of four
-// warps takes one item: a key range of one sequence and kv head, up to 2048 keys,
-// and up to 8, 16 or 32 of its q_len x G query rows.
+// Bound by the cache bytes: two operations a byte and query row. 256 decodes of
+// 500..8000 keys, 8 kv heads: 323 us for 2.2 GB, the copy rate; 64 of 512..4096, 4 kv
+// heads: 33 us for 150 MB (22 at the copy rate; a launch's start, its first loads and
+// the merge are 8 of them, and SMs end up to 4 apart); with 32 rows an item the chain
+// of a tile binds: 75 us where the bytes are 43. A CTA of four warps takes one item: a
+// key range of one sequence and kv head, up to 4096 keys, and up to 8, 16 or 32 of
+// its q_len x G query rows.
 //   * The warps take the range's 16-key tiles in turn, each with a ring of its own
 //     that it fills itself by cp.async, and meet at the end of the item only. (The
 //     codes of a block and kv head are contiguous, so a tile is a plain copy. Fed by
@@ -204,8 +208,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<D, kN>::kCtas) decode_kv8_kernel
 #pragma unroll
             for (int n = 0; n < kN; ++n) {
                 uint4 b;
-                if (kN == 4) b = *reinterpret_cast<const uint4 *>(q_sh + ((n * (D / 32) + c) * 32 + lane) * 16);
-                else b = make_uint4(qb[kN == 4 ? 0 : n][2 * c][0], qb[kN == 4 ? 0 : n][2 * c][1], qb[kN == 4 ? 0 : n][2 * c + 1][0], qb[kN == 4 ? 0 : n][2 * c + 1][1]);
+                if constexpr (kN == 4) b = *reinterpret_cast<const uint4 *>(q_sh + ((n * (D / 32) + c) * 32 + lane) * 16);
+                else b = make_uint4(qb[n][2 * c][0], qb[n][2 * c][1], qb[n][2 * c + 1][0], qb[n][2 * c + 1][1]);
                 mma_f16_16816(s[n], a[0], a[1], a[2], a[3], b.x, b.y);
                 mma_f16_16816(s[n], a[4], a[5], a[6], a[7], b.z, b.w);
             }

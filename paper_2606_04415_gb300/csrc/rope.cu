@@ -4,8 +4,10 @@
 // y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin for each pair of columns, with the
 // angle position[axis(pair)] * inv_freq[pair]; the inverse turns back, which
 // is also the gradient (the rotation is orthogonal). Bound by HBM: 4 bytes a
-// value against some 5 operations, and an angle costs about 40 instructions but
-// serves every head of its token.
+// value against some 5 operations, and an angle costs about 20 instructions but
+// serves every head of its token. 24000 tokens of 28 heads of 128: 54 us for 344 MB
+// (51 at the copy rate). The append beside it moves 201 MB for 8192 tokens of 32/8
+// heads in 38 us (30): a warp's chain of loads, angles and stores, at 28 warps an SM.
 #include "rope.cuh"
 
 namespace fnpu {
