@@ -313,7 +313,7 @@ int launch_append(const RopeArgs &r, const RopeAppendArgs &p, cudaStream_t st) {
     int groups = 1, hpw = 1;
     int64_t q_ctas = 0;
     if (p.q && p.q_heads > 0) {
-        hpw = rope_heads_per_warp(r.n, p.q_heads, 8, r.pairs, p.d);
+        hpw = rope_heads_per_warp(r.n, p.q_heads, 8, r.pairs, p.d, 32, 4);
         groups = (p.q_heads + hpw - 1) / hpw;
         q_ctas = (r.n * groups + warps - 1) / warps;
     }

@@ -13,8 +13,12 @@
 namespace fnpu {
 namespace {
 
-constexpr int kWarpsPerCta = 4, kCtasPerSm = 8;  // latency is hidden by warps: 64 registers, 32 warps an SM
-constexpr int kMaxPasses = 8;                    // over the heads, of one warp
+constexpr int kWarpsPerCta = 4, kCtasPerSm = 8, kAppendCtasPerSm = 7;  // latency is hidden by warps: 64 registers, 32 warps an SM
+// Passes over the heads of one warp, at most. The rotation by itself is best at 4 for
+// some waves (5000 tokens, 28 heads: 13.8 us, 15.4 with 7) and at 8 for many, where the
+// angles' work counts (24000 tokens on three axes: 53.7 us, 56.6 with 4); the append,
+// whose warps hold value rows too, at 8 (8000 tokens: 27.4 us, 28.9 with 4).
+constexpr int kFewPasses = 4, kMostPasses = 8, kManyWaves = 4;
 constexpr int kValues = 2;  // chunks of value rows that a lane of the append holds
 
 // A warp per token and group of heads_per_warp heads.
@@ -66,7 +70,7 @@ __global__ void __launch_bounds__(256)
 // The append: the query heads and then the key heads of a token are the heads
 // that turn, into q_out and into the token's cache slot; value rows are copied,
 // shared out among the token's warps.
-__global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm - 1)
+__global__ void __launch_bounds__(32 * kWarpsPerCta, kAppendCtasPerSm)
     rope_append_kernel(const __grid_constant__ RopeArgs r, const __grid_constant__ RopeAppendArgs p, int groups,
                        int heads_per_warp) {
     pdl_trigger();
@@ -117,14 +121,17 @@ int sm_count() {
 
 }  // namespace
 
-int rope_heads_per_warp(int64_t n, int heads, int width, int pairs, int d) {
-    // Angles are worked out once per warp, so a warp should have many heads; but
-    // a call of few tokens is its longest chain, and there each warp has one pass.
-    // The passes are shared out evenly.
-    const int hp = 32 / rope_lanes(width, pairs, d), passes = (heads + hp - 1) / hp;
-    const int64_t want = 32ll * sm_count();
-    int64_t groups = (want + n - 1) / n;
-    groups = groups < (passes + kMaxPasses - 1) / kMaxPasses ? (passes + kMaxPasses - 1) / kMaxPasses : groups > passes ? passes : groups;
+int rope_heads_per_warp(int64_t n, int heads, int width, int pairs, int d, int warps_per_sm, int most_passes) {
+    // Angles are worked out once per warp, so a warp should have many heads; but a
+    // call of few tokens is its longest chain, and there each warp has one pass. In
+    // between a token has as many warps as all tokens can have at once: a second
+    // wave for the last few costs more than longer warps (28 heads of 128 and their
+    // keys into a cache, 2000 tokens: 8.7 us with 2 groups, 10.3 with 3; 1200 tokens:
+    // 5.5 with 3, 6.7 with 4). Beyond one wave a warp has most_passes at most; the
+    // passes are shared out evenly.
+    const int hp = 32 / rope_lanes(width, pairs, d), passes = (heads + hp - 1) / hp, least = (passes + most_passes - 1) / most_passes;
+    int64_t groups = static_cast<int64_t>(warps_per_sm) * sm_count() / n;
+    groups = groups < least ? least : groups > passes ? passes : groups;
     return hp * static_cast<int>((passes + groups - 1) / groups);
 }
 
@@ -139,7 +146,9 @@ int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, i
         FNPU_CUDA_TRY(launch_ex(rope_any_kernel, grid, 256, 0, st, true, nullptr, r, xp, x_stride, heads, d, op, out_stride));
         return FNPU_OK;
     }
-    const int hpw = rope_heads_per_warp(r.n, heads, width, r.pairs, d), groups = (heads + hpw - 1) / hpw;
+    constexpr int kWarps = kWarpsPerCta * kCtasPerSm;  // resident on an SM
+    const int most = r.n < static_cast<int64_t>(kManyWaves) * kWarps * sm_count() ? kFewPasses : kMostPasses;
+    const int hpw = rope_heads_per_warp(r.n, heads, width, r.pairs, d, kWarps, most), groups = (heads + hpw - 1) / hpw;
     const int64_t ctas = (r.n * groups + kWarpsPerCta - 1) / kWarpsPerCta;
     if (ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
     FNPU_CUDA_TRY(launch_ex(width == 8 ? rope_kernel<8> : rope_kernel<4>, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, st, true, nullptr, r, xp, x_stride, heads, d, op,
@@ -149,7 +158,8 @@ int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, i
 
 int launch_rope_append(const RopeArgs &r, const RopeAppendArgs &p, void *stream) {
     const int heads = p.q_heads + p.kv_heads;
-    const int hpw = rope_heads_per_warp(r.n, heads, 8, r.pairs, p.d), groups = (heads + hpw - 1) / hpw;
+    const int hpw = rope_heads_per_warp(r.n, heads, 8, r.pairs, p.d, kWarpsPerCta * kAppendCtasPerSm, kMostPasses),
+              groups = (heads + hpw - 1) / hpw;
     const int64_t ctas = (r.n * groups + kWarpsPerCta - 1) / kWarpsPerCta;
     if (ctas > INT32_MAX) return FNPU_EUNSUPPORTED;
     FNPU_CUDA_TRY(launch_ex(rope_append_kernel, static_cast<int>(ctas), 32 * kWarpsPerCta, 0, static_cast<cudaStream_t>(stream), true,
