@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <exception>
 #include <mutex>
 #include <set>
 #include <type_traits>
@@ -1520,7 +1521,18 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     return FNPU_OK;
 }
 
-// A new plan for a validated step.
+// plan_fill, whose host lists may not fit: nothing is thrown through the C ABI.
+int plan_build(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const int32_t *query_len, const int32_t *context_len,
+               const uint8_t *phase, const int32_t *block_table, int32_t block_table_stride, const fnpu_plan_opts &o, const StepMeta &m,
+               int sms, void *stream) {
+    try {
+        return plan_fill(pl, desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, m, sms, stream);
+    } catch (const std::exception &) {  // bad_alloc, length_error
+        return FNPU_ENOMEM;
+    }
+}
+
+// A new plan for a step.
 int plan_new(const fnpu_attn_desc *desc, int32_t kv_format, int32_t num_seqs, const int32_t *query_len, const int32_t *context_len,
              const uint8_t *phase, const int32_t *block_table, int32_t block_table_stride, const fnpu_plan_opts *opts, void *stream,
              fnpu_plan **out) {
@@ -1536,8 +1548,7 @@ int plan_new(const fnpu_attn_desc *desc, int32_t kv_format, int32_t num_seqs, co
     fnpu_plan *pl = new (std::nothrow) fnpu_plan();
     if (!pl) return FNPU_ENOMEM;
     pl->kv_format = kv_format;
-    rc = plan_fill(pl, desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, m, sms,
-                   stream);
+    rc = plan_build(pl, desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, m, sms, stream);
     if (rc != FNPU_OK) {
         release_plan(pl);
         delete pl;
@@ -1579,8 +1590,7 @@ int fnpu_mixed_attn_replan(fnpu_plan *pl, int32_t num_seqs, const int32_t *query
     rc = plan_sms(o, &sms);
     if (rc != FNPU_OK) return rc;
     const fnpu_attn_desc desc = pl->desc;
-    return plan_fill(pl, &desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, m, sms,
-                     stream);
+    return plan_build(pl, &desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, m, sms, stream);
 }
 
 }  // extern "C"
