@@ -32,12 +32,20 @@ class RotaryCache:
             shape, dtype = (num_blocks * kv8_block_bytes(self.desc, kv_format),), torch.uint8
         self.k, self.v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
 
+    def _empty(self, stream, *outputs):
+        """Outputs (shape, dtype) allocated on the stream that writes them: memory that
+        the caching allocator gives out on another one may still be in use there."""
+        if stream is not None and isinstance(stream, int):
+            stream = self.torch.cuda.ExternalStream(stream, device=self.k.device)
+        with self.torch.cuda.stream(stream):
+            return [self.torch.empty(shape, dtype=dtype, device=self.k.device) for shape, dtype in outputs]
+
     def append(self, qkv, positions, slot_mapping, stream=None):
         """Store a step's keys and values and return its rotated queries.
         qkv: bf16 [tokens, Hq + 2 Hkv, d]; positions int32 [axes, tokens] (one axis:
         [tokens] will do); slot_mapping int64 [tokens]."""
         hq, hkv, d = self.heads
-        q = self.torch.empty((qkv.shape[0], hq, d), dtype=qkv.dtype, device=qkv.device)
+        q, = self._empty(stream, ((qkv.shape[0], hq, d), qkv.dtype))
         rope_append(self.desc, self.rope, self.inv_freq, positions, qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], slot_mapping,
                     q, self.k, self.v, kv_format=self.kv_format, stream=stream)
         return q
@@ -55,14 +63,13 @@ class RotaryCache:
 
     def attend(self, plan: Plan, q, stream=None):
         """(out bf16 [tokens, Hq, d], lse fp32 [tokens, Hq]) of the planned step."""
-        out = self.torch.empty_like(q)
-        lse = self.torch.empty(q.shape[:2], dtype=self.torch.float32, device=q.device)
+        out, lse = self._empty(stream, (q.shape, q.dtype), (q.shape[:2], self.torch.float32))
         mixed_attn_run(plan, q, self.k, self.v, out, lse, stream=stream)
         return out, lse
 
     def read(self, slots, stream=None):
         """The stored rows of ``slots``, as bf16 [n, Hkv, d] each."""
         _, hkv, d = self.heads
-        k, v = (self.torch.empty((slots.shape[0], hkv, d), dtype=self.torch.bfloat16, device=slots.device) for _ in range(2))
+        k, v = self._empty(stream, *(2 * [((slots.shape[0], hkv, d), self.torch.bfloat16)]))
         kv_read(self.desc, slots, self.k, self.v, k, v, kv_format=self.kv_format, stream=stream)
         return k, v

@@ -59,3 +59,34 @@ def test_read_gives_what_append_stored():
     want = qkv[:, :6].contiguous()
     fnpu.rope(fnpu.make_rope(64), f, pos, want)
     assert torch.equal(q, want[:, :4]) and torch.equal(k, want[:, 4:]) and torch.equal(v, qkv[:, 6:])
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_outputs_belong_to_the_stream_that_writes_them(raw):
+    """Memory that the caching allocator has back from the current stream, whose last
+    writer still waits there, is not the output of a call on another stream."""
+    import paper_2606_04415_gb300 as fnpu
+    from paper_2606_04415_gb300.rotary import RotaryCache
+    g = torch.Generator(device="cuda").manual_seed(2)
+    n, f = 300, torch.from_numpy((1e4 ** (-np.arange(32) / 32)).astype(np.float32)).cuda()
+    qkv = torch.randn((n, 8, 64), device="cuda", generator=g).to(torch.bfloat16)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    slots = torch.arange(n, device="cuda")
+    c = RotaryCache(4, 2, 64, 16, 20, fnpu.make_rope(64), f, fnpu.KV_INT8_BLOCK)
+    table = np.arange(20, dtype=np.int32)[None]
+    plan = c.plan(np.array([n]), np.array([n]), np.array([0]), table)
+    want_q = c.append(qkv, pos, slots)
+    want = (want_q, *c.attend(plan, want_q), *c.read(slots))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)  # the current stream is busy for some 50 ms
+    for t in want:
+        x = torch.empty_like(t)
+        x.fill_(7)
+        del x
+    stream = side.cuda_stream if raw else side
+    q = c.append(qkv, pos, slots, stream=stream)
+    got = (q, *c.attend(plan, q, stream=stream), *c.read(slots, stream=stream))
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
