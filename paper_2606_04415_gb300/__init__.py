@@ -399,27 +399,27 @@ def make_rope(rotary_dim: int, rotary_offset: int = 0, interleaved: bool = False
     return d
 
 
-_dtypes = None  # (rows, positions, frequencies): torch's dtypes, looked up once
+_dtypes = None  # (rows, positions, frequencies, slots): torch's dtypes, looked up once
 
 
 def _types():
     global _dtypes
     if _dtypes is None:
         import torch
-        _dtypes = (torch.bfloat16, torch.int32, torch.float32)
+        _dtypes = (torch.bfloat16, torch.int32, torch.float32, torch.int64)
     return _dtypes
 
 
-def _rows(x, tokens: int):
-    """Address and token stride of bf16 rows [tokens, heads, d] whose tokens may
-    lie apart (a slice of a fused projection's output)."""
+def _rows(x, shape):
+    """Address and token stride of bf16 rows of that shape, [tokens, heads, d], whose
+    tokens may lie apart (a slice of a fused projection's output)."""
     if not x.is_cuda:
         raise ValueError("expected a CUDA tensor")
     if x.dtype is not _types()[0]:
         raise TypeError("rows are bf16")
-    n, h, d = x.shape
-    if n != tokens:
-        raise ValueError("rows, positions and slots have the same number of tokens")
+    if x.shape != shape:
+        raise ValueError(f"expected rows of shape {tuple(shape)}, not {tuple(x.shape)}")
+    n, h, d = shape
     s, t, u = x.stride()
     if ((u != 1 and d > 1) or (t != d and h > 1)) and n:
         raise ValueError("the heads and columns of a token must be contiguous")
@@ -438,10 +438,8 @@ def rope(desc: RopeDesc, inv_freq, positions, x, out=None, stream=None) -> None:
     ``positions`` int32 [num_axes, n], ``inv_freq`` fp32 (``fnpu_rope``)."""
     n, h, d = x.shape
     out = x if out is None else out
-    if tuple(out.shape) != (n, h, d):
-        raise ValueError("out has the shape of x")
     _check_positions(desc, inv_freq, positions, n)
-    (xp, xs), (op, os_) = _rows(x, n), _rows(out, n)
+    (xp, xs), (op, os_) = _rows(x, x.shape), _rows(out, x.shape)
     rc = load().fnpu_rope(ctypes.byref(desc), _dptr(inv_freq), _dptr(positions), xp, xs, h, d, n, op, os_, _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_rope")
@@ -455,9 +453,16 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
     n = slot_mapping.numel()
     if rope is not None:
         _check_positions(rope, inv_freq, positions, n)
-    qp, qs = (None, 0) if q is None else _rows(q, n)
-    kp, ks = _rows(k_new, n)
-    vp, vs = (None, 0) if v_new is None else _rows(v_new, n)
+    if slot_mapping.dtype is not _types()[3]:
+        raise TypeError("slot_mapping is int64")
+    h, d, qp, qs, vp, vs = desc.num_kv_heads, desc.head_dim_qk, None, 0, None, 0
+    if q is not None:
+        qp, qs = _rows(q, (n, desc.num_q_heads, d))
+        if q_out is None or q_out.dtype is not _types()[0] or q_out.shape != q.shape:
+            raise ValueError("q_out is bf16, of the shape of q")
+    kp, ks = _rows(k_new, (n, h, d))
+    if v_new is not None:
+        vp, vs = _rows(v_new, (n, h, desc.head_dim_v))
     rc = (_lib or load()).fnpu_rope_append(ctypes.byref(desc), int(kv_format), None if rope is None else ctypes.byref(rope),
                                  _dptr(inv_freq), _dptr(positions), qp, qs, kp, ks, vp, vs, _dptr(slot_mapping), n,
                                  _dptr(q_out), _dptr(k_cache), _dptr(v_cache), _stream(stream))
@@ -467,6 +472,13 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
 
 def kv_read(desc: AttnDesc, slots, k_cache, v_cache, k_out, v_out, kv_format: int = KV_BF16, stream=None) -> None:
     """The rows that ``slots`` store, as bf16 (``fnpu_kv_read``)."""
+    bf16, _, _, int64 = _types()
+    rows = slots.shape[0] * desc.num_kv_heads
+    if slots.dtype is not int64:
+        raise TypeError("slots are int64")
+    if k_out.dtype is not bf16 or k_out.numel() != rows * desc.head_dim_qk or (
+            v_out is not None and (v_out.dtype is not bf16 or v_out.numel() != rows * desc.head_dim_v)):
+        raise ValueError("k_out and v_out are bf16 [n, Hkv, d]")
     rc = load().fnpu_kv_read(ctypes.byref(desc), int(kv_format), _dptr(slots), int(slots.shape[0]), _dptr(k_cache),
                              _dptr(v_cache), _dptr(k_out), _dptr(v_out), _stream(stream))
     if rc != FNPU_OK:

@@ -212,3 +212,29 @@ def test_append_latent_in_place():
     ko = torch.empty((n, 1, d), dtype=torch.bfloat16, device="cuda")
     fnpu.kv_read(desc, torch.from_numpy(slots).cuda(), kc, None, ko, None)
     assert torch.equal(ko, kc[slots]) and fnpu.check() == fnpu.FNPU_OK
+
+
+def test_append_and_read_refuse_other_shapes_and_types():
+    """Before any launch: a narrower slice, 32-bit slots and the like would be read past their end."""
+    import paper_2606_04415_gb300 as fnpu
+    n, hq, hkv, d = 5, 4, 2, 64
+    desc, rd, f = fnpu.make_desc(hq, hkv, d, d, 16, 2), fnpu.make_rope(d), torch.from_numpy(_freq(d // 2)).cuda()
+    pos, slots = torch.arange(n, dtype=torch.int32, device="cuda"), torch.arange(n, device="cuda")
+    qkv = torch.zeros((n, hq + 2 * hkv, d), dtype=torch.bfloat16, device="cuda")
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    kc, vc = (torch.zeros((32, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    qo, ko, vo = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(kc[:n]), torch.empty_like(kc[:n])
+
+    def append(q=q, k=k, v=v, slots=slots, qo=qo, f=f, pos=pos):
+        fnpu.rope_append(desc, rd, f, pos, q, k, v, slots, qo, kc, vc)
+
+    for bad in (dict(q=qkv[:, :3]), dict(k=qkv[:, 4:5]), dict(v=qkv[:, 7:]), dict(k=k[:, :, :32]), dict(slots=slots.int()), dict(qo=qo[:, :3]),
+                dict(qo=None), dict(qo=qo.half()), dict(k=k[:4]), dict(pos=pos.long()), dict(f=f[:31])):
+        with pytest.raises((ValueError, TypeError)):
+            append(**bad)
+    for bad in ((slots.int(), ko, vo), (slots, ko[:4], vo), (slots, ko, vo[:, :1]), (slots, ko.half(), vo), (slots, ko, vo.float())):
+        with pytest.raises((ValueError, TypeError)):
+            fnpu.kv_read(desc, bad[0], kc, vc, *bad[1:])
+    append()
+    fnpu.kv_read(desc, slots, kc, vc, ko, vo)
+    assert fnpu.check() == fnpu.FNPU_OK and not qo.any() and not ko.any()
