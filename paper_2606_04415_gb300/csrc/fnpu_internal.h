@@ -209,8 +209,11 @@ int launch_fp8_stage(const void *k_pool, const void *v_pool, const Fp8StageJob *
 // columns (8: 16 bytes, 4: 8 bytes), or 1: one by one.
 int launch_rope(const RopeArgs &r, const void *x, int64_t x_stride, int heads, int d, void *out, int64_t out_stride,
                 int width, void *stream);
-// Heads of a token that one warp turns, in a launch of warps_per_sm resident warps.
-int rope_heads_per_warp(int64_t n, int heads, int width, int pairs, int d, int warps_per_sm, int most_passes);
+// The heads and tokens that one warp turns, in a launch of warps_per_sm resident warps.
+struct RopeSplit {
+    int heads, tokens;
+};
+RopeSplit rope_split(int64_t n, int heads, int width, int pairs, int d, int warps_per_sm, int most_passes, bool many);
 int launch_rope_append(const RopeArgs &r, const RopeAppendArgs &p, void *stream);
 // 8-bit cache with a scale for each (block, kv head), format FNPU_KV_INT8_BLOCK or
 // FNPU_KV_E4M3_BLOCK: append (turning rows where r.pairs > 0), rows read back as

@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(512, 2)
         const int64_t w = static_cast<int64_t>(blockIdx.x - kv_ctas) * warps + warp, t = w / q_groups;
         if (t >= r.n) return;
         const int h0 = static_cast<int>(w - t * q_groups) * q_heads_per_warp;
-        rope_heads<8>(r, t, h0, min(p.q_heads, h0 + q_heads_per_warp), kD, lane,
+        rope_heads<8>(r, t, h0, min(p.q_heads, h0 + q_heads_per_warp), kD, lane, rope_lane<false>(lane, rope_lanes(8, r.pairs, kD), 1),
                       [&](int h) { return p.q + t * p.q_stride + static_cast<int64_t>(h) * kD; },
                       [&](int h) { return p.q_out + (t * p.q_heads + h) * kD; });
         return;
@@ -313,7 +313,7 @@ int launch_append(const RopeArgs &r, const RopeAppendArgs &p, cudaStream_t st) {
     int groups = 1, hpw = 1;
     int64_t q_ctas = 0;
     if (p.q && p.q_heads > 0) {
-        hpw = rope_heads_per_warp(r.n, p.q_heads, 8, r.pairs, p.d, 32, 4);
+        hpw = rope_split(r.n, p.q_heads, 8, r.pairs, p.d, 32, 4, false).heads;
         groups = (p.q_heads + hpw - 1) / hpw;
         q_ctas = (r.n * groups + warps - 1) / warps;
     }

@@ -116,22 +116,33 @@ __device__ __forceinline__ void rope_rotate(bool interleaved, const float (&cs)[
     }
 }
 
-// One warp rotates heads [h0, h1) of token t: src(h) and dst(h) give the rows
-// (dst null: the head is left out). A lane owns W pairs, whose angles it works out once
-// for all its heads, or two chunks that do not turn; the lanes of a head lie side by
-// side, and kRopeUnroll passes over the heads are in flight per lane. (Rows with more
-// chunks than a warp has lanes, a latent cache's, have those that do not turn copied
-// afterwards.)
+// One warp rotates heads [h0, h1) of one or more tokens: src(h) and dst(h) give the rows
+// of the calling lane's token (dst null: the head is left out). A lane owns W pairs,
+// whose angles it works out once for all its heads, or two chunks that do not turn; the
+// lanes of a head lie side by side, and kRopeUnroll passes over the heads are in flight
+// per lane. (Rows with more chunks than a warp has lanes, a latent cache's, have those
+// that do not turn copied afterwards; such a warp has one token.)
 constexpr int kRopeUnroll = 3;
 __host__ __device__ __forceinline__ int rope_lanes(int width, int pairs, int d) {  // lanes of a head
     const int turn = pairs / width, rest = ((d - 2 * pairs) / width + 1) >> 1;
     return turn + rest <= 32 ? turn + rest : turn;
 }
+// A lane's part: its chunk, token and first head, and the heads from pass to pass.
+struct RopeLane {
+    int chunk, token, head, step;
+    bool on;
+};
+template <bool kMany>
+__device__ __forceinline__ RopeLane rope_lane(int lane, int per, int tokens) {
+    const int g = lane / per, hp = 32 / per;
+    if (!kMany) return {lane - g * per, 0, g, hp, g < hp};
+    const int step = hp / tokens, token = g / step;
+    return {lane - g * per, token, g - token * step, step, token < tokens};
+}
 template <int W, class Src, class Dst>
-__device__ __forceinline__ void rope_heads(const RopeArgs &r, int64_t t, int h0, int h1, int d, int lane, Src src, Dst dst) {
+__device__ __forceinline__ void rope_heads(const RopeArgs &r, int64_t t, int h0, int h1, int d, int lane, const RopeLane &my, Src src, Dst dst) {
     using Chunk = typename RopeChunk<W>::Type;
-    const int turn = r.pairs / W, chunks = (d - 2 * r.pairs) / W, per = rope_lanes(W, r.pairs, d), hp = 32 / per;
-    const int lh = lane / per, c = lane - lh * per;
+    const int turn = r.pairs / W, chunks = (d - 2 * r.pairs) / W, per = rope_lanes(W, r.pairs, d), hp = my.step, c = my.chunk;
     const bool turns = c < turn;
     auto plain = [&](int j) { return W * j < r.offset ? W * j : W * j + 2 * r.pairs; };
     int ca, cb;
@@ -148,12 +159,12 @@ __device__ __forceinline__ void rope_heads(const RopeArgs &r, int64_t t, int h0,
         a[u] = *reinterpret_cast<const Chunk *>(row + ca);
         b[u] = *reinterpret_cast<const Chunk *>(row + cb);
     };
-    if (lh < hp) {
+    if (my.on) {
 #pragma unroll
-        for (int u = 0; u < kRopeUnroll; ++u) load(u, h0 + lh + u * hp);
+        for (int u = 0; u < kRopeUnroll; ++u) load(u, h0 + my.head + u * hp);
         float cs[W], sn[W];
         if (turns) rope_angles<W>(r, t, c, cs, sn);
-        for (int h = h0 + lh; h < h1; h += kRopeUnroll * hp) {
+        for (int h = h0 + my.head; h < h1; h += kRopeUnroll * hp) {
 #pragma unroll
             for (int u = 0; u < kRopeUnroll; ++u) {
                 if (h + u * hp >= h1) break;

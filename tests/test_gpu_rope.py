@@ -238,3 +238,45 @@ def test_append_and_read_refuse_other_shapes_and_types():
     append()
     fnpu.kv_read(desc, slots, kc, vc, ko, vo)
     assert fnpu.check() == fnpu.FNPU_OK and not qo.any() and not ko.any()
+
+
+# ------------------------------- few heads: several tokens beside each other in a warp
+
+@pytest.mark.parametrize("n,heads,d,rot,offset,axes,interleaved,inverse", [
+    (7301, 4, 80, 80, 0, 2, False, False), (9003, 4, 64, 32, 32, 1, True, False), (8000, 1, 128, 128, 0, 3, False, True),
+    (7777, 8, 64, 64, 0, 1, False, False), (7303, 2, 40, 8, 4, 2, False, True), (7301, 3, 576, 64, 512, 1, True, False)])
+def test_rope_many_tokens_of_few_heads(n, heads, d, rot, offset, axes, interleaved, inverse):
+    _, x, pos, axis, f, kw = _case(n, heads, d, rot, offset, axes, interleaved, inverse, seed=n, stride=heads * d + 8)
+    out = torch.full((n, heads, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    _run(x, out, pos, axis, f, kw)
+    _check(out, x, K8.rope(x.double().cpu().numpy(), pos, f, axis, **kw))
+    _run(x, x, pos, axis, f, kw)  # in place
+    assert torch.equal(x, out)
+
+
+@pytest.mark.parametrize("hq,hkv,d,bs,n", [(4, 2, 64, 16, 6401), (8, 1, 64, 32, 7003), (1, 1, 128, 16, 6500)])
+def test_append_bf16_many_tokens_of_few_heads(hq, hkv, d, bs, n):
+    import paper_2606_04415_gb300 as fnpu
+    rng = np.random.default_rng(n)
+    blocks = n // bs + 2
+    g = torch.Generator(device="cuda").manual_seed(n)
+    qkv = torch.randn((n, hq + 2 * hkv, d), device="cuda", generator=g).to(torch.bfloat16)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    slots = rng.permutation(blocks * bs)[:n].astype(np.int64)
+    slots[rng.integers(0, n, 50)] = -1
+    pos, f = rng.integers(0, 30000, (1, n)).astype(np.int32), _freq(d // 2)
+    kc, vc = (torch.randn((blocks * bs, hkv, d), device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    k0, v0 = kc.clone(), vc.clone()
+    qo = torch.empty((n, hq, d), dtype=torch.bfloat16, device="cuda")
+    args = (fnpu.make_desc(hq, hkv, d, d, bs, blocks), fnpu.make_rope(d), torch.from_numpy(f).cuda(), torch.from_numpy(pos).cuda(), q, k, v)
+    fnpu.rope_append(*args, torch.from_numpy(slots).cuda(), qo, kc, vc)
+    assert fnpu.check() == fnpu.FNPU_OK
+    _check(qo, q, K8.rope(q.double().cpu().numpy(), pos, f))
+    ok = np.flatnonzero(slots >= 0)
+    _check(kc[slots[ok]], k[ok], K8.rope(k.double().cpu().numpy(), pos, f)[ok])
+    assert torch.equal(vc[slots[ok]], v[ok])
+    rest = np.setdiff1d(np.arange(blocks * bs), slots)
+    assert torch.equal(kc[rest], k0[rest]) and torch.equal(vc[rest], v0[rest])
+    slots[n - 1] = blocks * bs  # past the pool
+    fnpu.rope_append(*args, torch.from_numpy(slots).cuda(), qo, kc, vc)
+    assert fnpu.check() == fnpu.FNPU_EDEVICE_RANGE and fnpu.check() == fnpu.FNPU_OK
