@@ -462,58 +462,75 @@ bool kv8_direct(const fnpu_attn_desc *d, int32_t n, const int32_t *query_len, co
     return direct < staged;
 }
 
-// Ranges of the 8-bit decode. An item costs its 16-key tiles and kKv8ItemTiles for
-// its start and end (its CTA's first loads, the meeting of its warps, the partial
-// result); the schedule is longest first on the CTAs that fit the device. One wave of
-// equal items is best where there is one (64 decodes of 512..4096 keys, 4 kv heads:
-// 592 items 34.0 us, 772 38.7, 1140 35.9); beyond, what the last items last weighs
-// against the starts (128 of 128..8192: 4096-key ranges 112 us, 2048 99.8, 1024
-// 104; 256 of 500..8000, 8 kv heads: 323, 328, 347). A light step ends sooner where no
-// SM has two items (20 of 300..4000, one kv head: 133 items 6.3, 161 7.3, 200 8.1).
-// The rows of a kv head (query token x query head) may go to items of 8, 16 or 32:
-// wide items read the codes once for more rows, narrow ones have a shorter chain a
-// tile (kKv8TileCost, in 1/20 of the narrow one's) and more CTAs an SM. (16 sequences
-// of 4 x 7 rows on 2000..30000 keys: 75 us in 32, 96 in 16; 3 of 9 x 7 on 200: 12.0 and
-// 8.1. 32 of 2 x 7 on 700..5000: 28.7 in 16, 31.7 in 8; 4 of them 15.0 and 13.2.)
-constexpr int32_t kKv8ItemTiles = 14;
+// Ranges and rows of the 8-bit decode's items. The CTAs of an SM share what it can
+// stream, so a step is modelled as its items longest first on the SMs, in tiles of 16
+// keys. An item costs its tiles and kKv8WholeTiles for its start and end, kKv8PieceTiles
+// where it is a piece of a split (a partial result to write and count; half of these in
+// the shorter tiles of d = 64). An SM with one CTA in place of all that fit takes
+// kKv8Alone times as long a tile (in between, in proportion); a sixth of the longest item
+// is added for what the order of the CTAs leaves uneven; and where not all items fit at
+// once, kKv8QueueTiles and up to a quarter of the longest, the more the emptier the second
+// wave. The rows of a kv head (query token x query head) may go to items of 8, 16 or 32:
+// wide items read the codes once for more rows, at kKv8TileUs a tile. A merge ends the step
+// kKv8MergeUs later, one in groups kKv8GroupsUs more. The constants are a fit to 140 steps
+// of 1 to 400 sequences, each in some 18 ranges for each count of rows: the choice
+// is 2% above the best of them on average (25% at most). (104 decodes of 283..1358 keys, 4 kv heads:
+// 19.4 us whole, 25.8 in ranges of 384; 11 of 60..4364: 10.2 in 384, 14.1 in 256, 16.6 in
+// 2048; 128 of 128..8192: 96 in 1536, 117 in 384, 110 in 4096; 16 sequences of 4 x 7 rows on
+// 2000..30000: 75 in 32 rows, 96 in 16; 32 of 5 x 7 on 145..590: 13.8 in 16, 15.0 in 32; 4 of
+// 2 x 7 on 700..5000: 8.9 in 8 rows and ranges of 640, 12.1 in 16.)
+constexpr int32_t kKv8PieceTiles = 13, kKv8WholeTiles = 6, kKv8QueueTiles = 10;
+constexpr double kKv8TileUs[3] = {0.065, 0.107, 0.195}, kKv8Alone[3] = {1.25, 1.25, 1.6}, kKv8MergeUs = 1.85, kKv8GroupsUs = 2.1;
 struct Kv8Split {
     int32_t rows, keys;
 };
 // `each(rows, add)` gives add(keys, items) of every sequence's groups of `rows` rows,
 // the most rows of a sequence being max_rows.
 template <typename Each>
-Kv8Split kv8_split(Each each, int64_t max_rows, int32_t sms) {
+Kv8Split kv8_split(Each each, int64_t max_rows, int32_t head_dim, int32_t sms) {
     thread_local std::vector<int32_t> hist;
+    const int32_t piece = head_dim == 64 ? (kKv8PieceTiles + 1) / 2 : kKv8PieceTiles;
+    const int32_t whole = head_dim == 64 ? (kKv8WholeTiles + 1) / 2 : kKv8WholeTiles;
     Kv8Split best{kv8_rows_per_item(max_rows), kKv8MaxItemKeys};
-    int64_t least = INT64_MAX;
-    for (int32_t rows = 8; rows <= kv8_rows_per_item(max_rows); rows *= 2) {
-        const int32_t slots = sms * (rows == 8 ? 4 : rows == 16 ? 3 : 2), cost = rows == 8 ? 20 : rows == 16 ? 24 : 29;
-        int32_t one_wave = kKv8MaxItemKeys;  // the shortest ranges that make one wave
-        for (int32_t lo = 4, hi = kKv8MaxItemKeys / 64; lo < hi;) {
-            const int32_t mid = (lo + hi) / 2;
-            int64_t n = 0;
-            each(rows, [&](int32_t keys, int64_t items) { n += (keys + 64 * mid - 1) / (64 * mid) * items; });
-            if (n <= slots) hi = mid;
-            else lo = mid + 1;
-            one_wave = 64 * hi;
+    double least = 1e30;
+    for (int32_t rows = 8, w = 0; rows <= kv8_rows_per_item(max_rows); rows *= 2, ++w) {
+        const int32_t ctas = 4 - w;  // that fit an SM
+        int32_t fit[2];  // the shortest ranges that make one item an SM, and as many as fit
+        for (int32_t i = 0, hi = kKv8MaxItemKeys / 64; i < 2; ++i) {
+            int32_t lo = 4;
+            while (lo < hi) {
+                const int32_t mid = (lo + hi) / 2;
+                int64_t n = 0;
+                each(rows, [&](int32_t keys, int64_t items) { n += (keys + 64 * mid - 1) / (64 * mid) * items; });
+                if (n <= (i ? ctas : 1) * sms) hi = mid;
+                else lo = mid + 1;
+            }
+            fit[i] = 64 * hi;
         }
-        for (int32_t sk : {one_wave, 256, 320, 384, 448, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
-            hist.assign(kKv8MaxItemKeys / 16 + kKv8ItemTiles + 1, 0);
-            int64_t all = 0, work = 0, longest = 0;
+        for (int32_t sk : {fit[1], fit[0], 128, 192, 256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
+            hist.assign(kKv8MaxItemKeys / 16 + kKv8PieceTiles + 1, 0);
+            int64_t work = 0, items = 0;
+            int32_t longest = 0, most = 1;
             each(rows, [&](int32_t keys, int64_t count) {
-                const int32_t n = (keys + sk - 1) / sk, tiles = (keys + 15) / 16, len = (tiles + n - 1) / n + kKv8ItemTiles;
-                const int64_t items = n * count;
+                const int32_t n = (keys + sk - 1) / sk, tiles = ((keys + 15) / 16 + n - 1) / n;
+                const int32_t len = tiles + (n > 1 ? piece : whole);
                 int32_t &h = hist[static_cast<size_t>(len)];
-                h = static_cast<int32_t>(std::min<int64_t>(h + items, INT32_MAX));
-                all += items;
-                work += items * len;
-                longest = std::max<int64_t>(longest, len);
+                h = static_cast<int32_t>(std::min<int64_t>(h + n * count, INT32_MAX));
+                items += n * count;
+                work += n * count * len;
+                longest = std::max(longest, tiles);
+                most = std::max(most, n);
             });
-            const int32_t c = all <= sms ? cost * 3 / 4 : cost;  // a CTA with an SM to itself
-            if (std::max((work + slots - 1) / slots, longest) * c >= least) continue;  // (no schedule is shorter)
-            const int64_t span = lpt_makespan(hist, slots, (least - 1) / c + 1);
-            if (span * c < least) {
-                least = span * c;
+            const double per_sm = static_cast<double>(items) / sms, waves = per_sm / ctas;
+            const double slow = 1.0 + (kKv8Alone[w] - 1.0) * std::max(0.0, ctas - std::max(1.0, per_sm)) / (ctas - 1);
+            double rest = longest / 6.0;
+            if (waves > 1.0) rest += kKv8QueueTiles + 0.25 * std::max(0.0, 2.0 - waves) * longest;
+            rest = rest * kKv8TileUs[w] + (most > 1 ? kKv8MergeUs : 0.0) + (most > kKv8MergeAtOnce ? kKv8GroupsUs : 0.0);
+            const double us = slow * kKv8TileUs[w];  // of a tile
+            if (rest + us * std::max<double>(static_cast<double>(work) / sms, longest) >= least) continue;  // (no schedule is shorter)
+            const double t = rest + us * static_cast<double>(lpt_makespan(hist, sms, static_cast<int64_t>(std::min((least - rest) / us, 1e12)) + 1));
+            if (t < least) {
+                least = t;
                 best = {rows, sk};
             }
         }
@@ -973,7 +990,7 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
             for (int32_t s = 0; s < num_seqs; ++s)
                 if (decode_queue(s))
                     kv8_row_groups(query_len[s], context_len[s], G, rows, [&](int32_t, int32_t keys) { add(keys, desc->num_kv_heads); });
-        }, kv8_rows, sms);
+        }, kv8_rows, desc->head_dim_qk, sms);
     pl->kv8_rows = kv8_plan.rows;
     if (kv8 && split == 0) {
         split = kv8_plan.keys;
