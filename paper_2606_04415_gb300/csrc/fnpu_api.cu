@@ -507,7 +507,7 @@ Kv8Split kv8_split(Each each, int64_t max_rows, int32_t head_dim, int32_t sms) {
             }
             fit[i] = 64 * hi;
         }
-        for (int32_t sk : {fit[1], fit[0], 128, 192, 256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 3072, 4096}) {
+        for (int32_t sk : {fit[1], fit[0], 128, 192, 256, 320, 384, 512, 640, 768, 1024, 1280, 1536, 2048, 2560, 4096}) {
             hist.assign(kKv8MaxItemKeys / 16 + kKv8PieceTiles + 1, 0);
             int64_t work = 0, items = 0;
             int32_t longest = 0, most = 1;
