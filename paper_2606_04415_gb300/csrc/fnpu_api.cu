@@ -188,7 +188,7 @@ constexpr double kDecodeAllBps = 4.0e12;
 
 // 8-bit block cache: sequences of up to this many rows a kv head (query tokens x
 // G) always go to the decode kernel, which reads the codes once for each item's
-// rows (40 sequences of 9 x 7 rows on 700..3000 keys: 62 us, 82 staged; of 18 x 7: 116
+// rows (40 sequences of 9 x 7 rows on 700..3000 keys: 66 us, 82 staged; of 18 x 7: 116
 // and 82).
 constexpr int64_t kKv8DecodeRows = 64;
 
