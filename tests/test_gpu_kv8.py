@@ -552,3 +552,19 @@ def test_large_pool_offsets():
         assert (np.abs(o.double().cpu().numpy() - ref_o) <= tol).all()
         assert (np.abs(l.double().cpu().numpy() - ref_l) <= 2e-5 * np.maximum(1, np.abs(ref_l))).all()
     assert fnpu.check() == fnpu.FNPU_OK
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_steps(seed):
+    """Steps of a random layout, batch and mix of lengths, with the planner's own rows
+    and ranges: of one-token decodes (even seeds), or with several tokens and chunks."""
+    r = np.random.default_rng(1000 + seed)
+    hq, hkv, d, bs = LAYOUTS[r.integers(len(LAYOUTS))]
+    n = int(np.exp(r.uniform(0, np.log(60))))
+    ctx = np.exp(r.uniform(0, np.log([300, 3000, 20000][r.integers(3)] if n < 12 else 1500), n)).astype(int)
+    ql = np.ones(n, int) if seed % 2 == 0 else np.minimum(ctx, r.choice([1, 1, 2, 3, 5, 9, 40, 130], n))
+    c = Cache(ctx.tolist(), hq, hkv, d, bs, FMTS[r.integers(2)], seed=seed)
+    c.fill(c.ctx)
+    ends = np.cumsum(ql)
+    rows = set(r.permutation(int(ends[-1]))[:40].tolist()) | set((ends - 1)[:12].tolist()) | set((ends - ql)[:12].tolist())
+    _attend(c, ql.tolist(), tokens=rows)
