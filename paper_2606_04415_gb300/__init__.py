@@ -260,10 +260,11 @@ def kv_append(desc: AttnDesc, k_new, v_new, slot_mapping, k_cache, v_cache, stre
 class Plan:
     """Owner of an ``fnpu_plan*``; destroyed with the object."""
 
-    def __init__(self, handle: int, desc: AttnDesc, num_tokens: int):
+    def __init__(self, handle: int, desc: AttnDesc, num_tokens: int, kv_format: int = KV_BF16):
         self.handle = handle
         self.desc = desc
         self.num_tokens = num_tokens
+        self.kv_format = kv_format
 
     def info(self) -> dict:
         pi, di, la = ctypes.c_int32(), ctypes.c_int32(), ctypes.c_int32()
@@ -316,6 +317,8 @@ def mixed_attn_replan(plan: Plan, query_len, context_len, phase, block_table,
 
 def mixed_attn_run(plan: Plan, q, k_cache, v_cache, out, lse, stream=None) -> None:
     """Attention of every planned query (``fnpu_mixed_attn_run``)."""
+    if plan.kv_format != KV_BF16:
+        _check_pools(plan.desc, plan.kv_format, k_cache, v_cache)
     rc = load().fnpu_mixed_attn_run(plan.handle, _dptr(q), _dptr(k_cache), _dptr(v_cache),
                                     _dptr(out), _dptr(lse), _stream(stream))
     if rc != FNPU_OK:
@@ -326,6 +329,8 @@ def mixed_step(plan: Plan, k_new, v_new, slot_mapping, q, k_cache, v_cache, out,
     """Append of the step's new rows and attention of every planned query in
     one call (``fnpu_mixed_step``; the same results as ``kv_append`` then
     ``mixed_attn_run``)."""
+    if plan.kv_format != KV_BF16:
+        _check_pools(plan.desc, plan.kv_format, k_cache, v_cache)
     rc = load().fnpu_mixed_step(plan.handle, _dptr(k_new), _dptr(v_new), _dptr(slot_mapping), _dptr(q),
                                 _dptr(k_cache), _dptr(v_cache), _dptr(out), _dptr(lse), _stream(stream))
     if rc != FNPU_OK:
@@ -399,14 +404,14 @@ def make_rope(rotary_dim: int, rotary_offset: int = 0, interleaved: bool = False
     return d
 
 
-_dtypes = None  # (rows, positions, frequencies, slots): torch's dtypes, looked up once
+_dtypes = None  # (rows, positions, frequencies, slots, 8-bit pools): torch's dtypes, looked up once
 
 
 def _types():
     global _dtypes
     if _dtypes is None:
         import torch
-        _dtypes = (torch.bfloat16, torch.int32, torch.float32, torch.int64)
+        _dtypes = (torch.bfloat16, torch.int32, torch.float32, torch.int64, torch.uint8)
     return _dtypes
 
 
@@ -424,6 +429,26 @@ def _rows(x, shape):
     if ((u != 1 and d > 1) or (t != d and h > 1)) and n:
         raise ValueError("the heads and columns of a token must be contiguous")
     return x.data_ptr(), s if n > 1 else max(s, h * d)
+
+
+def _check_pools(desc: AttnDesc, kv_format: int, k_cache, v_cache) -> None:
+    """Pools (where they are tensors) are of the format's type and hold every block
+    that ``desc`` speaks of: slots up to there are written and read."""
+    if desc.kv_fp8 or not KV_BF16 <= kv_format <= KV_E4M3_BLOCK:
+        return  # (refused by the library)
+    heads, slots = desc.num_kv_heads, desc.num_blocks * desc.block_size
+    if kv_format == KV_BF16:
+        dtype, k, v = _types()[0], slots * heads * desc.head_dim_qk, slots * heads * desc.head_dim_v
+    else:  # codes, then fp32 scales padded to 16 bytes a block
+        dtype = _types()[4]
+        k = v = slots * heads * desc.head_dim_qk + desc.num_blocks * ((heads + 3) // 4 * 16)
+    for x, n in ((k_cache, k),) if desc.v_in_k_latent else ((k_cache, k), (v_cache, v)):
+        if x is None or isinstance(x, int):
+            continue
+        if getattr(x, "dtype", None) is not dtype:
+            raise TypeError(f"the pools of cache format {kv_format} are {dtype} tensors")
+        if x.numel() < n:
+            raise ValueError(f"a pool of {desc.num_blocks} blocks has {n} elements, not {x.numel()}")
 
 
 def _check_positions(desc: RopeDesc, inv_freq, positions, n: int) -> None:
@@ -455,6 +480,7 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
         _check_positions(rope, inv_freq, positions, n)
     if slot_mapping.dtype is not _types()[3]:
         raise TypeError("slot_mapping is int64")
+    _check_pools(desc, kv_format, k_cache, v_cache)
     h, d, qp, qs, vp, vs = desc.num_kv_heads, desc.head_dim_qk, None, 0, None, 0
     if q is not None:
         qp, qs = _rows(q, (n, desc.num_q_heads, d))
@@ -472,10 +498,11 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
 
 def kv_read(desc: AttnDesc, slots, k_cache, v_cache, k_out, v_out, kv_format: int = KV_BF16, stream=None) -> None:
     """The rows that ``slots`` store, as bf16 (``fnpu_kv_read``)."""
-    bf16, _, _, int64 = _types()
+    bf16, _, _, int64, _ = _types()
     rows = slots.shape[0] * desc.num_kv_heads
     if slots.dtype is not int64:
         raise TypeError("slots are int64")
+    _check_pools(desc, kv_format, k_cache, v_cache)
     if k_out.dtype is not bf16 or k_out.numel() != rows * desc.head_dim_qk or (
             v_out is not None and (v_out.dtype is not bf16 or v_out.numel() != rows * desc.head_dim_v)):
         raise ValueError("k_out and v_out are bf16 [n, Hkv, d]")
@@ -504,4 +531,4 @@ def kv8_attn_plan(desc: AttnDesc, kv_format: int, query_len, context_len, phase,
                                    None if opts is None else ctypes.byref(opts), _stream(stream), ctypes.byref(out))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_kv8_attn_plan")
-    return Plan(out.value, desc, int(ql.sum()))
+    return Plan(out.value, desc, int(ql.sum()), int(kv_format))
