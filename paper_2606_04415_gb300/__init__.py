@@ -22,6 +22,7 @@ entry points raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -265,6 +266,7 @@ class Plan:
         self.desc = desc
         self.num_tokens = num_tokens
         self.kv_format = kv_format
+        self.shape = bytes(desc)  # as planned, whatever becomes of ``desc``
 
     def info(self) -> dict:
         pi, di, la = ctypes.c_int32(), ctypes.c_int32(), ctypes.c_int32()
@@ -318,7 +320,7 @@ def mixed_attn_replan(plan: Plan, query_len, context_len, phase, block_table,
 def mixed_attn_run(plan: Plan, q, k_cache, v_cache, out, lse, stream=None) -> None:
     """Attention of every planned query (``fnpu_mixed_attn_run``)."""
     if plan.kv_format != KV_BF16:
-        _check_pools(plan.desc, plan.kv_format, k_cache, v_cache)
+        _check_pools(plan.shape, plan.kv_format, k_cache, v_cache)
     rc = load().fnpu_mixed_attn_run(plan.handle, _dptr(q), _dptr(k_cache), _dptr(v_cache),
                                     _dptr(out), _dptr(lse), _stream(stream))
     if rc != FNPU_OK:
@@ -330,7 +332,7 @@ def mixed_step(plan: Plan, k_new, v_new, slot_mapping, q, k_cache, v_cache, out,
     one call (``fnpu_mixed_step``; the same results as ``kv_append`` then
     ``mixed_attn_run``)."""
     if plan.kv_format != KV_BF16:
-        _check_pools(plan.desc, plan.kv_format, k_cache, v_cache)
+        _check_pools(plan.shape, plan.kv_format, k_cache, v_cache)
     rc = load().fnpu_mixed_step(plan.handle, _dptr(k_new), _dptr(v_new), _dptr(slot_mapping), _dptr(q),
                                 _dptr(k_cache), _dptr(v_cache), _dptr(out), _dptr(lse), _stream(stream))
     if rc != FNPU_OK:
@@ -431,24 +433,36 @@ def _rows(x, shape):
     return x.data_ptr(), s if n > 1 else max(s, h * d)
 
 
-def _check_pools(desc: AttnDesc, kv_format: int, k_cache, v_cache) -> None:
-    """Pools (where they are tensors) are of the format's type and hold every block
-    that ``desc`` speaks of: slots up to there are written and read."""
+@functools.lru_cache(maxsize=64)
+def _pool_sizes(shape: bytes, kv_format: int):
+    """(type, elements of k_cache, of v_cache or None where there is none) of the pools of
+    a descriptor, given as its bytes; None for one that the library refuses."""
+    desc = AttnDesc.from_buffer_copy(shape)
     if desc.kv_fp8 or not KV_BF16 <= kv_format <= KV_E4M3_BLOCK:
-        return  # (refused by the library)
+        return None
     heads, slots = desc.num_kv_heads, desc.num_blocks * desc.block_size
     if kv_format == KV_BF16:
         dtype, k, v = _types()[0], slots * heads * desc.head_dim_qk, slots * heads * desc.head_dim_v
     else:  # codes, then fp32 scales padded to 16 bytes a block
         dtype = _types()[4]
         k = v = slots * heads * desc.head_dim_qk + desc.num_blocks * ((heads + 3) // 4 * 16)
-    for x, n in ((k_cache, k),) if desc.v_in_k_latent else ((k_cache, k), (v_cache, v)):
-        if x is None or isinstance(x, int):
+    return dtype, k, None if desc.v_in_k_latent else v
+
+
+def _check_pools(shape: bytes, kv_format: int, k_cache, v_cache) -> None:
+    """Pools (where they are tensors) are of the format's type and hold every block
+    that the descriptor speaks of: slots up to there are written and read."""
+    sizes = _pool_sizes(shape, kv_format)
+    if sizes is None:
+        return
+    dtype, k, v = sizes
+    for x, n in ((k_cache, k), (v_cache, v)):
+        if n is None or x is None or isinstance(x, int):
             continue
         if getattr(x, "dtype", None) is not dtype:
             raise TypeError(f"the pools of cache format {kv_format} are {dtype} tensors")
         if x.numel() < n:
-            raise ValueError(f"a pool of {desc.num_blocks} blocks has {n} elements, not {x.numel()}")
+            raise ValueError(f"a pool of this descriptor has {n} elements, not {x.numel()}")
 
 
 def _check_positions(desc: RopeDesc, inv_freq, positions, n: int) -> None:
@@ -480,7 +494,7 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
         _check_positions(rope, inv_freq, positions, n)
     if slot_mapping.dtype is not _types()[3]:
         raise TypeError("slot_mapping is int64")
-    _check_pools(desc, kv_format, k_cache, v_cache)
+    _check_pools(bytes(desc), kv_format, k_cache, v_cache)
     h, d, qp, qs, vp, vs = desc.num_kv_heads, desc.head_dim_qk, None, 0, None, 0
     if q is not None:
         qp, qs = _rows(q, (n, desc.num_q_heads, d))
@@ -502,7 +516,7 @@ def kv_read(desc: AttnDesc, slots, k_cache, v_cache, k_out, v_out, kv_format: in
     rows = slots.shape[0] * desc.num_kv_heads
     if slots.dtype is not int64:
         raise TypeError("slots are int64")
-    _check_pools(desc, kv_format, k_cache, v_cache)
+    _check_pools(bytes(desc), kv_format, k_cache, v_cache)
     if k_out.dtype is not bf16 or k_out.numel() != rows * desc.head_dim_qk or (
             v_out is not None and (v_out.dtype is not bf16 or v_out.numel() != rows * desc.head_dim_v)):
         raise ValueError("k_out and v_out are bf16 [n, Hkv, d]")

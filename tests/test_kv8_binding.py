@@ -127,4 +127,7 @@ def test_runs_of_8_bit_plans_check_the_pools(lib, fmt):
                 fnpu.mixed_attn_run(plan, q, *pools, q, lse, stream=0)
             with pytest.raises((ValueError, TypeError)):
                 fnpu.mixed_step(plan, rows, rows, slots, q, *pools, q, lse, stream=0)
+    plan.desc.num_blocks = 1  # the plan's block ids are of the descriptor that it was made with
+    with pytest.raises(ValueError):
+        fnpu.mixed_attn_run(plan, q, _byte_pool(BLOCK), _byte_pool(BLOCK), q, lse, stream=0)
     assert [name for name, _ in lib.calls] == ["fnpu_mixed_attn_run", "fnpu_mixed_step"]
