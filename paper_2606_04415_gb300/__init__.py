@@ -456,8 +456,14 @@ def _check_pools(shape: bytes, kv_format: int, k_cache, v_cache) -> None:
     if sizes is None:
         return
     dtype, k, v = sizes
+    try:  # tensors as they should be, first
+        if (not isinstance(k_cache, int) and k_cache.dtype is dtype and k_cache.numel() >= k and
+                (v is None or (v_cache.dtype is dtype and v_cache.numel() >= v))):
+            return
+    except AttributeError:
+        pass
     for x, n in ((k_cache, k), (v_cache, v)):
-        if n is None or x is None or isinstance(x, int):
+        if isinstance(x, int) or x is None or n is None:
             continue
         if getattr(x, "dtype", None) is not dtype:
             raise TypeError(f"the pools of cache format {kv_format} are {dtype} tensors")
