@@ -31,6 +31,7 @@ class RotaryCache:
         else:
             shape, dtype = (num_blocks * kv8_block_bytes(self.desc, kv_format),), torch.uint8
         self.k, self.v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        self.plan_of = (bytes(self.desc), kv_format)  # what a plan over this cache was made for
 
     def _empty(self, stream, *outputs):
         """Outputs (shape, dtype) allocated on the stream that writes them: memory that
@@ -39,6 +40,12 @@ class RotaryCache:
             stream = self.torch.cuda.ExternalStream(stream, device=self.k.device)
         with self.torch.cuda.stream(stream):
             return [self.torch.empty(shape, dtype=dtype, device=self.k.device) for shape, dtype in outputs]
+
+    def _own(self, plan: Plan) -> None:
+        """Layers share a plan, caches of another shape or format do not: it reads by its
+        own strides, and its block ids are of its own pool."""
+        if (plan.shape, plan.kv_format) != self.plan_of:
+            raise ValueError("the plan is of a cache of another shape or format")
 
     def append(self, qkv, positions, slot_mapping, stream=None):
         """Store a step's keys and values and return its rotated queries.
@@ -55,6 +62,7 @@ class RotaryCache:
         """A plan of a step over this cache; ``plan``: one of an earlier step to
         rebuild (no allocation in the steady state)."""
         if plan is not None:
+            self._own(plan)
             mixed_attn_replan(plan, query_len, context_len, phase, block_table, opts=opts, stream=stream)
             return plan
         if self.kv_format == KV_BF16:
@@ -63,6 +71,7 @@ class RotaryCache:
 
     def attend(self, plan: Plan, q, stream=None):
         """(out bf16 [tokens, Hq, d], lse fp32 [tokens, Hq]) of the planned step."""
+        self._own(plan)
         out, lse = self._empty(stream, (q.shape, q.dtype), (q.shape[:2], self.torch.float32))
         mixed_attn_run(plan, q, self.k, self.v, out, lse, stream=stream)
         return out, lse

@@ -131,3 +131,35 @@ def test_runs_of_8_bit_plans_check_the_pools(lib, fmt):
     with pytest.raises(ValueError):
         fnpu.mixed_attn_run(plan, q, _byte_pool(BLOCK), _byte_pool(BLOCK), q, lse, stream=0)
     assert [name for name, _ in lib.calls] == ["fnpu_mixed_attn_run", "fnpu_mixed_step"]
+
+
+@pytest.fixture
+def caches(monkeypatch):
+    """Cache objects of three formats whose pools and outputs have no memory."""
+    from paper_2606_04415_gb300.rotary import RotaryCache
+    f = Device(D // 2, dtype=torch.float32)
+    made = {fmt: RotaryCache(HQ, HKV, D, BS, BLOCKS, fnpu.make_rope(D), f, fmt, device="meta") for fmt, _ in GOOD}
+    for fmt, pool in GOOD:
+        made[fmt].k, made[fmt].v = pool(), pool()
+    monkeypatch.setattr(RotaryCache, "_empty", lambda self, stream, *outputs: [Device(*s, dtype=t) for s, t in outputs])
+    monkeypatch.setattr(fnpu, "_lib", Library())
+    return made
+
+
+def test_cache_refuses_another_caches_plan(caches):
+    """A plan of another format or shape reads by other strides, and block ids of a larger
+    pool lie past this one."""
+    meta = (np.array([N]), np.array([N]), np.array([0]), np.zeros((1, 1), np.int32))
+    q, calls = Device(N, HQ, D), fnpu._lib.calls
+    for fmt, cache in caches.items():
+        own = _plan(fmt)  # (another object of the same descriptor: layers share a plan)
+        cache.attend(own, q, stream=0)
+        cache.plan(*meta, plan=own, stream=0)
+        done = len(calls)
+        for bad in (_plan((fmt + 1) % 3), _plan((fmt + 2) % 3), _plan(fmt, _desc(num_blocks=BLOCKS + 1)), _plan(fmt, _desc(block_size=32)),
+                    _plan(fmt, _desc(num_q_heads=8))):
+            with pytest.raises(ValueError):
+                cache.attend(bad, q, stream=0)
+            with pytest.raises(ValueError):
+                cache.plan(*meta, plan=bad, stream=0)
+        assert len(calls) == done
