@@ -72,6 +72,10 @@ class RotaryCache:
     def attend(self, plan: Plan, q, stream=None):
         """(out bf16 [tokens, Hq, d], lse fp32 [tokens, Hq]) of the planned step."""
         self._own(plan)
+        if q.dtype is not self.torch.bfloat16:
+            raise TypeError("queries are bf16")
+        if q.shape != (plan.num_tokens, self.heads[0], self.heads[2]):  # (the outputs are of its size)
+            raise ValueError(f"expected the {plan.num_tokens} planned queries, not {tuple(q.shape)}")
         out, lse = self._empty(stream, (q.shape, q.dtype), (q.shape[:2], self.torch.float32))
         mixed_attn_run(plan, q, self.k, self.v, out, lse, stream=stream)
         return out, lse

@@ -163,3 +163,15 @@ def test_cache_refuses_another_caches_plan(caches):
             with pytest.raises(ValueError):
                 cache.plan(*meta, plan=bad, stream=0)
         assert len(calls) == done
+
+
+def test_attend_refuses_other_queries(caches):
+    """The planned rows are read from q and written to outputs of its size."""
+    calls = fnpu._lib.calls
+    for fmt, cache in caches.items():
+        plan = _plan(fmt)
+        for bad in (Device(N - 1, HQ, D), Device(N + 1, HQ, D), Device(N, HQ - 1, D), Device(N, HQ, D // 2), Device(N, HQ, D, dtype=torch.float16),
+                    Device(N * HQ, D)):
+            with pytest.raises((ValueError, TypeError)):
+                cache.attend(plan, bad, stream=0)
+        assert not calls
