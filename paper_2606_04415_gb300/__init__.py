@@ -430,7 +430,7 @@ def _rows(x, shape):
     s, t, u = x.stride()
     if ((u != 1 and d > 1) or (t != d and h > 1)) and n:
         raise ValueError("the heads and columns of a token must be contiguous")
-    return x.data_ptr(), s if n > 1 else max(s, h * d)
+    return x.data_ptr(), s if n > 1 else h * d  # (of one token any stride may be reported)
 
 
 @functools.lru_cache(maxsize=64)

@@ -175,3 +175,16 @@ def test_attend_refuses_other_queries(caches):
             with pytest.raises((ValueError, TypeError)):
                 cache.attend(plan, bad, stream=0)
         assert not calls
+
+
+def test_one_token_has_no_stride(lib):
+    """The stride between tokens means nothing where there is one; torch may report any."""
+    one = [Device(1, h, D, stride=(s, D, 1), ptr=4096 * (i + 1)) for i, (h, s) in enumerate(((HQ, 301), (HKV, 1), (HKV, 129)))]
+    fnpu.rope_append(_desc(), fnpu.make_rope(D), Device(D // 2, dtype=torch.float32), Device(1, 1, dtype=torch.int32), *one,
+                     Device(1, dtype=torch.int64), Device(1, HQ, D, ptr=4096), _bf16_pool(), _bf16_pool(), stream=0)
+    args = lib.calls[0][1]
+    assert args[6] == HQ * D and args[8] == HKV * D and args[10] == HKV * D  # q (in place), keys, values
+    x = Device(1, HQ, D, stride=(HQ * D + 9, D, 1))
+    fnpu.rope(fnpu.make_rope(D), Device(D // 2, dtype=torch.float32), Device(1, 1, dtype=torch.int32), x, Device(1, HQ, D), stream=0)
+    args = lib.calls[1][1]
+    assert args[4] == args[9] == HQ * D
