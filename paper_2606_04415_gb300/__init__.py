@@ -158,15 +158,13 @@ def status_str(code: int) -> str:
 
 def _dptr(x) -> Optional[int]:
     """Device address of a CUDA tensor / raw int / None."""
+    if x is None or isinstance(x, int):
+        return x
     try:  # a tensor as it should be, first
         if x.is_cuda and x.is_contiguous():
             return x.data_ptr()
     except AttributeError:
         pass
-    if x is None:
-        return None
-    if isinstance(x, int):
-        return x
     if hasattr(x, "data_ptr"):
         if not x.is_cuda:
             raise ValueError("expected a CUDA tensor")

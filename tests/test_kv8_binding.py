@@ -188,3 +188,15 @@ def test_one_token_has_no_stride(lib):
     fnpu.rope(fnpu.make_rope(D), Device(D // 2, dtype=torch.float32), Device(1, 1, dtype=torch.int32), x, Device(1, HQ, D), stream=0)
     args = lib.calls[1][1]
     assert args[4] == args[9] == HQ * D
+
+
+def test_raw_addresses_are_taken_as_they_are():
+    """An integer is not asked for a tensor's attributes first (0.5 us each)."""
+    class Address(int):
+        def __getattr__(self, name):
+            raise AssertionError(name)
+    assert fnpu._dptr(Address(4096)) == 4096 and fnpu._dptr(None) is None
+    assert fnpu._dptr(Device(3, ptr=64)) == 64
+    for bad, error in ((Device(3, contiguous=False), ValueError), (torch.zeros(3), ValueError), ([1], TypeError), (4.0, TypeError)):
+        with pytest.raises(error):
+            fnpu._dptr(bad)
