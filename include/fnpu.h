@@ -411,7 +411,8 @@ int fnpu_mla_expand(const fnpu_attn_desc *desc, const void *latent_cache, const 
  * rotary_dim / 2 + i), or with interleaved = 1 (rotary_offset + 2 i, + 2 i + 1); the
  * other columns are copied. inverse = 1 turns by the negative angle, which is also
  * the gradient: dx is the inverse of dy. Angles are good to about 1e-6 rad below
- * position 2^20 (the product is not rounded to fp32); any int32 position is valid.
+ * position 2^20 (the product is not rounded to fp32) and beyond it to 2^-47 of their
+ * size besides (1.5e-5 rad at 2^31); any int32 position is valid.
  */
 typedef struct {
     int32_t rotary_dim;        /* columns that turn: even, 2..256 */

@@ -10,22 +10,28 @@ namespace fnpu {
 // 100000 the rounded product alone is up to 0.004 rad off. In turns (angle / 2 pi)
 // only the fraction counts, so inv_freq / 2 pi is kept as a sum of two fp32 values
 // (48 bits) and the product's whole turns are dropped before anything small is
-// added. What is left is good to 2^-24 turns for positions below 2^20. (A position
-// beyond 2^24 is cut into two parts that fp32 holds exactly.)
+// added. What is left is good to 2^-24 turns for positions below 2^20, and is 0.52
+// turns at most there (0.71 up to 2^24). A position beyond 2^24 is cut into two parts
+// that fp32 holds exactly; the product's rounding error and the low half's product are
+// whole turns themselves there (up to 16 and 14 at 2^31), dropped likewise, so that the
+// hardware functions get half a turn. The angle is good to 2^-47 of itself.
 __device__ __forceinline__ float rope_turns(int32_t position, float inv_freq) {
     constexpr float kHi = 0.15915494f, kLo = 6.4206382e-09f;  // kHi + kLo = 1 / (2 pi) to 2^-53
     const float f = inv_freq * kHi;
     const float g = __fmaf_rn(inv_freq, kHi, -f) + inv_freq * kLo;
-    auto part = [&](float p) {
-        const float t = p * f;
-        return (t - rintf(t)) + (__fmaf_rn(p, f, -t) + p * g);
-    };
-    if (__builtin_expect(position > 1 << 24 || position < -(1 << 24), 0))
-        return part(static_cast<float>(position & ~4095)) + part(static_cast<float>(position & 4095));
-    return part(static_cast<float>(position));
+    if (__builtin_expect(position > 1 << 24 || position < -(1 << 24), 0)) {
+        auto part = [&](float p) {
+            const float t = p * f, r = __fmaf_rn(p, f, -t), u = p * g;
+            return (t - rintf(t)) + ((r - rintf(r)) + ((u - rintf(u)) + __fmaf_rn(p, g, -u)));
+        };
+        const float s = part(static_cast<float>(position & ~4095)) + part(static_cast<float>(position & 4095));
+        return s - rintf(s);
+    }
+    const float p = static_cast<float>(position), t = p * f;
+    return (t - rintf(t)) + (__fmaf_rn(p, f, -t) + p * g);
 }
-// cosine and sine of a turn's fraction (below 1.1): the hardware functions, whose
-// error of some 2^-20 is far below a bf16 result's
+// cosine and sine of a turn's fraction (0.71 at most, 0.52 below position 2^20): the
+// hardware functions, whose error of some 2^-20 is far below a bf16 result's
 __device__ __forceinline__ void rope_cos_sin(float turns, float &c, float &s) {
     const float a = turns * 6.2831853f;
     c = __cosf(a);
