@@ -517,8 +517,10 @@ int fnpu_kv_read(const fnpu_attn_desc *desc, int32_t kv_format, const int64_t *s
  * fnpu_plan_check, _info, _destroy. Sequences with at most 64 rows a kv head
  * (query_len x Hq / Hkv: one-token decodes, speculative verification, short
  * chunks) attend over the codes directly, of either phase, and so do those of up to
- * 2048 rows where none has more and the planner's model finds it shorter; the
- * others over a bf16 copy of their blocks that each run makes in the plan's workspace.
+ * 2048 rows where none has more, the planner's model finds it shorter and neither a
+ * decode share nor green contexts are asked for; the others over a bf16 copy of their
+ * blocks that each run makes in the plan's workspace. Only these are a prefill phase:
+ * a step without them has no share of SMs or phase times (FNPU_EUNSUPPORTED).
  * Errors: as fnpu_mixed_attn_plan_ex; FNPU_EINVAL for another kv_format;
  * FNPU_EUNSUPPORTED for shapes that the formats do not take and for
  * FNPU_PLAN_NO_TCGEN05.

@@ -946,8 +946,11 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     // with 128. The per-head kernel aims at about 3 waves of 2 CTAs per SM.
     // the queue a sequence's work enters: decode items for one-token decodes
     // (8-bit blocks: whatever has few rows a kv head, of either phase -- see kKv8DecodeRows)
+    // A caller that asks for a share of the SMs or for green contexts asks for two
+    // phases, so there middle chunks are not sent to the decode's queue by the model.
+    const bool asks = o.decode_share_pct > 0 || (o.flags & FNPU_PLAN_GREEN_CONTEXTS);
     const int64_t direct_rows =
-        kv8 && kv8_direct(desc, num_seqs, query_len, context_len, sms) ? kKv8MostRows : kKv8DecodeRows;
+        kv8 && !asks && kv8_direct(desc, num_seqs, query_len, context_len, sms) ? kKv8MostRows : kKv8DecodeRows;
     auto decode_queue = [&](int32_t s) {
         return kv8 ? static_cast<int64_t>(query_len[s]) * G <= direct_rows : phase[s] == 1 && query_len[s] == 1;
     };
@@ -1221,6 +1224,7 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
         // on 2 and 35 short decodes, 22.5 us by the model: 42.2, 47.5). Four kv
         // heads co-locate always: callers of such plans have always been able to
         // read their phase times and share, and a status does not depend on lengths.
+        // (Of an 8-bit cache it does: chunks of few rows are decodes, see above.)
         const double span = static_cast<double>(lpt_makespan(cost_histogram(item_tiles), sms)) * tile_scale * kTileSec;
         const bool wide = 4 * static_cast<int64_t>(tc_units.size()) > 3 * static_cast<int64_t>(sms);
         pl->coloc = span >= (dec_bytes >= 20e-6 * kDecodeAllBps ? 5e-6 : wide ? 25e-6 : 8e-6);
