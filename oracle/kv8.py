@@ -147,3 +147,52 @@ def attention(q, query_len, context_len, block_table, k_pool, v_pool, hkv, bs, d
                     lse[at + i, h] = m + math.log(w.sum())
         at += n
     return out, lse
+
+
+def attention_bound(q, query_len, context_len, block_table, k_pool, v_pool, hkv, bs, d, fmt, staged, scale=None, tokens=None):
+    """As ``attention``, and how far a computation in fp32 with weights rounded once may be
+    off: (out, lse, bound [T, Hq, d]). ``staged[s]``: sequence s attends over a bf16 copy of
+    its blocks (weights in bf16), else over the codes (weights in f16).
+
+    With p_j the softmax weights and u = 2^-9 (bf16) or 2^-11 (f16), weight j is off by at
+    most u p_j. In f16 there is a least step too: weights are w_j = c p_j 2^e_j with e_j the
+    exponent of the block's V scale and the largest w at least 1, so a code enters with
+    an error of 2^-25 / c at most, 1 / c <= max_i p_i 2^e_i. Roundings of different
+    weights are independent: the sum of n terms within a_j exceeds 7 sqrt(sum a_j^2)
+    with probability 2 exp(-49 / 2) < 5e-11 (Hoeffding). Row sums may take the rounded
+    weights or the exact ones, so a term is a weight's error times |v_j| + |out|. Scores are
+    good to the 2e-5 max(1, |lse|) that the log-sum-exp is held to; errors e_j of them move
+    the result by sum p_j e_j (v_j - out). The result is rounded to bf16, 2^-8 of it."""
+    scale = d ** -0.5 if scale is None else scale
+    T, hq, _ = q.shape
+    G = hq // hkv
+    out, lse, bound = np.zeros((T, hq, d)), np.zeros((T, hq)), np.full((T, hq, d), np.inf)
+    at = 0
+    for s, (n, c) in enumerate(zip(query_len, context_len)):
+        n, c = int(n), int(c)
+        mine = [i for i in range(n) if tokens is None or at + i in tokens]
+        if mine:
+            pos = np.arange(c)
+            sl = np.asarray(block_table)[s, pos // bs].astype(np.int64) * bs + pos % bs
+            k, v = read(k_pool, sl, hkv, bs, d, fmt), read(v_pool, sl, hkv, bs, d, fmt)
+            unit = views(v_pool, hkv, bs, d)[1].astype(np.float64)[sl // bs]  # 2^e of each key and head
+            a, a2, code2 = np.abs(v), v * v, (v / unit[:, :, None]) ** 2
+            for i in mine:
+                see = c - n + i + 1
+                for h in range(hq):
+                    kv = h // G
+                    x = (k[:see, kv] @ q[at + i, h]) * scale
+                    m = x.max()
+                    w = np.exp(x - m)
+                    p = w / w.sum()
+                    o = p @ v[:see, kv]
+                    out[at + i, h], lse[at + i, h] = o, m + math.log(w.sum())
+                    p2, size = p * p, np.abs(o)
+                    terms = p2 @ a2[:see, kv] + 2 * size * (p2 @ a[:see, kv]) + size ** 2 * p2.sum()
+                    var = terms * (2.0 ** -18 if staged[s] else 2.0 ** -22)
+                    if not staged[s]:
+                        var = var + (2.0 ** -25 * (p * unit[:see, kv]).max()) ** 2 * code2[:see, kv].sum(0)
+                    bound[at + i, h] = (2.0 ** -8 * size + 7 * np.sqrt(var) +
+                                        2e-5 * max(1.0, abs(lse[at + i, h])) * (p @ np.abs(v[:see, kv] - o)))
+        at += n
+    return out, lse, bound
