@@ -175,7 +175,7 @@ def attention_bound(q, query_len, context_len, block_table, k_pool, v_pool, hkv,
             pos = np.arange(c)
             sl = np.asarray(block_table)[s, pos // bs].astype(np.int64) * bs + pos % bs
             k, v = read(k_pool, sl, hkv, bs, d, fmt), read(v_pool, sl, hkv, bs, d, fmt)
-            unit = views(v_pool, hkv, bs, d)[1].astype(np.float64)[sl // bs]  # 2^e of each key and head
+            unit = views(v_pool, hkv, bs, d)[1][sl // bs].astype(np.float64)  # 2^e of each key and head
             a, a2, code2 = np.abs(v), v * v, (v / unit[:, :, None]) ** 2
             for i in mine:
                 see = c - n + i + 1
