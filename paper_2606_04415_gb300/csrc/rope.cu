@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(256)
         __nv_bfloat16 *to = out + t * out_stride + static_cast<int64_t>(h) * d;
         if (j < r.pairs) {
             float s, c;
-            rope_cos_sin(rope_turns(r.positions[r.axis[j] * r.n + t], r.inv_freq[j]), c, s);
+            rope_cos_sin(rope_turns_any(r.positions[r.axis[j] * r.n + t], r.inv_freq[j]), c, s);
             s *= r.sign;
             const int a = r.offset + (r.interleaved ? 2 * j : j), b = r.interleaved ? a + 1 : a + r.pairs;
             const float u = __bfloat162float(from[a]), v = __bfloat162float(from[b]);
