@@ -265,6 +265,7 @@ class Plan:
         self.num_tokens = num_tokens
         self.kv_format = kv_format
         self.shape = bytes(desc)  # as planned, whatever becomes of ``desc``
+        self.pools = None if kv_format == KV_BF16 else _layout(self.shape, kv_format)[4]
 
     def info(self) -> dict:
         pi, di, la = ctypes.c_int32(), ctypes.c_int32(), ctypes.c_int32()
@@ -317,8 +318,8 @@ def mixed_attn_replan(plan: Plan, query_len, context_len, phase, block_table,
 
 def mixed_attn_run(plan: Plan, q, k_cache, v_cache, out, lse, stream=None) -> None:
     """Attention of every planned query (``fnpu_mixed_attn_run``)."""
-    if plan.kv_format != KV_BF16:
-        _check_pools(plan.shape, plan.kv_format, k_cache, v_cache)
+    if plan.pools is not None:
+        _check_pools(plan.pools, k_cache, v_cache)
     rc = load().fnpu_mixed_attn_run(plan.handle, _dptr(q), _dptr(k_cache), _dptr(v_cache),
                                     _dptr(out), _dptr(lse), _stream(stream))
     if rc != FNPU_OK:
@@ -329,8 +330,8 @@ def mixed_step(plan: Plan, k_new, v_new, slot_mapping, q, k_cache, v_cache, out,
     """Append of the step's new rows and attention of every planned query in
     one call (``fnpu_mixed_step``; the same results as ``kv_append`` then
     ``mixed_attn_run``)."""
-    if plan.kv_format != KV_BF16:
-        _check_pools(plan.shape, plan.kv_format, k_cache, v_cache)
+    if plan.pools is not None:
+        _check_pools(plan.pools, k_cache, v_cache)
     rc = load().fnpu_mixed_step(plan.handle, _dptr(k_new), _dptr(v_new), _dptr(slot_mapping), _dptr(q),
                                 _dptr(k_cache), _dptr(v_cache), _dptr(out), _dptr(lse), _stream(stream))
     if rc != FNPU_OK:
@@ -420,7 +421,7 @@ def _rows(x, shape):
     tokens may lie apart (a slice of a fused projection's output)."""
     if not x.is_cuda:
         raise ValueError("expected a CUDA tensor")
-    if x.dtype is not _types()[0]:
+    if x.dtype is not (_dtypes or _types())[0]:
         raise TypeError("rows are bf16")
     if x.shape != shape:
         raise ValueError(f"expected rows of shape {tuple(shape)}, not {tuple(x.shape)}")
@@ -432,28 +433,26 @@ def _rows(x, shape):
 
 
 @functools.lru_cache(maxsize=64)
-def _pool_sizes(shape: bytes, kv_format: int):
-    """(type, elements of k_cache, of v_cache or None where there is none) of the pools of
-    a descriptor, given as its bytes; None for one that the library refuses."""
+def _layout(shape: bytes, kv_format: int):
+    """What a descriptor, given as its bytes, and a cache format ask of a call's tensors:
+    (query heads, kv heads, d_qk, d_v, pools), the last (type, elements of k_cache, of
+    v_cache or None where there is none), or None for a cache that the library refuses."""
     desc = AttnDesc.from_buffer_copy(shape)
-    if desc.kv_fp8 or not KV_BF16 <= kv_format <= KV_E4M3_BLOCK:
-        return None
-    heads, slots = desc.num_kv_heads, desc.num_blocks * desc.block_size
-    if kv_format == KV_BF16:
-        dtype, k, v = _types()[0], slots * heads * desc.head_dim_qk, slots * heads * desc.head_dim_v
-    else:  # codes, then fp32 scales padded to 16 bytes a block
-        dtype = _types()[4]
-        k = v = slots * heads * desc.head_dim_qk + desc.num_blocks * ((heads + 3) // 4 * 16)
-    return dtype, k, None if desc.v_in_k_latent else v
+    heads, slots, pools = desc.num_kv_heads, desc.num_blocks * desc.block_size, None
+    if kv_format == KV_BF16 and not desc.kv_fp8:
+        pools = (_types()[0], slots * heads * desc.head_dim_qk, None if desc.v_in_k_latent else slots * heads * desc.head_dim_v)
+    elif kv_format in (KV_INT8_BLOCK, KV_E4M3_BLOCK) and not desc.kv_fp8 and not desc.v_in_k_latent:
+        n = slots * heads * desc.head_dim_qk + desc.num_blocks * ((heads + 3) // 4 * 16)  # codes; fp32 scales of a block
+        pools = (_types()[4], n, n)
+    return desc.num_q_heads, heads, desc.head_dim_qk, desc.head_dim_v, pools
 
 
-def _check_pools(shape: bytes, kv_format: int, k_cache, v_cache) -> None:
+def _check_pools(pools, k_cache, v_cache) -> None:
     """Pools (where they are tensors) are of the format's type and hold every block
     that the descriptor speaks of: slots up to there are written and read."""
-    sizes = _pool_sizes(shape, kv_format)
-    if sizes is None:
+    if pools is None:
         return
-    dtype, k, v = sizes
+    dtype, k, v = pools
     try:  # tensors as they should be, first
         if (not isinstance(k_cache, int) and k_cache.dtype is dtype and k_cache.numel() >= k and
                 (v is None or (v_cache.dtype is dtype and v_cache.numel() >= v))):
@@ -464,7 +463,7 @@ def _check_pools(shape: bytes, kv_format: int, k_cache, v_cache) -> None:
         if isinstance(x, int) or x is None or n is None:
             continue
         if getattr(x, "dtype", None) is not dtype:
-            raise TypeError(f"the pools of cache format {kv_format} are {dtype} tensors")
+            raise TypeError(f"the pools of this cache are {dtype} tensors")
         if x.numel() < n:
             raise ValueError(f"a pool of this descriptor has {n} elements, not {x.numel()}")
 
@@ -472,7 +471,8 @@ def _check_pools(shape: bytes, kv_format: int, k_cache, v_cache) -> None:
 def _check_positions(desc: RopeDesc, inv_freq, positions, n: int) -> None:
     if inv_freq.numel() != desc.rotary_dim >> 1 or positions.numel() != desc.num_axes * n:
         raise ValueError("inv_freq is [rotary_dim / 2] and positions are [num_axes, tokens]")
-    if inv_freq.dtype is not _types()[2] or positions.dtype is not _types()[1]:
+    types = _dtypes or _types()
+    if inv_freq.dtype is not types[2] or positions.dtype is not types[1]:
         raise TypeError("inv_freq is fp32 and positions are int32")
 
 
@@ -496,17 +496,19 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
     n = slot_mapping.numel()
     if rope is not None:
         _check_positions(rope, inv_freq, positions, n)
-    if slot_mapping.dtype is not _types()[3]:
+    bf16, _, _, int64, _ = _dtypes or _types()
+    if slot_mapping.dtype is not int64:
         raise TypeError("slot_mapping is int64")
-    _check_pools(bytes(desc), kv_format, k_cache, v_cache)
-    h, d, qp, qs, vp, vs = desc.num_kv_heads, desc.head_dim_qk, None, 0, None, 0
+    hq, h, d, dv, pools = _layout(bytes(desc), kv_format)
+    _check_pools(pools, k_cache, v_cache)
+    qp, qs, vp, vs = None, 0, None, 0
     if q is not None:
-        qp, qs = _rows(q, (n, desc.num_q_heads, d))
-        if q_out is None or q_out.dtype is not _types()[0] or q_out.shape != q.shape:
+        qp, qs = _rows(q, (n, hq, d))
+        if q_out is None or q_out.dtype is not bf16 or q_out.shape != q.shape:
             raise ValueError("q_out is bf16, of the shape of q")
     kp, ks = _rows(k_new, (n, h, d))
     if v_new is not None:
-        vp, vs = _rows(v_new, (n, h, desc.head_dim_v))
+        vp, vs = _rows(v_new, (n, h, dv))
     rc = (_lib or load()).fnpu_rope_append(ctypes.byref(desc), int(kv_format), None if rope is None else ctypes.byref(rope),
                                  _dptr(inv_freq), _dptr(positions), qp, qs, kp, ks, vp, vs, _dptr(slot_mapping), n,
                                  _dptr(q_out), _dptr(k_cache), _dptr(v_cache), _stream(stream))
@@ -516,13 +518,14 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
 
 def kv_read(desc: AttnDesc, slots, k_cache, v_cache, k_out, v_out, kv_format: int = KV_BF16, stream=None) -> None:
     """The rows that ``slots`` store, as bf16 (``fnpu_kv_read``)."""
-    bf16, _, _, int64, _ = _types()
-    rows = slots.shape[0] * desc.num_kv_heads
+    bf16, _, _, int64, _ = _dtypes or _types()
     if slots.dtype is not int64:
         raise TypeError("slots are int64")
-    _check_pools(bytes(desc), kv_format, k_cache, v_cache)
-    if k_out.dtype is not bf16 or k_out.numel() != rows * desc.head_dim_qk or (
-            v_out is not None and (v_out.dtype is not bf16 or v_out.numel() != rows * desc.head_dim_v)):
+    _, h, d, dv, pools = _layout(bytes(desc), kv_format)
+    _check_pools(pools, k_cache, v_cache)
+    rows = slots.shape[0] * h
+    if k_out.dtype is not bf16 or k_out.numel() != rows * d or (
+            v_out is not None and (v_out.dtype is not bf16 or v_out.numel() != rows * dv)):
         raise ValueError("k_out and v_out are bf16 [n, Hkv, d]")
     rc = load().fnpu_kv_read(ctypes.byref(desc), int(kv_format), _dptr(slots), int(slots.shape[0]), _dptr(k_cache),
                              _dptr(v_cache), _dptr(k_out), _dptr(v_out), _stream(stream))
