@@ -459,7 +459,11 @@ int fnpu_rope(const fnpu_rope_desc *rope, const float *inv_freq, const int32_t *
  * append to a block that holds rows already (its first slot is not among the
  * appended) keeps the larger of the exponent so far and the one that the new rows
  * need; where it grows, the rows before are stored anew from their stored values.
- * An append of a block's first slot starts the block afresh, whatever it held.
+ * An append of a block's first slot starts the block afresh, whatever it held; a
+ * block's first rows must include its first slot, or they meet the exponent of what
+ * was there before. Since an append may store the block's other rows anew, a block that
+ * several sequences share (a common prefix) must be full before it is shared, and
+ * nothing may read a block while an append to it runs.
  * NaN is stored as zero and an infinity as the largest magnitude; they, and finite
  * magnitudes above the largest at e = 60 (which saturate), raise the library-wide
  * device flag (FNPU_EDEVICE_RANGE from fnpu_check).

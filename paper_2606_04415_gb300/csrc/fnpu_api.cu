@@ -183,13 +183,17 @@ void release_plan(fnpu_plan *pl) {
 // whole device about 4 TB/s.
 constexpr double kTileSec = 1.5e-6;
 constexpr double kDecodeSmBps = 69e9;
-constexpr double kDecodeSmBpsFp8 = 50e9;  // (bytes of the FP8 cache: the conversion bounds it)
+// Bytes of the FP8 cache, whose conversion bounds it. The 8-bit block cache is planned with
+// the same figure: its decode reads faster (some 190 GB/s an SM by itself), but what it
+// reads on a few SMs beside a prefill has not been measured.
+constexpr double kDecodeSmBpsFp8 = 50e9;
 constexpr double kDecodeAllBps = 4.0e12;
 
 // 8-bit block cache: sequences of up to this many rows a kv head (query tokens x
 // G) always go to the decode kernel, which reads the codes once for each item's
 // rows (40 sequences of 9 x 7 rows on 700..3000 keys: 66 us, 82 staged; of 18 x 7: 116
-// and 82).
+// and 82). (66 in the ranges that kv8_split chooses; whole sequences in items of 32
+// rows take 50, so with a better model the line might lie higher.)
 constexpr int64_t kKv8DecodeRows = 64;
 
 // Two packed Q tiles of one kv head (the tcgen05 prefill unit) before its key

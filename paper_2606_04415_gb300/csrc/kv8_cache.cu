@@ -263,7 +263,9 @@ __global__ void __launch_bounds__(256)
 
 // ----------------------------------------------------------------- staging
 //
-// The tcgen05 prefill takes bf16 operands, which hold the stored values exactly.
+// The tcgen05 prefill takes bf16 operands, which hold the stored values exactly; f16
+// would not hold their range. Its weights are then bf16 too, 2^-9 off at most each where the
+// decode kernel's are f16 and 2^-11: whether a middle chunk is staged depends on the step.
 // A CTA writes one kv head of a source block, K and V, as bf16 rows [slots][kv
 // heads][d] of block `dst`; rows past `valid` are zero.
 template <int kFormat>

@@ -7,13 +7,15 @@
 // value against some 5 operations, and an angle costs about 20 instructions but
 // serves every head of its token. 24000 tokens of 28 heads of 128: 54 us for 344 MB
 // (51 at the copy rate). The append beside it moves 201 MB for 8192 tokens of 32/8
-// heads in 38 us (30): a warp's chain of loads, angles and stores, at 28 warps an SM.
+// heads in 37.6 us (30): a warp's chain of loads, angles and stores, at 28 warps an SM.
 #include "rope.cuh"
 
 namespace fnpu {
 namespace {
 
-constexpr int kWarpsPerCta = 4, kCtasPerSm = 8, kAppendCtasPerSm = 7;  // latency is hidden by warps: 64 registers, 32 warps an SM
+// Latency is hidden by warps: 32 an SM for the rotation (64 registers), 28 for the append
+// (72, and still 32 bytes of spills a thread, 48 where a warp has several tokens).
+constexpr int kWarpsPerCta = 4, kCtasPerSm = 8, kAppendCtasPerSm = 7;
 // Passes over the heads of one warp, at most. The rotation by itself is best at 4 for
 // some waves (5000 tokens, 28 heads: 13.8 us, 15.4 with 7) and at 8 for many, where the
 // angles' work counts (24000 tokens on three axes: 53.7 us, 56.6 with 4); the append,
@@ -42,7 +44,9 @@ __global__ void __launch_bounds__(32 * kWarpsPerCta, kCtasPerSm)
 }
 
 // Any even rotary width, offset, stride and alignment: a thread per pair of a
-// row, then per column that does not turn.
+// row, then per column that does not turn. For rows that are off 8 bytes; an angle a pair
+// and 2-byte accesses: 24000 tokens of 28 heads of 128 one column off take 310 us (54
+// aligned, 51 at the copy rate), 20000 of 8 x 80 49 us.
 __global__ void __launch_bounds__(256)
     rope_any_kernel(const __grid_constant__ RopeArgs r, const __nv_bfloat16 *x, int64_t x_stride, int heads, int d,
                     __nv_bfloat16 *out, int64_t out_stride) {
