@@ -174,6 +174,13 @@ def _dptr(x) -> Optional[int]:
     raise TypeError(f"cannot take a device address of {type(x)!r}")
 
 
+def _tptr(x) -> Optional[int]:
+    """``_dptr`` of what is known to be a tensor, but for one that it refuses."""
+    if x.is_cuda and x.is_contiguous():
+        return x.data_ptr()
+    return _dptr(x)
+
+
 _raw_stream = None  # (device index) -> raw handle of torch's current stream
 _current_device = None  # () -> index of the current device
 
@@ -318,10 +325,8 @@ def mixed_attn_replan(plan: Plan, query_len, context_len, phase, block_table,
 
 def mixed_attn_run(plan: Plan, q, k_cache, v_cache, out, lse, stream=None) -> None:
     """Attention of every planned query (``fnpu_mixed_attn_run``)."""
-    if plan.pools is not None:
-        _check_pools(plan.pools, k_cache, v_cache)
-    rc = load().fnpu_mixed_attn_run(plan.handle, _dptr(q), _dptr(k_cache), _dptr(v_cache),
-                                    _dptr(out), _dptr(lse), _stream(stream))
+    kp, vp = (_dptr(k_cache), _dptr(v_cache)) if plan.pools is None else _pool_addresses(plan.pools, k_cache, v_cache)
+    rc = load().fnpu_mixed_attn_run(plan.handle, _dptr(q), kp, vp, _dptr(out), _dptr(lse), _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_mixed_attn_run")
 
@@ -330,10 +335,9 @@ def mixed_step(plan: Plan, k_new, v_new, slot_mapping, q, k_cache, v_cache, out,
     """Append of the step's new rows and attention of every planned query in
     one call (``fnpu_mixed_step``; the same results as ``kv_append`` then
     ``mixed_attn_run``)."""
-    if plan.pools is not None:
-        _check_pools(plan.pools, k_cache, v_cache)
-    rc = load().fnpu_mixed_step(plan.handle, _dptr(k_new), _dptr(v_new), _dptr(slot_mapping), _dptr(q),
-                                _dptr(k_cache), _dptr(v_cache), _dptr(out), _dptr(lse), _stream(stream))
+    kp, vp = (_dptr(k_cache), _dptr(v_cache)) if plan.pools is None else _pool_addresses(plan.pools, k_cache, v_cache)
+    rc = load().fnpu_mixed_step(plan.handle, _dptr(k_new), _dptr(v_new), _dptr(slot_mapping), _dptr(q), kp, vp,
+                                _dptr(out), _dptr(lse), _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_mixed_step")
 
@@ -447,25 +451,26 @@ def _layout(shape: bytes, kv_format: int):
     return desc.num_q_heads, heads, desc.head_dim_qk, desc.head_dim_v, pools
 
 
-def _check_pools(pools, k_cache, v_cache) -> None:
-    """Pools (where they are tensors) are of the format's type and hold every block
-    that the descriptor speaks of: slots up to there are written and read."""
-    if pools is None:
-        return
-    dtype, k, v = pools
-    try:  # tensors as they should be, first
-        if (not isinstance(k_cache, int) and k_cache.dtype is dtype and k_cache.numel() >= k and
-                (v is None or (v_cache.dtype is dtype and v_cache.numel() >= v))):
-            return
-    except AttributeError:
-        pass
-    for x, n in ((k_cache, k), (v_cache, v)):
-        if isinstance(x, int) or x is None or n is None:
-            continue
-        if getattr(x, "dtype", None) is not dtype:
-            raise TypeError(f"the pools of this cache are {dtype} tensors")
-        if x.numel() < n:
-            raise ValueError(f"a pool of this descriptor has {n} elements, not {x.numel()}")
+def _pool_addresses(pools, k_cache, v_cache):
+    """The addresses of both pools, which (where they are tensors) are of the format's type
+    and hold every block that the descriptor speaks of: slots up to there are written and
+    read."""
+    if pools is not None:
+        dtype, k, v = pools
+        try:  # tensors as they should be, first
+            if (not isinstance(k_cache, int) and k_cache.dtype is dtype and k_cache.numel() >= k and v is not None and
+                    v_cache.dtype is dtype and v_cache.numel() >= v):
+                return _tptr(k_cache), _tptr(v_cache)
+        except AttributeError:
+            pass
+        for x, n in ((k_cache, k), (v_cache, v)):
+            if isinstance(x, int) or x is None or n is None:
+                continue
+            if getattr(x, "dtype", None) is not dtype:
+                raise TypeError(f"the pools of this cache are {dtype} tensors")
+            if x.numel() < n:
+                raise ValueError(f"a pool of this descriptor has {n} elements, not {x.numel()}")
+    return _dptr(k_cache), _dptr(v_cache)
 
 
 def _check_positions(desc: RopeDesc, inv_freq, positions, n: int) -> None:
@@ -483,7 +488,7 @@ def rope(desc: RopeDesc, inv_freq, positions, x, out=None, stream=None) -> None:
     out = x if out is None else out
     _check_positions(desc, inv_freq, positions, n)
     (xp, xs), (op, os_) = _rows(x, x.shape), _rows(out, x.shape)
-    rc = load().fnpu_rope(ctypes.byref(desc), _dptr(inv_freq), _dptr(positions), xp, xs, h, d, n, op, os_, _stream(stream))
+    rc = load().fnpu_rope(ctypes.byref(desc), _tptr(inv_freq), _tptr(positions), xp, xs, h, d, n, op, os_, _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_rope")
 
@@ -494,24 +499,26 @@ def rope_append(desc: AttnDesc, rope: Optional[RopeDesc], inv_freq, positions, q
     slots, and store its values (``fnpu_rope_append``); q, k_new and v_new are
     [n, heads, d], their tokens possibly apart. ``rope`` None: rows as they are."""
     n = slot_mapping.numel()
+    fp, pp = None, None
     if rope is not None:
         _check_positions(rope, inv_freq, positions, n)
+        fp, pp = _tptr(inv_freq), _tptr(positions)
     bf16, _, _, int64, _ = _dtypes or _types()
     if slot_mapping.dtype is not int64:
         raise TypeError("slot_mapping is int64")
     hq, h, d, dv, pools = _layout(bytes(desc), kv_format)
-    _check_pools(pools, k_cache, v_cache)
-    qp, qs, vp, vs = None, 0, None, 0
+    kc, vc = _pool_addresses(pools, k_cache, v_cache)
+    qp, qs, op, vp, vs = None, 0, None, None, 0
     if q is not None:
         qp, qs = _rows(q, (n, hq, d))
         if q_out is None or q_out.dtype is not bf16 or q_out.shape != q.shape:
             raise ValueError("q_out is bf16, of the shape of q")
+        op = _tptr(q_out)
     kp, ks = _rows(k_new, (n, h, d))
     if v_new is not None:
         vp, vs = _rows(v_new, (n, h, dv))
-    rc = (_lib or load()).fnpu_rope_append(ctypes.byref(desc), int(kv_format), None if rope is None else ctypes.byref(rope),
-                                 _dptr(inv_freq), _dptr(positions), qp, qs, kp, ks, vp, vs, _dptr(slot_mapping), n,
-                                 _dptr(q_out), _dptr(k_cache), _dptr(v_cache), _stream(stream))
+    rc = (_lib or load()).fnpu_rope_append(ctypes.byref(desc), int(kv_format), None if rope is None else ctypes.byref(rope), fp, pp,
+                                           qp, qs, kp, ks, vp, vs, _tptr(slot_mapping), n, op, kc, vc, _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_rope_append")
 
@@ -522,13 +529,13 @@ def kv_read(desc: AttnDesc, slots, k_cache, v_cache, k_out, v_out, kv_format: in
     if slots.dtype is not int64:
         raise TypeError("slots are int64")
     _, h, d, dv, pools = _layout(bytes(desc), kv_format)
-    _check_pools(pools, k_cache, v_cache)
+    kc, vc = _pool_addresses(pools, k_cache, v_cache)
     rows = slots.shape[0] * h
     if k_out.dtype is not bf16 or k_out.numel() != rows * d or (
             v_out is not None and (v_out.dtype is not bf16 or v_out.numel() != rows * dv)):
         raise ValueError("k_out and v_out are bf16 [n, Hkv, d]")
-    rc = load().fnpu_kv_read(ctypes.byref(desc), int(kv_format), _dptr(slots), int(slots.shape[0]), _dptr(k_cache),
-                             _dptr(v_cache), _dptr(k_out), _dptr(v_out), _stream(stream))
+    rc = (_lib or load()).fnpu_kv_read(ctypes.byref(desc), int(kv_format), _tptr(slots), slots.shape[0], kc, vc, _tptr(k_out),
+                                       _dptr(v_out), _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_kv_read")
 
