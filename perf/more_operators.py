@@ -239,6 +239,8 @@ def prepare(case, seed):
             x["plan"] = fnpu.window_attn_plan(x["desc"], case["window"], case["sinks"], x["q_len"], x["ctx"], x["phase"], x["bt"])
         elif case["path"] == "rows":
             x["most"] = int(x["ctx"].max())
+            n = fnpu.window_decode_workspace(x["desc"], case["window"], case["sinks"], len(x["ctx"]), x["most"])
+            x["workspace"] = torch.empty(n, dtype=torch.uint8, device="cuda")
         else:
             x["pages"] = fnpu.make_pages(case["bs"], x["blocks"])
             x["workspace"] = torch.empty(fnpu.pages_workspace(x["pages"], x["R"]), dtype=torch.uint8, device="cuda")
@@ -388,7 +390,7 @@ def run(x):
             x["fnpu"].mixed_attn_run(x["plan"], x["q"], x["k"], x["v"], x["out"], x["lse"])
         elif own:
             x["fnpu"].window_decode(x["desc"], case["window"], case["sinks"], x["ctx_dev"], x["bt_dev"], x["most"], x["q"], x["k"], x["v"],
-                                    x["out"], x["lse"])
+                                    x["out"], x["lse"], x["workspace"])
         else:
             n, t = case["chunks"], case["chunks"] * case["chunk"]
             _attend(x, 0, n, 0, t, x["out"], x["lse"])
