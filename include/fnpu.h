@@ -533,6 +533,63 @@ int fnpu_kv8_attn_plan(const fnpu_attn_desc *desc, int32_t kv_format, int32_t nu
                        const int32_t *context_len, const uint8_t *phase, const int32_t *block_table,
                        int32_t block_table_stride, const fnpu_plan_opts *opts, void *stream, fnpu_plan **out);
 
+/*
+ * Attention with a sliding window and sinks. A query at position p of its
+ * sequence sees key j iff
+ *   j <= p  and  (j > p - window  or  j < sinks):
+ * the last `window` keys, its own among them, and the first `sinks` of the
+ * sequence, which stay visible however long it becomes. Softmax, O and LSE run
+ * over the visible keys; all else is as in fnpu_mixed_attn_plan_ex, whose
+ * arguments these are, and the plan is run, re-planned (with the same window),
+ * checked and destroyed like any other. window >= the longest context is causal
+ * attention; any window >= 1 and sinks >= 0 will do.
+ * Only what some query of the step sees is read. A block of a sequence that lies
+ * wholly between its sinks and the window of its first query in the step may be
+ * gone: its block-table entry may hold anything (-1, another sequence's block),
+ * and hidden rows of other blocks may hold anything too, NaN included. (A row
+ * that one query of a prefill chunk sees and another does not must be finite.)
+ * Supports split K/V bf16 caches, d_qk = d_v in {64, 128}: one-token decodes with
+ * Hq / Hkv <= 8 and blocks of a multiple of 16 tokens, prefill chunks and
+ * multi-token decodes with blocks of 16, 32 or 64.
+ * Errors: as fnpu_mixed_attn_plan_ex; FNPU_EINVAL for window < 1 or sinks < 0;
+ * FNPU_EUNSUPPORTED for other caches and with FNPU_PLAN_NO_TCGEN05.
+ */
+int fnpu_window_attn_plan(const fnpu_attn_desc *desc, int32_t window, int32_t sinks, int32_t num_seqs,
+                          const int32_t *query_len, const int32_t *context_len, const uint8_t *phase,
+                          const int32_t *block_table, int32_t block_table_stride, const fnpu_plan_opts *opts,
+                          void *stream, fnpu_plan **out);
+
+/*
+ * The same for one token a sequence without a plan: lengths and block table are
+ * device data, as fnpu_pages_fork leaves them, so a decode loop needs no host
+ * work between its steps and can be captured in a graph.
+ *   context_len   device int32 [num_seqs], each in [0, max_context_len] (counts the
+ *                 new token); 0: an empty row, whose out is 0 and whose lse is -inf
+ *   block_table   device int32 [num_seqs, block_table_stride], stride >=
+ *                 ceil(max_context_len / block_size); hidden blocks as above
+ *   max_context_len  host bound on context_len; with the window it sizes the grid
+ *   split_keys    keys per split, a multiple of 64; 0 leaves it to the library
+ *   workspace     device, 16-byte aligned, of at least the bytes that
+ *                 fnpu_window_decode_workspace gives for the same arguments (NULL where
+ *                 that is 0); calls that overlap on the GPU, captured graphs among them,
+ *                 need one each. Nothing in it is kept from call to call.
+ * A sequence whose context_len lies outside [0, max_context_len] is skipped (its
+ * rows stay as they were) and a visible block's id outside [0, num_blocks) is never
+ * loaded (the sequence's result is then undefined); either raises the library-wide
+ * error flag (FNPU_EDEVICE_RANGE from fnpu_check). The first call on a device
+ * loads the kernels' code: make it before a stream capture.
+ * Supports what fnpu_window_attn_plan does for one-token decodes.
+ * Errors: FNPU_EINVAL for bad arguments or a workspace that is too small,
+ * FNPU_EUNSUPPORTED, FNPU_ECUDA. Nothing is launched on error.
+ */
+int fnpu_window_decode_workspace(const fnpu_attn_desc *desc, int32_t window, int32_t sinks, int32_t num_seqs,
+                                 int32_t max_context_len, int32_t split_keys, int64_t *bytes);
+int fnpu_window_decode(const fnpu_attn_desc *desc, int32_t window, int32_t sinks, int32_t num_seqs,
+                       const int32_t *context_len, const int32_t *block_table, int32_t block_table_stride,
+                       int32_t max_context_len, int32_t split_keys, const void *q, const void *k_cache,
+                       const void *v_cache, void *out, float *lse, void *workspace, int64_t workspace_bytes,
+                       void *stream);
+
 #ifdef __cplusplus
 }
 #endif

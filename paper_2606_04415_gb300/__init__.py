@@ -12,6 +12,8 @@ kernels. Functions carry the C names without the ``fnpu_`` prefix:
     rope_append(desc, rope, inv_freq, positions, q, k_new, v_new, slot_mapping, q_out, k_cache, v_cache, kv_format=0)
     kv_read(desc, slots, k_cache, v_cache, k_out, v_out, kv_format=0)
     kv8_attn_plan(desc, kv_format, query_len, context_len, phase, block_table, opts=None, stream=None)
+    window_attn_plan(desc, window, sinks, query_len, context_len, phase, block_table, opts=None, stream=None)
+    window_decode(desc, window, sinks, context_len, block_table, max_context_len, q, k_cache, v_cache, out, lse, workspace)
     check(stream=None), plan_check(plan, stream=None), status_str(code)
 
 Device arguments are CUDA torch tensors (torch supplies device memory and
@@ -54,7 +56,8 @@ EXPORTED = (
     "fnpu_version", "fnpu_decode_attn_noalloc", "fnpu_last_cuda_error", "fnpu_plan_phase_ms",
     "fnpu_dispatch_next_share", "fnpu_mla_expand", "fnpu_mixed_attn_replan",
     "fnpu_plan_decode_share", "fnpu_mixed_step", "fnpu_rope", "fnpu_rope_append", "fnpu_kv_read",
-    "fnpu_kv8_block_bytes", "fnpu_kv8_attn_plan",
+    "fnpu_kv8_block_bytes", "fnpu_kv8_attn_plan", "fnpu_window_attn_plan", "fnpu_window_decode_workspace",
+    "fnpu_window_decode",
 )
 
 
@@ -136,7 +139,12 @@ def load(build_if_missing: bool = True):
     lib.fnpu_kv8_block_bytes.argtypes = [ctypes.POINTER(AttnDesc), i32, i64p]
     lib.fnpu_kv8_attn_plan.argtypes = [ctypes.POINTER(AttnDesc), i32, i32, P, P, P, P, i32, ctypes.POINTER(PlanOpts), P,
                                        ctypes.POINTER(P)]
-    for name in ("fnpu_rope", "fnpu_rope_append", "fnpu_kv_read", "fnpu_kv8_block_bytes", "fnpu_kv8_attn_plan"):
+    DP = ctypes.POINTER(AttnDesc)
+    lib.fnpu_window_attn_plan.argtypes = [DP, i32, i32, i32, P, P, P, P, i32, ctypes.POINTER(PlanOpts), P, ctypes.POINTER(P)]
+    lib.fnpu_window_decode_workspace.argtypes = [DP, i32, i32, i32, i32, i32, i64p]
+    lib.fnpu_window_decode.argtypes = [DP, i32, i32, i32, P, P, i32, i32, i32, P, P, P, P, P, P, i64, P]
+    for name in ("fnpu_rope", "fnpu_rope_append", "fnpu_kv_read", "fnpu_kv8_block_bytes", "fnpu_kv8_attn_plan",
+                 "fnpu_window_attn_plan", "fnpu_window_decode_workspace", "fnpu_window_decode"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("fnpu_kv_append", "fnpu_mixed_attn_plan", "fnpu_mixed_attn_plan_ex",
                  "fnpu_mixed_attn_run", "fnpu_plan_check", "fnpu_check", "fnpu_plan_info",
@@ -560,3 +568,66 @@ def kv8_attn_plan(desc: AttnDesc, kv_format: int, query_len, context_len, phase,
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_kv8_attn_plan")
     return Plan(out.value, desc, int(ql.sum()), int(kv_format))
+
+
+def window_attn_plan(desc: AttnDesc, window: int, sinks: int, query_len, context_len, phase, block_table,
+                     opts: Optional[PlanOpts] = None, stream=None) -> Plan:
+    """A plan in which a query sees the last ``window`` keys up to its own and the
+    first ``sinks`` of its sequence (``fnpu_window_attn_plan``); blocks that no
+    query sees may be gone from the block table."""
+    arrays, addr = _step_meta(query_len, context_len, phase, block_table)
+    ql = arrays[0]
+    out = ctypes.c_void_p()
+    rc = load().fnpu_window_attn_plan(ctypes.byref(desc), int(window), int(sinks), ql.shape[0], *addr,
+                                      None if opts is None else ctypes.byref(opts), _stream(stream), ctypes.byref(out))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_window_attn_plan")
+    plan = Plan(out.value, desc, int(ql.sum()))
+    plan.window = (int(window), int(sinks))
+    return plan
+
+
+def window_decode_workspace(desc: AttnDesc, window: int, sinks: int, num_seqs: int, max_context_len: int, split_keys: int = 0) -> int:
+    """Bytes of workspace that ``window_decode`` needs for these arguments."""
+    out = ctypes.c_int64()
+    rc = load().fnpu_window_decode_workspace(ctypes.byref(desc), int(window), int(sinks), int(num_seqs), int(max_context_len),
+                                             int(split_keys), ctypes.byref(out))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_window_decode_workspace")
+    return out.value
+
+
+def _int32(x, name: str, *shape):
+    """Address of a contiguous int32 tensor of that shape (None: any extent)."""
+    if x.dtype is not (_dtypes or _types())[1]:
+        raise TypeError(f"{name} is int32")
+    if x.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, x.shape)):
+        raise ValueError(f"expected {name} of shape {shape}, not {tuple(x.shape)}")
+    return _tptr(x)
+
+
+def window_decode(desc: AttnDesc, window: int, sinks: int, context_len, block_table, max_context_len: int, q, k_cache, v_cache, out,
+                  lse, workspace, split_keys: int = 0, stream=None) -> None:
+    """One token a sequence under a window and sinks, with lengths and block table
+    on the device (``fnpu_window_decode``); ``workspace``: a byte tensor of
+    ``window_decode_workspace`` bytes, not shared by calls that may overlap."""
+    n = context_len.shape[0]
+    bf16, _, fp32, _, _ = _dtypes or _types()
+    hq, _, d, _, pools = _layout(bytes(desc), KV_BF16)
+    cp, bp = _int32(context_len, "context_len", None), _int32(block_table, "block_table", n, None)
+    for x in (q, out):
+        if x.dtype is not bf16 or x.shape != (n, hq, d):
+            raise ValueError("q and out are bf16 [rows, Hq, d]")
+    if lse.dtype is not fp32 or lse.shape != (n, hq):
+        raise ValueError("lse is fp32 [rows, Hq]")
+    kp, vp = _pool_addresses(pools, k_cache, v_cache)
+    rc = (_lib or load()).fnpu_window_decode(ctypes.byref(desc), int(window), int(sinks), n, cp, bp, block_table.shape[1],
+                                             int(max_context_len), int(split_keys), _tptr(q), kp, vp, _tptr(out), _tptr(lse),
+                                             *_workspace(workspace), _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_window_decode")
+
+
+def _workspace(x):
+    """(address, bytes) of a workspace tensor or None."""
+    return (None, 0) if x is None else (_tptr(x), x.numel() * x.element_size())

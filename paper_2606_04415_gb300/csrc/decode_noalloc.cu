@@ -307,7 +307,7 @@ int scratch_address(float **out) {
             cudaGetLastError();
             return FNPU_ECUDA;
         }
-        for (int rc : {prepare_decode_tma_noplan(), prepare_noalloc<64>(), prepare_noalloc<128>()})
+        for (int rc : {prepare_decode_tma_noplan(false), prepare_noalloc<64>(), prepare_noalloc<128>()})
             if (rc != FNPU_OK) return rc;
         g_scratch_addr[dev] = static_cast<float *>(ptr);
     }

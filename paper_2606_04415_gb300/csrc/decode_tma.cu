@@ -55,6 +55,15 @@
 // a sequence and head group, CTA b takes items b, b + grid, ... that its
 // sequence's context reaches, and lengths and block ids, which are device
 // data, are checked as they are read.
+//
+// With a window and sinks (kWindow: visible keys are those below p.sinks and
+// from lo = ctx - window on) an item's keys are virtual: the gap of whole 16-key
+// stages between the sinks' last and the window's first is cut out, stage v of
+// the sequence being stage v below the sinks' end and v + skip from there on.
+// Items, splits and the merge then work as on a shorter sequence, every stage
+// has a visible key, and at most two have hidden ones in their middle, which
+// are masked and whose V rows are zeroed like those past the context. Block ids
+// are held a stage, not a block, as the jump may lie inside a block.
 #include <math.h>
 
 #include "common.cuh"
@@ -64,7 +73,7 @@ namespace fnpu {
 namespace {
 
 constexpr int kHkv = 4;          // kv heads per item
-constexpr int kKeys = 16;        // keys per stage
+constexpr int kKeys = kDecodeStageKeys;  // keys per stage
 constexpr int kWarps = 4;        // compute warps, one per kv head
 constexpr int kThreads = 32 * (kWarps + 1);  // + the TMA producer warp
 constexpr int kHalfBytes = kHkv * kKeys * 128;  // all heads, one 64-column half
@@ -105,7 +114,20 @@ struct DtGeo {
     int split, ns, part_base, group;
     int b0, b1, b2, b3;  // ids of the item's first four blocks
     int head0;      // first kv head
+    int skip, lo;   // window: stages left out behind the sinks, first key of the window
 };
+
+// Real key of a virtual one (both at the start of a stage).
+__device__ __forceinline__ int real_key(const AttnParams &p, int skip, int key) {
+    return key < p.sink_keys ? key : key + skip * kKeys;
+}
+// The virtual sequence of a context under p's window: keys, stages left out, first key of the window.
+__device__ __forceinline__ void window_of(const AttnParams &p, int ctx, int &keys, int &skip, int &lo) {
+    lo = ctx > p.window ? ctx - p.window : 0;
+    skip = (lo - p.sink_keys) / kKeys;
+    if (lo < p.sink_keys) skip = 0;
+    keys = ctx - skip * kKeys;
+}
 
 template <int D>
 __device__ __forceinline__ void load_q(const AttnParams &p, int t, int head, int g8, int c,
@@ -133,8 +155,13 @@ __device__ __forceinline__ void bf16x2_split(float x, float y, uint32_t &part, u
     rest = pack_bf16x2(x - __uint_as_float(a & 0xFFFF0000u), y - __uint_as_float(b & 0xFFFF0000u));
 }
 
-// block ids of the item's blocks, relative block `lane` in lane `lane`
+// block ids of the item's blocks, relative block `lane` in lane `lane` (window: of stage `lane`)
+template <bool kWindow>
 __device__ __forceinline__ int load_blk_lane(const AttnParams &p, const DtGeo &g, int lane) {
+    if constexpr (kWindow) {
+        const int key = g.kb + lane * kKeys;
+        return key < g.ke ? __ldg(p.block_table + static_cast<int64_t>(g.bt_row) * p.bt_stride + real_key(p, g.skip, key) / p.block_size) : 0;
+    }
     const int b0 = g.kb / p.block_size;
     const int nblk = (g.ke - 1) / p.block_size - b0 + 1;
     return lane < nblk ? __ldg(p.block_table + static_cast<int64_t>(g.bt_row) * p.bt_stride + b0 + lane) : 0;
@@ -150,7 +177,7 @@ __device__ __forceinline__ int load_blk_lane(const AttnParams &p, const DtGeo &g
 // heads) and 1.77e-3 with one (64), where one operand gives 1.81e-3 and 1.83e-3
 // and two 1.64e-3 and 1.66e-3. They cost 43.2 -> 45.0 us of that call, and a
 // light step of four kv heads, which always had one, would pay 14.3 -> 15.0.
-template <int D, bool kRagged, int kStages, bool kNoPlan, bool kFineP>
+template <int D, bool kRagged, int kStages, bool kNoPlan, bool kFineP, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 3)
     decode_tma_kernel(const AttnParams p, const __grid_constant__ DtMaps maps) {
     using Cfg = DtCfg<D, kStages>;
@@ -178,11 +205,13 @@ __global__ void __launch_bounds__(kThreads, 3)
     auto noplan_item = [&](int i, DecodeItem &it) -> bool {
         const int groups = (p.num_kv_heads + kHkv - 1) / kHkv, per = p.na_num_seqs * groups;
         const int split = i / per, r = i - split * per, seq = r / groups, hg = r - seq * groups;
-        const int ctx = p.na_ctx[seq];
+        int ctx = p.na_ctx[seq];
+        if (kWindow && ctx == 0) return false;  // an empty row, written at the start
         if (ctx < 1 || ctx > p.na_max_ctx) {
             if (split == 0 && hg == 0) atomicOr(p.err, 2);
             return false;
         }
+        if constexpr (kWindow) window_of(p, ctx, ctx, it.row_begin, it.q_len);
         const int kb = split * p.na_split;
         if (kb >= ctx) return false;
         it.seq = it.q_start = it.bt_row = seq;
@@ -193,9 +222,14 @@ __global__ void __launch_bounds__(kThreads, 3)
         it.num_splits = (ctx + p.na_split - 1) / p.na_split;
         it.part_base = seq * p.na_max_splits;
         it.group = 0;
-        const int b0 = kb / p.block_size, b1 = (it.key_end - 1) / p.block_size;
-        for (int j = 0; j < 4; ++j)
-            it.blk[j] = b0 + j <= b1 ? p.block_table[static_cast<int64_t>(seq) * p.bt_stride + b0 + j] : 0;
+        const int32_t *row = p.block_table + static_cast<int64_t>(seq) * p.bt_stride;
+        if constexpr (kWindow) {
+            for (int j = 0; j < 4; ++j)
+                it.blk[j] = kb + j * kKeys < it.key_end ? row[real_key(p, it.row_begin, kb + j * kKeys) / p.block_size] : 0;
+        } else {
+            const int b0 = kb / p.block_size, b1 = (it.key_end - 1) / p.block_size;
+            for (int j = 0; j < 4; ++j) it.blk[j] = b0 + j <= b1 ? row[b0 + j] : 0;
+        }
         return true;
     };
     auto noplan_next = [&](int i) -> int {  // the first item from i on, in steps of the grid, that there is
@@ -213,6 +247,15 @@ __global__ void __launch_bounds__(kThreads, 3)
         }
     };
     if (kNoPlan) pdl_wait();  // lengths and block ids may come from the kernel before
+    if constexpr (kNoPlan && kWindow) {  // rows without a key: output 0, log-sum-exp -inf
+        for (int s = blockIdx.x; s < p.na_num_seqs; s += static_cast<int>(gridDim.x)) {
+            if (p.na_ctx[s] != 0) continue;
+            const int64_t row = static_cast<int64_t>(s) * p.num_q_heads;
+            for (int e = tid; e < p.num_q_heads * (D / 8); e += kThreads)
+                (static_cast<uint4 *>(p.out) + row * (D / 8))[e] = make_uint4(0u, 0u, 0u, 0u);
+            for (int e = tid; e < p.num_q_heads; e += kThreads) p.lse[row + e] = -INFINITY;
+        }
+    }
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             tc::mbar_init(FULL(s), 1);
@@ -253,6 +296,8 @@ __global__ void __launch_bounds__(kThreads, 3)
         g.part_base = it.part_base;
         g.group = it.group;
         g.head0 = it.kvh;
+        g.skip = kWindow ? it.row_begin : 0;
+        g.lo = kWindow ? it.q_len : 0;
         return g;
     };
 
@@ -271,8 +316,8 @@ __global__ void __launch_bounds__(kThreads, 3)
     auto issue = [&](const DtGeo &g, int j, int blk_lane, int gs) -> bool {
         const int st = gs % kStages;
         if (gs >= kStages && !wait(EMPTY(st), ((gs / kStages) - 1) & 1)) return false;
-        const int key0 = g.kb + j * kKeys;
-        const int rel = key0 / bs - g.kb / bs;  // warp-uniform
+        const int key0 = kWindow ? real_key(p, g.skip, g.kb + j * kKeys) : g.kb + j * kKeys;
+        const int rel = kWindow ? j : key0 / bs - g.kb / bs;  // warp-uniform
         int blk;
         if (rel < 4) {  // from the item itself: the lanes' block-id loads may still be in flight
             blk = rel == 0 ? g.b0 : rel == 1 ? g.b1 : rel == 2 ? g.b2 : g.b3;
@@ -311,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 3)
         DecodeItem it{};
         if (idx < n_items) it = item_at(idx);
         DtGeo cur = geo_of(it);
-        int blk_lane = idx < n_items ? load_blk_lane(p, cur, lane) : 0;
+        int blk_lane = idx < n_items ? load_blk_lane<kWindow>(p, cur, lane) : 0;
         for (int k = 0; ok && idx < n_items; ++k) {
             int a = 0;
             if (!kNoPlan && lane == 0) a = static_cast<int>(gridDim.x) + atomicAdd(sched, 1);  // the next item
@@ -333,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 3)
                 if (!issue(cur, i, blk_lane, gs)) { ok = false; break; }
                 if (idx_n < n_items && i == s1) {
                     nxt = geo_of(nit);
-                    blk_lane_n = load_blk_lane(p, nxt, lane);
+                    blk_lane_n = load_blk_lane<kWindow>(p, nxt, lane);
                 }
             }
             if (!ok) break;
@@ -377,11 +422,28 @@ __global__ void __launch_bounds__(kThreads, 3)
                 const uint32_t sK = s_base + st * Cfg::kStageBytes, sV = sK + Cfg::kTileBytes;
                 const int nv = nkeys - i * kKeys;  // valid keys in this stage (>= 1)
                 const bool tail = nv < kKeys;
+                // (window) hidden slots [d0, d1) between the sinks and the window
+                int d0 = 0, d1 = 0;
+                if constexpr (kWindow) {
+                    const int kr = real_key(p, cur.skip, cur.kb + i * kKeys);
+                    d0 = p.sinks > kr ? p.sinks - kr : 0;
+                    d1 = cur.lo - kr < kKeys ? cur.lo - kr : kKeys;
+                }
+                const bool hidden = kWindow && d0 < d1;
                 if (has_head(cur)) {  // (warp-uniform; else the warp only releases the stage)
                     if (tail) {  // zero this head's V rows past the item's keys
                         for (int e = lane; e < (kKeys - nv) * 8 * (D / 64); e += 32) {
                             const int hh = e / ((kKeys - nv) * 8), rem = e % ((kKeys - nv) * 8);
                             const int sl = nv + rem / 8, ch = rem % 8;
+                            *reinterpret_cast<uint4 *>(smem + st * Cfg::kStageBytes + Cfg::kTileBytes + hh * kHalfBytes +
+                                                       (wh * kKeys + sl) * 128 + ch * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        __syncwarp();
+                    }
+                    if (hidden) {  // and its hidden ones
+                        for (int e = lane; e < (d1 - d0) * 8 * (D / 64); e += 32) {
+                            const int hh = e / ((d1 - d0) * 8), rem = e % ((d1 - d0) * 8);
+                            const int sl = d0 + rem / 8, ch = rem % 8;
                             *reinterpret_cast<uint4 *>(smem + st * Cfg::kStageBytes + Cfg::kTileBytes + hh * kHalfBytes +
                                                        (wh * kKeys + sl) * 128 + ch * 16) = make_uint4(0u, 0u, 0u, 0u);
                         }
@@ -394,7 +456,8 @@ __global__ void __launch_bounds__(kThreads, 3)
                         ldmatrix_x4(a0, a1, a2, a3, sK + dt_off(lr + 8 * (lj & 1), wh, 2 * kk + (lj >> 1)));
                         mma_bf16_16816(s, a0, a1, a2, a3, qb[kk][0], qb[kk][1]);
                     }
-                    const bool v0 = g8 < nv, v1 = g8 + 8 < nv;
+                    const bool v0 = g8 < nv && !(hidden && g8 >= d0 && g8 < d1);
+                    const bool v1 = g8 + 8 < nv && !(hidden && g8 + 8 >= d0 && g8 + 8 < d1);
                     const float x0 = v0 ? s[0] * p.scale_log2 : -INFINITY;
                     const float x1 = v0 ? s[1] * p.scale_log2 : -INFINITY;
                     const float x2 = v1 ? s[2] * p.scale_log2 : -INFINITY;
@@ -435,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 3)
                         mma_bf16_16816(o[mt], a0, a1, a2, a3, pb0, pb1);
                         if constexpr (kFineP) mma_bf16_16816(o[mt], a0, a1, a2, a3, pe0, pe1);
                     }
-                    if (tail) tc::fence_proxy_async_smem();  // order the zeroing before the next TMA write
+                    if (tail || hidden) tc::fence_proxy_async_smem();  // order the zeroing before the next TMA write
                 }
                 __syncwarp();
                 tc::mbar_arrive_warp(EMPTY(st));
@@ -527,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 3)
 // flight, so a token of up to 32 splits costs a few memory round trips.
 constexpr int kMergeWarps = 4;
 
-template <int D, bool kNoPlan>
+template <int D, bool kNoPlan, bool kWindow>
 __global__ void __launch_bounds__(32 * kMergeWarps) split_merge_kernel(const AttnParams p) {
     constexpr int kV = D / 4;                 // float4 per row
     constexpr int kC = (kV + 31) / 32;        // float4 columns per lane
@@ -540,8 +603,13 @@ __global__ void __launch_bounds__(32 * kMergeWarps) split_merge_kernel(const Att
     MergeGroup mg;
     if constexpr (kNoPlan) {
         mg.token = wg / Hq;
-        const int ctx = p.na_ctx[mg.token];
-        if (ctx <= p.na_split || ctx > p.na_max_ctx) return;  // one split: already written; out of range: skipped
+        int ctx = p.na_ctx[mg.token];
+        if (ctx > p.na_max_ctx) return;  // out of range: skipped
+        if constexpr (kWindow) {
+            int skip, lo;
+            if (ctx > 0) window_of(p, ctx, ctx, skip, lo);
+        }
+        if (ctx <= p.na_split) return;  // one split: already written
         mg.num_splits = (ctx + p.na_split - 1) / p.na_split;
         mg.part_base = mg.token * p.na_max_splits;
     } else {
@@ -627,9 +695,9 @@ bool encode_slot_major_map(CUtensorMap *m, const void *base, int d, int hkv, int
 }
 
 // (setting an attribute also loads the kernel's code)
-template <int D, bool kRagged, int kStages, bool kNoPlan, bool kFineP>
+template <int D, bool kRagged, int kStages, bool kNoPlan, bool kFineP, bool kWindow>
 int prepare_dt() {
-    auto kernel = decode_tma_kernel<D, kRagged, kStages, kNoPlan, kFineP>;
+    auto kernel = decode_tma_kernel<D, kRagged, kStages, kNoPlan, kFineP, kWindow>;
     FNPU_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        DtCfg<D, kStages>::kSmemBytes));
     FNPU_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
@@ -637,15 +705,15 @@ int prepare_dt() {
     return FNPU_OK;
 }
 
-template <int D, bool kRagged, int kStages, bool kNoPlan, bool kFineP>
+template <int D, bool kRagged, int kStages, bool kNoPlan, bool kFineP, bool kWindow>
 int launch_dt(const AttnParams &p, cudaStream_t st, int grid, bool after_prev) {
     using Cfg = DtCfg<D, kStages>;
-    auto kernel = decode_tma_kernel<D, kRagged, kStages, kNoPlan, kFineP>;
+    auto kernel = decode_tma_kernel<D, kRagged, kStages, kNoPlan, kFineP, kWindow>;
     DtMaps maps;
     if (!encode_slot_major_map(&maps.k, p.k_cache, D, p.num_kv_heads, p.block_size, p.num_blocks) ||
         !encode_slot_major_map(&maps.v, p.v_cache, D, p.num_kv_heads, p.block_size, p.num_blocks))
         return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled (decode)");
-    const int rc = prepare_dt<D, kRagged, kStages, kNoPlan, kFineP>();
+    const int rc = prepare_dt<D, kRagged, kStages, kNoPlan, kFineP, kWindow>();
     if (rc != FNPU_OK) return rc;
     FNPU_CUDA_TRY(launch_ex(kernel, grid, kThreads, Cfg::kSmemBytes, st, after_prev, nullptr, p, maps));
     return FNPU_OK;
@@ -655,53 +723,53 @@ int launch_dt(const AttnParams &p, cudaStream_t st, int grid, bool after_prev) {
 // for d = 64), and all of them should be in flight whatever the number of CTAs on
 // it (d = 64, 2 kv heads, 64 decodes of 500..4000 keys: 28.2 us a step with half
 // of them, 24.3 with all; 25.9 since P goes in as two operands).
-template <int D, bool kRagged, bool kNoPlan, bool kFineP>
+template <int D, bool kRagged, bool kNoPlan, bool kFineP, bool kWindow>
 int launch_dt(const AttnParams &p, cudaStream_t st, int max_ctas, bool alone) {
     const int grid = p.num_ditems < max_ctas ? p.num_ditems : max_ctas;
     const int sms = max_ctas / 3;
     constexpr int k = 128 / D;  // (stages of 16 KB for d = 64)
-    if (alone && grid <= sms) return launch_dt<D, kRagged, 6 * k, kNoPlan, kFineP>(p, st, grid, alone);
-    if (alone && grid <= 2 * sms) return launch_dt<D, kRagged, 3 * k, kNoPlan, kFineP>(p, st, grid, alone);
-    return launch_dt<D, kRagged, 2 * k, kNoPlan, kFineP>(p, st, grid, alone);
+    if (alone && grid <= sms) return launch_dt<D, kRagged, 6 * k, kNoPlan, kFineP, kWindow>(p, st, grid, alone);
+    if (alone && grid <= 2 * sms) return launch_dt<D, kRagged, 3 * k, kNoPlan, kFineP, kWindow>(p, st, grid, alone);
+    return launch_dt<D, kRagged, 2 * k, kNoPlan, kFineP, kWindow>(p, st, grid, alone);
 }
 
 // every kernel that a call without a plan may come to for head width D
-template <int D>
+template <int D, bool kWindow>
 int prepare_noplan() {
     constexpr int k = 128 / D;
-    for (int rc : {prepare_dt<D, true, 2 * k, true, true>(), prepare_dt<D, true, 3 * k, true, true>(),
-                   prepare_dt<D, true, 6 * k, true, true>(), prepare_dt<D, false, 2 * k, true, true>(),
-                   prepare_dt<D, false, 3 * k, true, true>(), prepare_dt<D, false, 6 * k, true, true>()})
+    for (int rc : {prepare_dt<D, true, 2 * k, true, true, kWindow>(), prepare_dt<D, true, 3 * k, true, true, kWindow>(),
+                   prepare_dt<D, true, 6 * k, true, true, kWindow>(), prepare_dt<D, false, 2 * k, true, true, kWindow>(),
+                   prepare_dt<D, false, 3 * k, true, true, kWindow>(), prepare_dt<D, false, 6 * k, true, true, kWindow>()})
         if (rc != FNPU_OK) return rc;
     cudaFuncAttributes a;
-    FNPU_CUDA_TRY(cudaFuncGetAttributes(&a, split_merge_kernel<D, true>));
+    FNPU_CUDA_TRY(cudaFuncGetAttributes(&a, split_merge_kernel<D, true, kWindow>));
     return FNPU_OK;
 }
 
-template <int D, bool kNoPlan>
+template <int D, bool kNoPlan, bool kWindow>
 int launch_dt_heads(const AttnParams &p, cudaStream_t st, int max_ctas, bool alone) {
-    if (p.num_kv_heads % kHkv != 0) return launch_dt<D, true, kNoPlan, true>(p, st, max_ctas, alone);
-    if (kNoPlan || p.num_kv_heads != 4) return launch_dt<D, false, kNoPlan, true>(p, st, max_ctas, alone);
-    return launch_dt<D, false, kNoPlan, kNoPlan>(p, st, max_ctas, alone);
+    if (p.num_kv_heads % kHkv != 0) return launch_dt<D, true, kNoPlan, true, kWindow>(p, st, max_ctas, alone);
+    if (kNoPlan || p.num_kv_heads != 4) return launch_dt<D, false, kNoPlan, true, kWindow>(p, st, max_ctas, alone);
+    return launch_dt<D, false, kNoPlan, kNoPlan, kWindow>(p, st, max_ctas, alone);
 }
 
-template <bool kNoPlan>
+template <bool kNoPlan, bool kWindow>
 int launch_dt_shape(const AttnParams &p, cudaStream_t st, int max_ctas, bool alone) {
     switch (p.head_dim_qk) {
-        case 64: return launch_dt_heads<64, kNoPlan>(p, st, max_ctas, alone);
-        case 128: return launch_dt_heads<128, kNoPlan>(p, st, max_ctas, alone);
+        case 64: return launch_dt_heads<64, kNoPlan, kWindow>(p, st, max_ctas, alone);
+        case 128: return launch_dt_heads<128, kNoPlan, kWindow>(p, st, max_ctas, alone);
         default: return FNPU_EUNSUPPORTED;
     }
 }
 
-template <bool kNoPlan>
+template <bool kNoPlan, bool kWindow>
 int launch_merge(const AttnParams &p, cudaStream_t st) {
     const int blocks = (p.num_mgroups * p.num_q_heads + kMergeWarps - 1) / kMergeWarps;
     void (*kernel)(AttnParams) = nullptr;
     switch (p.head_dim_v) {
-        case 64: kernel = split_merge_kernel<64, kNoPlan>; break;
-        case 128: kernel = split_merge_kernel<128, kNoPlan>; break;
-        case 512: kernel = kNoPlan ? nullptr : split_merge_kernel<512, false>; break;
+        case 64: kernel = split_merge_kernel<64, kNoPlan, kWindow>; break;
+        case 128: kernel = split_merge_kernel<128, kNoPlan, kWindow>; break;
+        case 512: kernel = kNoPlan ? nullptr : split_merge_kernel<512, false, false>; break;
         default: break;
     }
     if (!kernel) return FNPU_EUNSUPPORTED;
@@ -721,27 +789,31 @@ int decode_tma_heads_per_item() { return kHkv; }
 
 int launch_decode_tma(const AttnParams &p, void *stream, int max_ctas, bool alone) {
     if (p.num_ditems == 0) return FNPU_OK;
-    const int rc = launch_dt_shape<false>(p, static_cast<cudaStream_t>(stream), max_ctas, alone);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int rc = p.window > 0 ? launch_dt_shape<false, true>(p, st, max_ctas, alone)
+                                : launch_dt_shape<false, false>(p, st, max_ctas, alone);
     if (rc != FNPU_OK) return rc;
     return launch_split_merge(p, stream);
 }
 
-int prepare_decode_tma_noplan() {
+int prepare_decode_tma_noplan(bool window) {
     (void)tensor_map_encoder();  // (looked up once; a launch reports it if there is none)
-    const int rc = prepare_noplan<64>();
-    return rc != FNPU_OK ? rc : prepare_noplan<128>();
+    const int rc = window ? prepare_noplan<64, true>() : prepare_noplan<64, false>();
+    if (rc != FNPU_OK) return rc;
+    return window ? prepare_noplan<128, true>() : prepare_noplan<128, false>();
 }
 
 int launch_decode_tma_noplan(const AttnParams &p, void *stream, int max_ctas) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int rc = launch_dt_shape<true>(p, st, max_ctas, true);
+    const bool window = p.window > 0;
+    const int rc = window ? launch_dt_shape<true, true>(p, st, max_ctas, true) : launch_dt_shape<true, false>(p, st, max_ctas, true);
     if (rc != FNPU_OK || p.na_max_splits == 1) return rc;
-    return launch_merge<true>(p, st);
+    return window ? launch_merge<true, true>(p, st) : launch_merge<true, false>(p, st);
 }
 
 int launch_split_merge(const AttnParams &p, void *stream) {
     if (p.num_mgroups == 0) return FNPU_OK;
-    return launch_merge<false>(p, static_cast<cudaStream_t>(stream));
+    return launch_merge<false, false>(p, static_cast<cudaStream_t>(stream));
 }
 
 }  // namespace fnpu

@@ -33,6 +33,7 @@ struct fnpu_plan {
     int32_t num_sms = 0;
     int32_t flags = 0;
     int32_t kv_format = FNPU_KV_BF16;  // 8-bit block formats: fnpu_kv8_attn_plan
+    fnpu::Window window;               // fnpu_window_attn_plan: keys that a query sees
     int32_t kv8_rows = 8;              // ... rows (query token x query head of a kv head) of a decode item
     bool use_tc = false;
     bool use_dt = false;
@@ -841,7 +842,8 @@ struct StepMeta {
 // Host checks of a plan's arguments: nothing is launched or allocated.
 int validate_meta(const fnpu_attn_desc *desc, int32_t num_seqs, const int32_t *query_len,
                   const int32_t *context_len, const uint8_t *phase, const int32_t *block_table,
-                  int32_t block_table_stride, const fnpu_plan_opts &o, StepMeta *m, int32_t kv_format = FNPU_KV_BF16) {
+                  int32_t block_table_stride, const fnpu_plan_opts &o, StepMeta *m, int32_t kv_format = FNPU_KV_BF16,
+                  const Window &window = Window{}) {
     int st;
     if (!shape_ok(desc, &st)) return st;
     if (kv_format < FNPU_KV_BF16 || kv_format > FNPU_KV_E4M3_BLOCK) return FNPU_EINVAL;
@@ -863,7 +865,13 @@ int validate_meta(const fnpu_attn_desc *desc, int32_t num_seqs, const int32_t *q
         if (nb > block_table_stride) return FNPU_EINVAL;
         const int32_t *row = block_table + static_cast<int64_t>(s) * block_table_stride;
         int32_t lo = INT32_MAX, hi = INT32_MIN;  // (a min/max pass over the row vectorises)
-        for (int32_t j = 0; j < nb; ++j) {
+        // (with a window, of the blocks that hold a key which some query sees)
+        const int32_t open = window.first_key(c - q + 1) / bs, shut = window.size > 0 ? std::min(nb, window.sinks / bs + (window.sinks % bs != 0)) : 0;
+        for (int32_t j = 0; j < std::min(shut, open); ++j) {
+            lo = std::min(lo, row[j]);
+            hi = std::max(hi, row[j]);
+        }
+        for (int32_t j = open; j < nb; ++j) {
             lo = std::min(lo, row[j]);
             hi = std::max(hi, row[j]);
         }
@@ -878,6 +886,13 @@ int validate_meta(const fnpu_attn_desc *desc, int32_t num_seqs, const int32_t *q
         const bool kv8_ok = kv8_supported(desc) && !(o.flags & FNPU_PLAN_NO_TCGEN05) &&
                             prefill_tc_supported(desc->head_dim_qk, desc->head_dim_v, desc->block_size,
                                                  desc->num_q_heads / desc->num_kv_heads);
+        if (window.size > 0 && (desc->kv_fp8 || desc->v_in_k_latent || (o.flags & FNPU_PLAN_NO_TCGEN05) ||
+                                desc->head_dim_qk != desc->head_dim_v ||
+                                (r.has_decode && !decode_tma_supported(desc->head_dim_qk, desc->head_dim_v,
+                                                                       desc->num_q_heads / desc->num_kv_heads, desc->block_size)) ||
+                                (r.has_prefill && !prefill_tc_supported(desc->head_dim_qk, desc->head_dim_v, desc->block_size,
+                                                                        desc->num_q_heads / desc->num_kv_heads))))
+            return FNPU_EUNSUPPORTED;
         const int ks = kv_format != FNPU_KV_BF16 ? (kv8_ok ? FNPU_OK : FNPU_EUNSUPPORTED)
                                                  : kernel_support(desc, r.has_decode, r.has_prefill);
         if (ks != FNPU_OK) return ks;
@@ -959,9 +974,25 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
         return kv8 ? static_cast<int64_t>(query_len[s]) * G <= direct_rows : phase[s] == 1 && query_len[s] == 1;
     };
     // a decode item with its sequence's fields and its first four block ids
+    // (with a window: the keys of the virtual sequence, and the blocks of the first four stages)
+    const Window &win = pl->window;
+    const bool windowed = win.size > 0;
+    const int32_t sink_keys = win.sink_keys(kDecodeStageKeys);
+    auto skipped = [&](int32_t s) {  // whole stages between the sinks and a decode's window
+        return std::max(0, win.first_key(context_len[s]) / kDecodeStageKeys - sink_keys / kDecodeStageKeys);
+    };
+    auto decode_keys = [&](int32_t s) { return windowed ? context_len[s] - kDecodeStageKeys * skipped(s) : context_len[s]; };
     auto decode_item = [&](int32_t s, int32_t kvh, int32_t kb, int32_t ke, int32_t sp, int32_t ns, int32_t base,
                            int32_t grp) {
         DecodeItem it{s, kvh, kb, ke, sp, ns, base, grp, seqs[s].q_start, seqs[s].bt_row, 0, query_len[s], {0, 0, 0, 0}};
+        if (windowed) {
+            it.row_begin = skipped(s);
+            it.q_len = win.first_key(context_len[s]);
+            for (int32_t i = 0, k = kb; i < 4 && k < ke; ++i, k += kDecodeStageKeys)
+                it.blk[i] = block_table[static_cast<int64_t>(s) * block_table_stride +
+                                        (k < sink_keys ? k : k + kDecodeStageKeys * it.row_begin) / bs];
+            return it;
+        }
         for (int32_t i = 0; i < 4 && kb / bs + i <= (ke - 1) / bs; ++i)
             it.blk[i] = block_table[static_cast<int64_t>(s) * block_table_stride + kb / bs + i];
         return it;
@@ -970,11 +1001,11 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
     int64_t kv8_rows = 1;
     for (int32_t s = 0; s < num_seqs; ++s)
         if (decode_queue(s)) {
-            dec_keys += context_len[s];
+            dec_keys += decode_keys(s);
             ++num_dec;
             kv8_rows = std::max(kv8_rows, static_cast<int64_t>(query_len[s]) * G);
         }
-    if (pl->use_dt && !kv8 && desc->num_kv_heads <= 2 && desc->head_dim_qk == 64 && o.decode_share_pct == 0 &&
+    if (pl->use_dt && !kv8 && !windowed && desc->num_kv_heads <= 2 && desc->head_dim_qk == 64 && o.decode_share_pct == 0 &&
         !(o.flags & FNPU_PLAN_GREEN_CONTEXTS)) {
         // One or two 64-wide kv heads leave three or two of the TMA kernel's four
         // compute warps idle. It is the faster one while a step is light (20 of
@@ -1018,8 +1049,8 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
             int32_t longest = 0;
             for (int32_t s = 0; s < num_seqs; ++s)
                 if (decode_queue(s)) {
-                    items += static_cast<int64_t>((context_len[s] + 63) / 64) * hgroups;
-                    longest = std::max(longest, context_len[s]);
+                    items += static_cast<int64_t>((decode_keys(s) + 63) / 64) * hgroups;
+                    longest = std::max(longest, decode_keys(s));
                 }
             if (items <= 2LL * sms && longest <= 32 * 64) split = 64;
         } else if (pl->use_dt && split > 320 && desc->num_kv_heads != 4 && num_dec < 3LL * sms &&
@@ -1033,7 +1064,7 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
             split = std::min(split, 512);
             int64_t items = 0;
             for (int32_t s = 0; s < num_seqs; ++s)
-                if (decode_queue(s)) items += static_cast<int64_t>((context_len[s] + split - 1) / split) * hgroups;
+                if (decode_queue(s)) items += static_cast<int64_t>((decode_keys(s) + split - 1) / split) * hgroups;
             if (items > 3LL * sms && items < 6LL * sms) split = 320;
         }
     }
@@ -1152,15 +1183,16 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
             // items over groups of kv heads, cut at whole 16-key stages; a
             // split sequence is merged by the merge kernel (at most 256
             // splits: its scratch grows with them)
-            const int32_t sk = std::max((split + 15) / 16 * 16, (c + 256 * 64 - 1) / (256 * 64) * 64);
-            const int32_t ns = (c + sk - 1) / sk;
+            const int32_t keys = decode_keys(s);
+            const int32_t sk = std::max((split + 15) / 16 * 16, (keys + 256 * 64 - 1) / (256 * 64) * 64);
+            const int32_t ns = (keys + sk - 1) / sk;
             const int32_t base = ns > 1 ? parts : 0;
             if (ns > 1) {
                 mgroups.push_back(MergeGroup{qs, ns, parts, 0});
                 parts += ns;
             }
             for (int32_t sp = 0; sp < ns; ++sp) {
-                const int32_t kb = sp * sk, ke = std::min(c, kb + sk);
+                const int32_t kb = sp * sk, ke = std::min(keys, kb + sk);
                 for (int32_t hg = 0; hg < hgroups; ++hg)
                     ditems.push_back(decode_item(s, hg * hpi, kb, ke, sp, ns, base, 0));
             }
@@ -1182,7 +1214,15 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
             const int32_t P2 = prefill_tc_rows_per_item(G), KT = prefill_tc_keys_per_tile();
             for (int32_t r0 = 0; r0 < q; r0 += P2) {
                 const int32_t rows = std::min(P2, q - r0);
-                const int32_t ntiles = (prefix + r0 + rows + KT - 1) / KT;
+                int32_t ntiles = (prefix + r0 + rows + KT - 1) / KT;
+                if (windowed) {
+                    // virtual tiles: those between the sinks and the first row's window are
+                    // left out; a row may see no key of a split piece, so pieces start anywhere
+                    ntiles -= std::max(0, win.first_key(prefix + r0 + 1) / KT - win.sink_keys(KT) / KT);
+                    for (int32_t kvh = 0; kvh < desc->num_kv_heads; ++kvh)
+                        tc_units.push_back(TcUnit{s, kvh, r0, rows, ntiles, ntiles - 1, 0, ntiles});
+                    continue;
+                }
                 const bool dual = q <= P2 / 2 && ntiles >= kDualTiles && desc->head_dim_qk == desc->head_dim_v;
                 const int32_t per = dual ? 2 : 1;
                 for (int32_t kvh = 0; kvh < desc->num_kv_heads; ++kvh)
@@ -1560,12 +1600,12 @@ int plan_build(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, cons
 // A new plan for a step.
 int plan_new(const fnpu_attn_desc *desc, int32_t kv_format, int32_t num_seqs, const int32_t *query_len, const int32_t *context_len,
              const uint8_t *phase, const int32_t *block_table, int32_t block_table_stride, const fnpu_plan_opts *opts, void *stream,
-             fnpu_plan **out) {
+             fnpu_plan **out, const Window &window = Window{}) {
     if (!out) return FNPU_EINVAL;
     fnpu_plan_opts o = {};
     if (opts) o = *opts;
     StepMeta m;
-    int rc = validate_meta(desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, &m, kv_format);
+    int rc = validate_meta(desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, &m, kv_format, window);
     if (rc != FNPU_OK) return rc;
     int sms = 0;
     rc = plan_sms(o, &sms);
@@ -1573,6 +1613,7 @@ int plan_new(const fnpu_attn_desc *desc, int32_t kv_format, int32_t num_seqs, co
     fnpu_plan *pl = new (std::nothrow) fnpu_plan();
     if (!pl) return FNPU_ENOMEM;
     pl->kv_format = kv_format;
+    pl->window = window;
     rc = plan_build(pl, desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o, m, sms, stream);
     if (rc != FNPU_OK) {
         release_plan(pl);
@@ -1601,6 +1642,14 @@ int fnpu_kv8_attn_plan(const fnpu_attn_desc *desc, int32_t kv_format, int32_t nu
     return plan_new(desc, kv_format, num_seqs, query_len, context_len, phase, block_table, block_table_stride, opts, stream, out);
 }
 
+int fnpu_window_attn_plan(const fnpu_attn_desc *desc, int32_t window, int32_t sinks, int32_t num_seqs, const int32_t *query_len,
+                          const int32_t *context_len, const uint8_t *phase, const int32_t *block_table, int32_t block_table_stride,
+                          const fnpu_plan_opts *opts, void *stream, fnpu_plan **out) {
+    if (window < 1 || sinks < 0) return FNPU_EINVAL;
+    return plan_new(desc, FNPU_KV_BF16, num_seqs, query_len, context_len, phase, block_table, block_table_stride, opts, stream, out,
+                    Window{window, std::min(sinks, kMostSinks)});
+}
+
 int fnpu_mixed_attn_replan(fnpu_plan *pl, int32_t num_seqs, const int32_t *query_len, const int32_t *context_len,
                            const uint8_t *phase, const int32_t *block_table, int32_t block_table_stride,
                            const fnpu_plan_opts *opts, void *stream) {
@@ -1609,7 +1658,7 @@ int fnpu_mixed_attn_replan(fnpu_plan *pl, int32_t num_seqs, const int32_t *query
     if (opts) o = *opts;
     StepMeta m;
     int rc = validate_meta(&pl->desc, num_seqs, query_len, context_len, phase, block_table, block_table_stride, o,
-                           &m, pl->kv_format);
+                           &m, pl->kv_format, pl->window);
     if (rc != FNPU_OK) return rc;  // the plan is unchanged
     int sms = 0;
     rc = plan_sms(o, &sms);
@@ -1665,6 +1714,9 @@ AttnParams run_params(const fnpu_plan *pl, const void *q, const void *k_cache, c
     p.pcounters = pl->d_pcounters;
     p.err = pl->d_err;
     p.sched = pl->d_err + 2;
+    p.window = pl->window.size;
+    p.sinks = pl->window.sinks;
+    p.sink_keys = pl->window.sink_keys(kDecodeStageKeys);
     return p;
 }
 

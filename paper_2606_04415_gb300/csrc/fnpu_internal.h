@@ -20,6 +20,9 @@ namespace fnpu {
 // 8-bit block kernel: the item is rows [row_begin, row_begin + the rows that the
 // kernel takes) of the q_len x G rows (token, query head of the kv head) of the
 // sequence, at most kKv8MaxItemKeys keys; blk[0] is the sequence's context length.
+// With a window (TMA kernel): the keys are virtual, row_begin is the number of
+// 16-key stages left out behind the sinks, q_len the first key of the window and
+// blk[i] the block of the item's stage i.
 struct DecodeItem {
     int32_t seq, kvh, key_begin, key_end;
     int32_t split, num_splits, part_base, group;
@@ -130,6 +133,9 @@ struct AttnParams {
     // a wait that gave up)
     const int32_t *na_ctx;
     int32_t na_num_seqs, na_max_ctx, na_split, na_max_splits;
+    // sliding window (0: none): a query at position p sees keys p - window + 1 .. p
+    // and those below `sinks`; sink_keys: sinks up to a whole stage or key tile
+    int32_t window, sinks, sink_keys;
 };
 
 // Rotation of column pairs: pair i of a row turns by positions[axis[i]][t] *
@@ -157,6 +163,18 @@ struct RopeAppendArgs {
     int32_t q_heads, kv_heads, d, d_v, block_size;
     int *err;                 // the library-wide error flag
 };
+
+// A sliding window (size 0: none): a query at position p sees keys p - size + 1 .. p
+// and the first `sinks` of its sequence.
+struct Window {
+    int32_t size = 0, sinks = 0;
+    // the first key of the window of a query at the end of `keys` keys
+    int32_t first_key(int32_t keys) const { return size > 0 && keys > size ? keys - size : 0; }
+    // the sinks up to a whole tile of `tile` keys
+    int32_t sink_keys(int32_t tile) const { return (sinks + tile - 1) / tile * tile; }
+};
+constexpr int32_t kMostSinks = INT32_MAX - 1024;  // (more see as much: room to round up)
+constexpr int kDecodeStageKeys = 16;              // keys of a stage of the TMA decode kernel
 
 // cuTensorMapEncodeTiled, looked up once through the runtime's driver entry
 // point (the library does not link the driver library); null if unavailable.
@@ -246,7 +264,7 @@ int launch_decode_tma_noplan(const AttnParams &p, void *stream, int max_ctas);
 // Loads every kernel that launch_decode_tma_noplan may launch on the current
 // device: which one follows from the batch, and a first use later could load
 // code under a stream capture or where no device memory may be taken.
-int prepare_decode_tma_noplan();
+int prepare_decode_tma_noplan(bool window);
 int launch_prefill_mma(const AttnParams &p, void *stream);
 int launch_mla(const AttnParams &p, void *stream);
 // tcgen05 latent attention: items are (token, d_v half, key range) of 128 heads

@@ -44,6 +44,15 @@
 //                   so that V(j+1) loads while both S of the next tile run.
 // TMEM (512 columns): S0 at 0, S1 at 128 (fp32, P over their first 64
 // columns); O0 at 256, O1 at 384.
+//
+// With a window and sinks (kWindow) an item's key tiles are virtual: those wholly
+// between the sinks and its first row's window are cut out, tile v of the item
+// being tile v below the sinks' end and v + skip from there on. Keys that no row
+// of the item sees are not loaded where their whole block is hidden (its page may
+// be gone: a box past the pool lands as zeros); the others' V rows are zeroed like
+// those past the context, in up to three tiles an item, so each V stage has a
+// barrier of its own for that. A row may see no key of a split piece, whose
+// partial result is then 0 with a log-sum-exp of -inf.
 // Every mbarrier wait is bounded; a timeout raises the plan's error flag and
 // the CTA drains its tensor-core work and copies, frees its tensor memory and
 // exits. Launched as a programmatic dependent of the kernel before it (the step's
@@ -95,7 +104,8 @@ struct TcCfg {
     // qfull qempty vzero itemfull[2] itemempty[2] drain mlx oread
     static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 8 + 3 + 4 + 3;
     static constexpr int kMlOff = kBarOff + 8 * kNumBars + 32;  // (m, l) of both paths' rows (dual items)
-    static constexpr int kSmemUsed = kMlOff + 2 * 128 * 8;
+    static constexpr int kVzOff = kMlOff + 2 * 128 * 8;         // window: a barrier for each V stage's zeroed rows
+    static constexpr int kSmemUsed = kVzOff + 8 * kVStages;
     // at least 116 KB so that no two CTAs share an SM (each holds all 512 TMEM columns)
     static constexpr int kSmemBytes = kSmemUsed > 116 * 1024 ? kSmemUsed : 116 * 1024;
     static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
@@ -106,18 +116,30 @@ struct TcMaps {
 };
 
 // dual: one Q tile, its even key tiles on tile 0's path and its odd ones on tile 1's
-template <bool kDual>
+template <bool kDual, bool kWindow = false>
 struct ItemGeomT {
+    int sink_tiles, skip, lo;  // window: tiles of the sinks, tiles left out behind them, first key of the first row's window
     int kvh, p0, rows, prefix, ctx, kt0, ntiles, q_start, bt_row;
     int ns, split, pbase, cnt;  // key splits of the tile pair, this split, first partial, merge counter
     bool tail_fix;
     bool dual;
+    // the 128-key tile of the sequence that the item's i-th tile is
+    __device__ __forceinline__ int tile(int i) const {
+        const int v = kt0 + i;
+        return kWindow && v >= sink_tiles ? v + skip : v;
+    }
+    // hidden keys [a, b) of the 128 from k0 on, between the sinks and the first row's window
+    __device__ __forceinline__ bool hidden(const AttnParams &p, int k0, int &a, int &b) const {
+        a = p.sinks > k0 ? p.sinks - k0 : 0;
+        b = lo - k0 < kKeys ? lo - k0 : kKeys;
+        return kWindow && a < b;
+    }
 };
 
-template <bool kDual>
-__device__ __forceinline__ ItemGeomT<kDual> item_geom(const AttnParams &p, int idx) {
+template <bool kDual, bool kWindow>
+__device__ __forceinline__ ItemGeomT<kDual, kWindow> item_geom(const AttnParams &p, int idx) {
     const PrefillItem it = p.pitems[idx];  // carries its sequence's fields: one load
-    ItemGeomT<kDual> g;
+    ItemGeomT<kDual, kWindow> g;
     g.kvh = it.head;
     g.p0 = it.row_begin;
     g.rows = it.rows;
@@ -131,7 +153,15 @@ __device__ __forceinline__ ItemGeomT<kDual> item_geom(const AttnParams &p, int i
     g.split = it.split;
     g.pbase = it.part_base;
     g.cnt = it.group;
-    g.tail_fix = it.kt_end * kKeys > g.ctx;
+    if constexpr (kWindow) {
+        const int first = it.prefix + it.row_begin;
+        g.lo = first >= p.window ? first - p.window + 1 : 0;
+        g.sink_tiles = (p.sinks + kKeys - 1) / kKeys;
+        g.skip = g.lo / kKeys > g.sink_tiles ? g.lo / kKeys - g.sink_tiles : 0;
+    } else {
+        g.lo = g.sink_tiles = g.skip = 0;
+    }
+    g.tail_fix = (g.tile(g.ntiles - 1) + 1) * kKeys > g.ctx;
     g.dual = kDual && it.dual != 0;
     return g;
 }
@@ -187,7 +217,7 @@ __device__ __noinline__ bool fused_append(const AttnParams &p, int tid, volatile
 // prefill: its codes are dequantised to f16 first)
 // kDual: the plan has items of a single Q tile on both paths (a kernel of its
 // own: the code for them costs the others 2 to 4% through the instruction cache)
-template <int DQ, int DV, bool F16, bool kDual>
+template <int DQ, int DV, bool F16, bool kDual, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
     prefill_tc_kernel(const AttnParams p, const __grid_constant__ TcMaps maps) {
     using Cfg = TcCfg<DQ, DV>;
@@ -207,6 +237,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t QFULL = b0 + 64, QEMPTY = b0 + 72, VZERO = b0 + 80;
     auto ITEMFULL = [&](int k) { return b0 + 88 + 8 * k; };
     auto ITEMEMPTY = [&](int k) { return b0 + 104 + 8 * k; };
+    auto VZ = [&](int s) { return s_base + Cfg::kVzOff + 8 * s; };  // (window)
     const uint32_t DRAIN = b0 + 120, MLX = b0 + 128, OREAD = b0 + 136;
     float2 *ml = reinterpret_cast<float2 *>(smem + Cfg::kMlOff);
     uint8_t *misc = smem + Cfg::kBarOff + 8 * Cfg::kNumBars;
@@ -230,6 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int s = 0; s < kVStages; ++s) {
             tc::mbar_init(VFULL(s), 1);
             tc::mbar_init(VEMPTY(s), 1);
+            if (kWindow) tc::mbar_init(VZ(s), 1);
         }
         for (int w = 0; w < 2; ++w) {
             tc::mbar_init(SFULL(w), 1);
@@ -305,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 idx = __shfl_sync(0xffffffffu, item_slot[slot], 0);
                 if (idx < 0) break;
             }
-            const ItemGeomT<kDual> it = item_geom<kDual>(p, idx);
+            const ItemGeomT<kDual, kWindow> it = item_geom<kDual, kWindow>(p, idx);
             const int ukvh = __shfl_sync(0xffffffffu, it.kvh, 0);
             // both Q tiles, once the previous item's last S is done (loading them
             // after the item's first K tiles, with an L2 prefetch ahead, was
@@ -327,17 +359,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int nblk_seq = (it.ctx + bs - 1) / bs;
             // block ids of the next tile, one per lane, loaded a tile ahead so
             // that the TMA issue never waits on a block-table read
-            const int b00 = it.kt0 * per_tile;
-            int blk_next = (lane < per_tile && b00 + lane < nblk_seq) ? __ldg(bt + b00 + lane) : 0;
+            // (window: a hidden block is read from past the pool, as zeros)
+            auto block_at = [&](int j) -> int {
+                if (kWindow && j * bs >= p.sinks && (j + 1) * bs <= it.lo) return p.num_blocks;
+                return __ldg(bt + j);
+            };
+            const int b00 = it.tile(0) * per_tile;
+            int blk_next = (lane < per_tile && b00 + lane < nblk_seq) ? block_at(b00 + lane) : 0;
             bool ok = true;
             for (int i = 0; i < it.ntiles; ++i, ++g) {
                 if (is_k && i == 0 && !load_q()) { ok = false; break; }
                 const int st = g % nst;
                 const int blk_cur = blk_next;
-                const int jn = b00 + (i + 1) * per_tile + lane;
-                blk_next = (i + 1 < it.ntiles && lane < per_tile && jn < nblk_seq) ? __ldg(bt + jn) : 0;
+                const int jn = it.tile(i + 1) * per_tile + lane;
+                blk_next = (i + 1 < it.ntiles && lane < per_tile && jn < nblk_seq) ? block_at(jn) : 0;
                 if (g >= nst && !wait(is_k ? KEMPTY(st) : VEMPTY(st), ((g / nst) - 1) & 1)) { ok = false; break; }
-                int nvalid = nblk_seq - b00 - i * per_tile;
+                int nvalid = nblk_seq - it.tile(i) * per_tile;
                 nvalid = nvalid < 0 ? 0 : (nvalid > per_tile ? per_tile : nvalid);
                 nvalid = __shfl_sync(0xffffffffu, nvalid, 0);
                 const uint32_t bar = is_k ? KFULL(st) : VFULL(st);
@@ -349,7 +386,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
                 if (lb < nvalid) tc::tma_load_4d(dst + lh * Cfg::kHalf + lb * bs * 128, map, bar, lh * 64, ukvh, 0, blk);
                 __syncwarp();
-                if (!is_k && i == it.ntiles - 1 && it.tail_fix) {
+                if constexpr (kWindow) {
+                    const int k0 = it.tile(i) * kKeys;
+                    int a, b;
+                    const bool mid = it.hidden(p, k0, a, b), tail = i == it.ntiles - 1 && it.tail_fix;
+                    if (!is_k && (mid || tail)) {
+                        // zero the V rows that no row of the item sees
+                        if (!wait(VFULL(st), (g / nst) & 1)) { ok = false; break; }
+                        if (!mid) a = b = 0;
+                        const int t0 = tail ? it.ctx - k0 : kKeys;
+                        for (int e = lane; e < kKeys * 8 * (DV / 64); e += 32) {
+                            const int h = e / (kKeys * 8), row = e / 8 % kKeys, ch = e % 8;
+                            if ((row >= a && row < b) || row >= t0)
+                                *reinterpret_cast<uint4 *>(smem + Cfg::kVOff + st * Cfg::kVTileBytes + h * Cfg::kHalf +
+                                                           row * 128 + ch * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        tc::fence_proxy_async_smem();
+                        __syncwarp();
+                        tc::mbar_arrive_warp(VZ(st));
+                    }
+                } else if (!is_k && i == it.ntiles - 1 && it.tail_fix) {
                     // zero V rows of keys >= ctx (stale slots, unloaded blocks)
                     if (!wait(VFULL(st), (g / nst) & 1)) { ok = false; break; }
                     const int r0 = it.ctx - (it.kt0 + i) * kKeys;
@@ -384,6 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t utmem = __shfl_sync(0xffffffffu, tmem, 0);
         const uint32_t us_base = __shfl_sync(0xffffffffu, s_base, 0);
         int gk = 0, gv = 0, t0 = 0, t1 = 0, nfix = 0;  // ring positions, tiles done by each Q tile
+        uint32_t vz = 0;  // (window) parity of each V stage's next zeroing
         bool ok = true, issued = false;
         auto issue_s = [&](int w, int st) {
             if (tc::elect_one()) {
@@ -415,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!wait(ITEMFULL(slot), (k >> 1) & 1)) { ok = false; break; }
             const int idx = __shfl_sync(0xffffffffu, item_slot[slot], 0);
             if (idx < 0) break;
-            const ItemGeomT<kDual> it = item_geom<kDual>(p, idx);
+            const ItemGeomT<kDual, kWindow> it = item_geom<kDual, kWindow>(p, idx);
             const int n = __shfl_sync(0xffffffffu, it.ntiles, 0);
             const bool tail = __shfl_sync(0xffffffffu, it.tail_fix ? 1 : 0, 0) != 0;
             // PV_0(u - 1), S_0(u), PV_1(u - 1), S_1(u) for u = 0 .. n: each product
@@ -430,7 +487,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // (one V stage: both P V first, so that the next V tile loads
                 // while both S of the next key tile run)
                 constexpr bool kPvFirst = Cfg::kVStages == 1;
-                if (u > 0) {
+                if (kWindow && u > 0) {
+                    int a, b;
+                    const bool fix = __shfl_sync(0xffffffffu, it.hidden(p, it.tile(u - 1) * kKeys, a, b) || (u == n && tail) ? 1 : 0, 0) != 0;
+                    if (!wait(fix ? VZ(vst) : VFULL(vst), fix ? (vz >> vst) & 1u : static_cast<uint32_t>(gv / kVStages) & 1u) ||
+                        !wait(PFULL(0), T & 1) || (u == 1 && k >= 1 && !wait(OFREE(0), (k - 1) & 1))) {
+                        ok = false;
+                        break;
+                    }
+                    if (fix) vz ^= 1u << vst;
+                    tc::fence_after_sync();
+                    issue_pv(0, vst, acc);
+                    if (u == n) tc::commit_warp(ODONE(0));
+                } else if (u > 0) {
                     if (u == n && tail) {
                         if (!wait(VZERO, nfix & 1)) { ok = false; break; }
                     } else if (!wait(VFULL(vst), (gv / kVStages) & 1)) {
@@ -528,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!wait(ITEMFULL(slot), (k >> 1) & 1)) break;
             const int idx = item_slot[slot];
             if (idx < 0) break;
-            const ItemGeomT<kDual> it = item_geom<kDual>(p, idx);
+            const ItemGeomT<kDual, kWindow> it = item_geom<kDual, kWindow>(p, idx);
             const int pw = it.p0 + (kDual && it.dual ? 0 : w * P);
             const int nw = kDual && it.dual ? (it.ntiles + 1 - w) / 2 : it.ntiles;  // key tiles of this path
             const bool row_ok = (r < P * G) && (pw + pl < it.p0 + it.rows);
@@ -553,9 +622,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::tmem_wait_ld();
                 // tiles that reach past the first row's position need the causal
                 // mask; all others are fully visible to every row of the tile
-                const int k0 = (it.kt0 + (kDual && it.dual ? 2 * i + w : i)) * kKeys;
+                const int k0 = it.tile(kDual && it.dual ? 2 * i + w : i) * kKeys;
                 const bool masked_tile = k0 + kKeys - 1 > min_pos;
-                if (masked_tile) {
+                if (kWindow && k0 <= min_pos + P - 1 - p.window && k0 + kKeys > p.sinks) {
+                    // and tiles that begin before the last row's window, past the sinks
+                    const int hi = pos - k0, lo = hi - p.window, sk = p.sinks - k0;
+#pragma unroll
+                    for (int j = 0; j < kKeys; ++j)
+                        if (j > hi || (j <= lo && j >= sk)) s[j] = __float_as_uint(-INFINITY);
+                } else if (masked_tile) {
 #pragma unroll
                     for (int j = 0; j < kKeys; ++j)
                         if (k0 + j > pos) s[j] = __float_as_uint(-INFINITY);
@@ -624,7 +699,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::fence_after_sync();
             uint4 *orow = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) +
                                                     (tok * p.num_q_heads + head) * DV);
-            const float inv = 1.f / l;  // (a dual item's row may see no key on one path; it has its own sums)
+            const bool none = kWindow && l == 0.f;  // no key of a split piece is visible to the row
+            const float inv = none ? 0.f : 1.f / l;  // (a dual item's row may see no key on one path; it has its own sums)
             if (kDual && it.dual) {
                 // One Q tile on both paths: each path has the row's maximum and
                 // sum over its key tiles, and both O are in tensor memory, same
@@ -762,7 +838,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tc::tmem_wait_ld();
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        po[(c * 8 + j) * 128] = make_float4(__uint_as_float(o[4 * j]) * inv, __uint_as_float(o[4 * j + 1]) * inv,
+                        po[(c * 8 + j) * 128] = none ? make_float4(0.f, 0.f, 0.f, 0.f) :
+                                                make_float4(__uint_as_float(o[4 * j]) * inv, __uint_as_float(o[4 * j + 1]) * inv,
                                                             __uint_as_float(o[4 * j + 2]) * inv, __uint_as_float(o[4 * j + 3]) * inv);
                 }
                 const float my_lse = m_run + log2f(l);
@@ -800,7 +877,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 ws = fast_exp2(my_lse - M);
 #pragma unroll
                                 for (int j = 0; j < 8; ++j)
-                                    v[j] = make_float4(__uint_as_float(o[4 * j]) * inv, __uint_as_float(o[4 * j + 1]) * inv,
+                                    v[j] = none ? make_float4(0.f, 0.f, 0.f, 0.f) :
+                                           make_float4(__uint_as_float(o[4 * j]) * inv, __uint_as_float(o[4 * j + 1]) * inv,
                                                        __uint_as_float(o[4 * j + 2]) * inv, __uint_as_float(o[4 * j + 3]) * inv);
                             } else {
                                 ws = fast_exp2(lse_of(sp) - M);
@@ -893,7 +971,7 @@ bool encode_q_map(CUtensorMap *m, const void *base, int d, int hq, int64_t T, in
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DQ, int DV, bool F16, bool kDual>
+template <int DQ, int DV, bool F16, bool kDual, bool kWindow = false>
 int launch_tc(const AttnParams &p, cudaStream_t st, int max_ctas, cudaEvent_t started, bool pdl) {
     using Cfg = TcCfg<DQ, DV>;
     TcMaps maps;
@@ -901,7 +979,7 @@ int launch_tc(const AttnParams &p, cudaStream_t st, int max_ctas, cudaEvent_t st
         !encode_cache_map(&maps.v, p.v_cache, DV, p.num_kv_heads, p.block_size, p.num_blocks, F16) ||
         !encode_q_map(&maps.q, p.q, DQ, p.num_q_heads, p.num_tokens, p.group, kRows / p.group, F16))
         return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
-    auto kernel = prefill_tc_kernel<DQ, DV, F16, kDual>;
+    auto kernel = prefill_tc_kernel<DQ, DV, F16, kDual, kWindow>;
     FNPU_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes));
     FNPU_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
                                        cudaSharedmemCarveoutMaxShared));
@@ -935,6 +1013,11 @@ int launch_prefill_tc(const AttnParams &p, void *stream, int max_ctas, void *sta
         if (p.head_dim_qk != 128 || p.head_dim_v != 128) return FNPU_EUNSUPPORTED;
         return dual ? launch_tc<128, 128, true, true>(p, st, max_ctas, ev, pdl)
                     : launch_tc<128, 128, true, false>(p, st, max_ctas, ev, pdl);
+    }
+    if (p.window > 0) {  // (its plans have no dual items)
+        if (p.head_dim_qk == 64 && p.head_dim_v == 64) return launch_tc<64, 64, false, false, true>(p, st, max_ctas, ev, pdl);
+        if (p.head_dim_qk == 128 && p.head_dim_v == 128) return launch_tc<128, 128, false, false, true>(p, st, max_ctas, ev, pdl);
+        return FNPU_EUNSUPPORTED;
     }
     if (p.head_dim_qk == 64 && p.head_dim_v == 64)
         return dual ? launch_tc<64, 64, false, true>(p, st, max_ctas, ev, pdl)
