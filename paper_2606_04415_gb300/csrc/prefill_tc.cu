@@ -161,7 +161,9 @@ __device__ __forceinline__ ItemGeomT<kDual, kWindow> item_geom(const AttnParams 
     } else {
         g.lo = g.sink_tiles = g.skip = 0;
     }
-    g.tail_fix = (g.tile(g.ntiles - 1) + 1) * kKeys > g.ctx;
+    // (dual items have no window; the plain forms here and at the block ids keep
+    // their kernel's registers as they were: 76 bytes of spills, else 84)
+    g.tail_fix = (kDual ? it.kt_end : g.tile(g.ntiles - 1) + 1) * kKeys > g.ctx;
     g.dual = kDual && it.dual != 0;
     return g;
 }
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (is_k && i == 0 && !load_q()) { ok = false; break; }
                 const int st = g % nst;
                 const int blk_cur = blk_next;
-                const int jn = it.tile(i + 1) * per_tile + lane;
+                const int jn = (kDual ? b00 + (i + 1) * per_tile : it.tile(i + 1) * per_tile) + lane;
                 blk_next = (i + 1 < it.ntiles && lane < per_tile && jn < nblk_seq) ? block_at(jn) : 0;
                 if (g >= nst && !wait(is_k ? KEMPTY(st) : VEMPTY(st), ((g / nst) - 1) & 1)) { ok = false; break; }
                 int nvalid = nblk_seq - it.tile(i) * per_tile;
