@@ -590,6 +590,151 @@ int fnpu_window_decode(const fnpu_attn_desc *desc, int32_t window, int32_t sinks
                        const void *v_cache, void *out, float *lse, void *workspace, int64_t workspace_bytes,
                        void *stream);
 
+/*
+ * Selection of a beam search. Each of num_groups requests has num_beams beams; row
+ * g * num_beams + b of `logits` are the next token's logits of beam b of group g. A
+ * continuation (b, v) has the total
+ *   scores[b] + (x_v - m) - ln sum_u exp(x_u - m),   m = max_u x_u,
+ * and the num_select best of a group come out in order, ties to the lowest b, then
+ * the lowest v (within a row the order is that of the logits). A beam whose
+ * `finished` flag is set has one continuation, end_token at its own score (none
+ * with end_token -1); a logit of -inf or NaN is no candidate, +inf counts as the
+ * largest finite value, and a beam whose score is -inf or NaN has no continuation
+ * (the idle beams of a first step). Where a group has fewer than num_select, the
+ * rest come out with score -inf, parent -1 and token -1.
+ * Exponentials are summed in fp32 a slice of a row and combined in 64 bits, and
+ * totals are compared in 64 bits.
+ *   logits        device, row_stride values between rows (>= vocab; the start of a
+ *                 row needs the alignment of its type only)
+ *   scores        device fp32 [num_groups, num_beams]
+ *   finished      device uint8 [num_groups, num_beams], or NULL
+ *   out_scores    device fp32 [num_groups, num_select]
+ *   out_parents   device int32, the same shape: the row of logits that is continued
+ *                 (what fnpu_pages_fork takes); out_tokens likewise
+ *   workspace     device, 16-byte aligned, of the bytes that
+ *                 fnpu_beam_select_workspace gives; calls that overlap on the GPU need
+ *                 one each. Nothing in it is kept from call to call.
+ * Outputs must not overlap the inputs. num_beams <= 128, num_select <= 64, vocab <= 2^24
+ * (FNPU_EUNSUPPORTED beyond).
+ * Errors: FNPU_EINVAL for NULL or misaligned pointers, a bad shape, an end_token
+ * outside [-1, vocab), a workspace that is too small; FNPU_ECUDA.
+ */
+#define FNPU_LOGITS_BF16 0
+#define FNPU_LOGITS_FP32 1
+typedef struct {
+    int32_t num_groups;
+    int32_t num_beams;   /* rows of logits a group */
+    int32_t vocab;
+    int32_t num_select;  /* continuations a group */
+    int32_t dtype;       /* FNPU_LOGITS_* */
+    int32_t end_token;   /* of finished beams; -1: none */
+} fnpu_beam_desc;
+int fnpu_beam_select_workspace(const fnpu_beam_desc *desc, int64_t *bytes);
+int fnpu_beam_select(const fnpu_beam_desc *desc, const void *logits, int64_t row_stride, const float *scores,
+                     const uint8_t *finished, float *out_scores, int32_t *out_parents, int32_t *out_tokens,
+                     void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * The pages of a cache: which blocks of a pool the rows of a block table hold, kept
+ * on the device, so that beams can share, fork and drop them between two steps
+ * without a copy to the host. The state is the caller's:
+ *   table   int32 [rows, width]: entry j of a row is the block of its positions
+ *           j bs .. (j + 1) bs - 1 (bs = block_size), negative where it was freed; only the first
+ *           ceil(length / bs) entries of a row are read
+ *   length  int32 [rows]: tokens that a row holds
+ *   refs    int32 [num_blocks]: how many places hold a block -- entries of rows, and
+ *           whatever else the caller counts (a prefix kept for later requests).
+ *           A block with none is free. Free blocks are taken lowest id first, in
+ *           the order of the rows, so every result is determined by its inputs.
+ * One table covers all layers: every layer's pool has a block of each id.
+ * Ids >= num_blocks, lengths outside [0, width * bs], parents >= rows and counts
+ * that would fall below zero raise the library-wide error flag (FNPU_EDEVICE_RANGE from
+ * fnpu_check) and are skipped; nothing is read or written out of bounds. Calls on
+ * the same state must be ordered by the caller (one stream, or events). All device
+ * pointers need the alignment of their type, workspaces 16 bytes; inputs and outputs
+ * must not overlap but for what is said. rows <= 8192 (FNPU_EUNSUPPORTED).
+ */
+typedef struct {
+    int32_t block_size;
+    int32_t num_blocks;
+} fnpu_pages_desc;
+
+/* Bytes of workspace for fnpu_pages_fork and fnpu_pages_compact of up to `rows` rows
+ * (calls that overlap on the GPU need one each; nothing is kept in it). */
+int fnpu_pages_workspace(const fnpu_pages_desc *desc, int32_t rows, int64_t *bytes);
+
+/*
+ * Give pages up. A row whose `ends` flag is set (device uint8 [rows], may be NULL)
+ * gives up all of them and has length 0 then. Of every other row, with window >= 1,
+ * those go that the row's next tokens do not see: entries whose positions all lie at
+ * or past `sinks` and before length + 1 - window (fnpu_window_attn_plan's rule for a
+ * query at position `length`). Entries given up become -1 and their blocks' counts
+ * fall by one. window = 0: only `ends`.
+ */
+int fnpu_pages_free(const fnpu_pages_desc *desc, int32_t *table, int32_t *length, int32_t rows, int32_t width,
+                    const uint8_t *ends, int32_t window, int32_t sinks, int32_t *refs, void *stream);
+
+/*
+ * The rows of the next step. New row r continues row parents[r] (device int32
+ * [new_rows]; negative: an empty row; parents may repeat, rows that none continues
+ * give their pages up) and gets room for `grow` more tokens:
+ *   - it holds its parent's pages, shared;
+ *   - where the parent's last page is partly filled (length % bs != 0) and grow >= 1,
+ *     the row is about to write to it: if other holders are counted than new rows whose last
+ *     page it is, each of those rows takes a copy, else all but the lowest of them do.
+ *     A copy is a new block in the row's table and a pair (held block, new block) in `copies`;
+ *   - then new blocks up to ceil((length + grow) / bs) entries.
+ * Rows take their blocks in order; one whose blocks are not all there (or that would
+ * not fit the width) is not served: it holds its parent's pages, all shared, has its parent's length,
+ * and its slots are -1; later rows that need none are served.
+ *   parents     NULL: new row r continues row r (new_rows = rows); new_table may then be
+ *               table, and new_length length. (With new_rows = 0 every row gives its pages up)
+ *   new_table   int32 [new_rows, width], entries past a row's pages are set to -1
+ *   new_length  int32 [new_rows]: length + grow of the rows that were served
+ *   slots       int64 [new_rows, grow]: the slots of a row's next tokens (what
+ *               fnpu_rope_append and fnpu_kv_append take); -1 where there is none. NULL with grow = 0
+ *   copies      int32 [new_rows, 2]: the pair of a row, or -1, -1
+ *   stats       int32 [4]: blocks that are free then, blocks taken, rows not served,
+ *               copies
+ * The copies have to be made (fnpu_kv_copy_blocks, every layer) before the rows
+ * attend or append; the sources are left as they are.
+ */
+int fnpu_pages_fork(const fnpu_pages_desc *desc, const int32_t *table, const int32_t *length, int32_t rows, int32_t width,
+                    const int32_t *parents, int32_t new_rows, int32_t grow, int32_t *refs, int32_t *new_table,
+                    int32_t *new_length, int64_t *slots, int32_t *copies, int32_t *stats, void *workspace,
+                    int64_t workspace_bytes, void *stream);
+
+/*
+ * Live pages to the lowest ids. With n blocks that have holders, the i-th highest
+ * live block moves to the i-th lowest free one while that is lower, at most
+ * max_copies of them; after all moves the live blocks are 0 .. n - 1.
+ *   table     entries of live pages are rewritten
+ *   copies    int32 [max_copies, 2]: pairs (from, to), then -1, -1; to be made
+ *             (fnpu_kv_copy_blocks, every layer) before the new ids are used
+ *   remap     int32 [num_blocks]: where each block's contents are then, -1 for free
+ *             ones (for holders outside the table)
+ *   stats     int32 [2]: live blocks, blocks moved
+ */
+int fnpu_pages_compact(const fnpu_pages_desc *desc, int32_t *table, const int32_t *length, int32_t rows, int32_t width,
+                       int32_t *refs, int32_t *copies, int32_t max_copies, int32_t *remap, int32_t *stats, void *workspace,
+                       int64_t workspace_bytes, void *stream);
+
+/*
+ * Copy blocks within the pools of num_pools layers: for every pair of `copies` (device
+ * int32 [num_copies, 2]) with no negative id, block copies[i][0] to block copies[i][1]
+ * in every pool, bit for bit, in one launch for up to 64 layers.
+ *   desc, kv_format   the cache, as in fnpu_rope_append (bf16, latent, FP8 with
+ *                     kv_fp8 = 1 and kv_format = FNPU_KV_BF16, or 8-bit blocks)
+ *   k_pools, v_pools  host arrays of num_pools device pointers, read by the call (v_pools
+ *                     NULL for a latent cache); 16-byte aligned pools
+ * No block may be the target of two pairs, or of one and the source of another. Ids
+ * >= num_blocks raise the library-wide error flag and are skipped.
+ * Errors of these calls: FNPU_EINVAL for NULL or misaligned pointers, bad shapes and small
+ * workspaces, FNPU_EUNSUPPORTED, FNPU_ECUDA. Nothing is launched on error.
+ */
+int fnpu_kv_copy_blocks(const fnpu_attn_desc *desc, int32_t kv_format, const int32_t *copies, int32_t num_copies,
+                        void *const *k_pools, void *const *v_pools, int32_t num_pools, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,6 +14,11 @@ kernels. Functions carry the C names without the ``fnpu_`` prefix:
     kv8_attn_plan(desc, kv_format, query_len, context_len, phase, block_table, opts=None, stream=None)
     window_attn_plan(desc, window, sinks, query_len, context_len, phase, block_table, opts=None, stream=None)
     window_decode(desc, window, sinks, context_len, block_table, max_context_len, q, k_cache, v_cache, out, lse, workspace)
+    beam_select(logits, scores, out_scores, out_parents, out_tokens, workspace, finished=None, end_token=-1, stream=None)
+    pages_free(pages, table, length, refs, ends=None, window=0, sinks=0, stream=None)
+    pages_fork(pages, table, length, refs, new_table, new_length, slots, copies, stats, workspace, parents=None, stream=None)
+    pages_compact(pages, table, length, refs, copies, remap, stats, workspace, stream=None)
+    kv_copy_blocks(desc, copies, k_pools, v_pools, kv_format=0, stream=None)
     check(stream=None), plan_check(plan, stream=None), status_str(code)
 
 Device arguments are CUDA torch tensors (torch supplies device memory and
@@ -57,7 +62,8 @@ EXPORTED = (
     "fnpu_dispatch_next_share", "fnpu_mla_expand", "fnpu_mixed_attn_replan",
     "fnpu_plan_decode_share", "fnpu_mixed_step", "fnpu_rope", "fnpu_rope_append", "fnpu_kv_read",
     "fnpu_kv8_block_bytes", "fnpu_kv8_attn_plan", "fnpu_window_attn_plan", "fnpu_window_decode_workspace",
-    "fnpu_window_decode",
+    "fnpu_window_decode", "fnpu_beam_select_workspace", "fnpu_beam_select", "fnpu_pages_workspace", "fnpu_pages_free",
+    "fnpu_pages_fork", "fnpu_pages_compact", "fnpu_kv_copy_blocks",
 )
 
 
@@ -87,6 +93,15 @@ class RopeDesc(ctypes.Structure):
     _fields_ = [("rotary_dim", ctypes.c_int32), ("rotary_offset", ctypes.c_int32),
                 ("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32),
                 ("num_axes", ctypes.c_int32), ("pair_axis", ctypes.c_void_p)]
+
+
+class BeamDesc(ctypes.Structure):
+    _fields_ = [("num_groups", ctypes.c_int32), ("num_beams", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("num_select", ctypes.c_int32), ("dtype", ctypes.c_int32), ("end_token", ctypes.c_int32)]
+
+
+class PagesDesc(ctypes.Structure):
+    _fields_ = [("block_size", ctypes.c_int32), ("num_blocks", ctypes.c_int32)]
 
 
 _lib = None
@@ -143,8 +158,19 @@ def load(build_if_missing: bool = True):
     lib.fnpu_window_attn_plan.argtypes = [DP, i32, i32, i32, P, P, P, P, i32, ctypes.POINTER(PlanOpts), P, ctypes.POINTER(P)]
     lib.fnpu_window_decode_workspace.argtypes = [DP, i32, i32, i32, i32, i32, i64p]
     lib.fnpu_window_decode.argtypes = [DP, i32, i32, i32, P, P, i32, i32, i32, P, P, P, P, P, P, i64, P]
+    BP = ctypes.POINTER(BeamDesc)
+    lib.fnpu_beam_select_workspace.argtypes = [BP, i64p]
+    lib.fnpu_beam_select.argtypes = [BP, P, i64, P, P, P, P, P, P, i64, P]
+    GP = ctypes.POINTER(PagesDesc)
+    lib.fnpu_pages_workspace.argtypes = [GP, i32, i64p]
+    lib.fnpu_pages_free.argtypes = [GP, P, P, i32, i32, P, i32, i32, P, P]
+    lib.fnpu_pages_fork.argtypes = [GP, P, P, i32, i32, P, i32, i32, P, P, P, P, P, P, P, i64, P]
+    lib.fnpu_pages_compact.argtypes = [GP, P, P, i32, i32, P, P, i32, P, P, P, i64, P]
+    lib.fnpu_kv_copy_blocks.argtypes = [DP, i32, P, i32, P, P, i32, P]
     for name in ("fnpu_rope", "fnpu_rope_append", "fnpu_kv_read", "fnpu_kv8_block_bytes", "fnpu_kv8_attn_plan",
-                 "fnpu_window_attn_plan", "fnpu_window_decode_workspace", "fnpu_window_decode"):
+                 "fnpu_window_attn_plan", "fnpu_window_decode_workspace", "fnpu_window_decode", "fnpu_beam_select_workspace",
+                 "fnpu_beam_select", "fnpu_pages_workspace", "fnpu_pages_free", "fnpu_pages_fork", "fnpu_pages_compact",
+                 "fnpu_kv_copy_blocks"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("fnpu_kv_append", "fnpu_mixed_attn_plan", "fnpu_mixed_attn_plan_ex",
                  "fnpu_mixed_attn_run", "fnpu_plan_check", "fnpu_check", "fnpu_plan_info",
@@ -631,3 +657,118 @@ def window_decode(desc: AttnDesc, window: int, sinks: int, context_len, block_ta
 def _workspace(x):
     """(address, bytes) of a workspace tensor or None."""
     return (None, 0) if x is None else (_tptr(x), x.numel() * x.element_size())
+
+
+def beam_select_workspace(groups: int, beams: int, vocab: int, select: int, fp32: bool = True) -> int:
+    """Bytes of workspace that ``beam_select`` needs (with ``fp32`` for logits of either type)."""
+    need = []
+    for dtype in ((0, 1) if fp32 else (0,)):
+        out = ctypes.c_int64()
+        d = BeamDesc(int(groups), int(beams), int(vocab), int(select), dtype, -1)
+        rc = load().fnpu_beam_select_workspace(ctypes.byref(d), ctypes.byref(out))
+        if rc != FNPU_OK:
+            raise FnpuError(rc, "fnpu_beam_select_workspace")
+        need.append(out.value)
+    return max(need)
+
+
+def beam_select(logits, scores, out_scores, out_parents, out_tokens, workspace, finished=None, end_token: int = -1, stream=None) -> None:
+    """The best continuations of every group of beams (``fnpu_beam_select``):
+    logits bf16 or fp32 [groups, beams, vocab], rows possibly apart; scores fp32 and
+    ``finished`` uint8 [groups, beams]; outputs [groups, select]. ``out_parents``
+    are rows of logits, group * beams + beam."""
+    bf16, int32, fp32, _, uint8 = _dtypes or _types()
+    if not logits.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if logits.dtype is not bf16 and logits.dtype is not fp32:
+        raise TypeError("logits are bf16 or fp32")
+    g, b, v = logits.shape
+    sg, sb, sv = logits.stride()
+    if b == 1:
+        sb = sg if g > 1 else v
+    if (sv != 1 and v > 1) or (g > 1 and sg != b * sb):
+        raise ValueError("rows of logits are contiguous and equally far apart")
+    k = out_scores.shape[-1]
+    for x, name, dtype, shape in ((scores, "scores", fp32, (g, b)), (out_scores, "out_scores", fp32, (g, k)),
+                                  (out_parents, "out_parents", int32, (g, k)), (out_tokens, "out_tokens", int32, (g, k)),
+                                  (finished, "finished", uint8, (g, b))):
+        if x is not None and (x.dtype is not dtype or x.shape != shape):
+            raise ValueError(f"{name} is {dtype} of shape {shape}")
+    d = BeamDesc(g, b, v, k, 0 if logits.dtype is bf16 else 1, int(end_token))
+    rc = (_lib or load()).fnpu_beam_select(ctypes.byref(d), logits.data_ptr(), sb, _tptr(scores), _dptr(finished), _tptr(out_scores),
+                                           _tptr(out_parents), _tptr(out_tokens), *_workspace(workspace), _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_beam_select")
+
+
+def make_pages(block_size: int, num_blocks: int) -> PagesDesc:
+    return PagesDesc(int(block_size), int(num_blocks))
+
+
+def pages_workspace(pages: PagesDesc, rows: int) -> int:
+    """Bytes of workspace that ``pages_fork`` and ``pages_compact`` need for up to ``rows`` rows."""
+    out = ctypes.c_int64()
+    rc = load().fnpu_pages_workspace(ctypes.byref(pages), int(rows), ctypes.byref(out))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_pages_workspace")
+    return out.value
+
+
+def pages_free(pages: PagesDesc, table, length, refs, ends=None, window: int = 0, sinks: int = 0, stream=None) -> None:
+    """Give up the pages of rows that end (``ends`` uint8 [rows]) and those behind the
+    window of a row's next token, in place (``fnpu_pages_free``)."""
+    rows, width = table.shape
+    if ends is not None and (ends.dtype is not (_dtypes or _types())[4] or ends.shape != (rows,)):
+        raise ValueError("ends is uint8 [rows]")
+    rc = (_lib or load()).fnpu_pages_free(ctypes.byref(pages), _int32(table, "table", rows, width), _int32(length, "length", rows), rows,
+                                          width, _dptr(ends), int(window), int(sinks), _int32(refs, "refs", pages.num_blocks),
+                                          _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_pages_free")
+
+
+def pages_fork(pages: PagesDesc, table, length, refs, new_table, new_length, slots, copies, stats, workspace, parents=None,
+               stream=None) -> None:
+    """The rows of the next step: row r continues row ``parents[r]``, with room for
+    slots.shape[1] more tokens (``fnpu_pages_fork``); ``refs`` changes in place."""
+    rows, width = table.shape
+    n, grow = slots.shape
+    if slots.dtype is not (_dtypes or _types())[3]:
+        raise TypeError("slots are int64")
+    if parents is None and n != rows:
+        raise ValueError("without parents every row continues itself")
+    rc = (_lib or load()).fnpu_pages_fork(
+        ctypes.byref(pages), _int32(table, "table", rows, width), _int32(length, "length", rows), rows, width,
+        None if parents is None else _int32(parents, "parents", n), n, grow, _int32(refs, "refs", pages.num_blocks),
+        _int32(new_table, "new_table", n, width), _int32(new_length, "new_length", n), _tptr(slots) if grow else None,
+        _int32(copies, "copies", n, 2), _int32(stats, "stats", 4), *_workspace(workspace), _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_pages_fork")
+
+
+def pages_compact(pages: PagesDesc, table, length, refs, copies, remap, stats, workspace, stream=None) -> None:
+    """Live pages to the lowest ids, at most copies.shape[0] of them, in place
+    (``fnpu_pages_compact``); ``kv_copy_blocks`` makes the copies."""
+    rows, width = table.shape
+    rc = (_lib or load()).fnpu_pages_compact(
+        ctypes.byref(pages), _int32(table, "table", rows, width), _int32(length, "length", rows), rows, width,
+        _int32(refs, "refs", pages.num_blocks), _int32(copies, "copies", None, 2), copies.shape[0],
+        _int32(remap, "remap", pages.num_blocks), _int32(stats, "stats", 2), *_workspace(workspace), _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_pages_compact")
+
+
+def kv_copy_blocks(desc: AttnDesc, copies, k_pools, v_pools=None, kv_format: int = KV_BF16, stream=None) -> None:
+    """Copy blocks copies[i][0] to copies[i][1] in the pools of every layer
+    (``fnpu_kv_copy_blocks``); ``k_pools`` and ``v_pools``: sequences of pools."""
+    pools = _layout(bytes(desc), kv_format)[4]
+    n = len(k_pools)
+    if v_pools is not None and len(v_pools) != n:
+        raise ValueError("as many V pools as K pools")
+    kv = [_pool_addresses(pools, k, v) for k, v in zip(k_pools, v_pools if v_pools is not None else [None] * n)]
+    ptrs = ctypes.c_void_p * n
+    rc = (_lib or load()).fnpu_kv_copy_blocks(ctypes.byref(desc), int(kv_format), _int32(copies, "copies", None, 2), copies.shape[0],
+                                              ptrs(*(k for k, _ in kv)), None if v_pools is None else ptrs(*(v for _, v in kv)), n,
+                                              _stream(stream))
+    if rc != FNPU_OK:
+        raise FnpuError(rc, "fnpu_kv_copy_blocks")

@@ -164,6 +164,52 @@ struct RopeAppendArgs {
     int *err;                 // the library-wide error flag
 };
 
+// Selection of a beam search: rows of logits (groups x beams), each in `slices`
+// pieces; parts: (maximum, sum of exp(x - maximum)) of each, keys: its best `select`.
+struct BeamArgs {
+    const void *logits;
+    int64_t stride;  // values between rows
+    const float *scores;
+    const uint8_t *finished;  // may be null
+    float2 *parts;
+    uint64_t *keys;
+    float *out_scores;
+    int32_t *out_parents, *out_tokens;
+    int32_t groups, beams, vocab, select, end_token, slices;
+};
+void beam_split(const fnpu_beam_desc *d, int *values, int *slices);
+int launch_beam_select(const BeamArgs &a, int values, bool fp32, void *stream);
+
+// Page operations (pages.cu); see fnpu.h. Workspace pieces are laid out by the host.
+constexpr int32_t kPagesChunk = 8192;    // counts that a CTA looks through
+constexpr int32_t kPagesMaxRows = 8192;
+struct PagesArgs {
+    int32_t *table;             // rows x width (fork: the old one, read only)
+    const int32_t *length;
+    const int32_t *parents;     // may be null: row r continues row r
+    int32_t *refs;
+    int32_t *new_table, *new_length, *copies, *stats, *remap;
+    int64_t *slots;
+    // workspace: free or live blocks of each chunk; of each new row: length, last page if
+    // partly filled (-1: none, -2: the row cannot grow), its count; of each block: rows
+    // whose last page it is, the lowest of them (fork) or the free and moving blocks' places (compact)
+    int32_t *chunk_count, *row_length, *row_tail, *row_refs, *block_a, *block_b;
+    int *err;                   // the library-wide error flag
+    int32_t block_size, num_blocks, rows, width, new_rows, grow, max_copies, chunks;
+};
+int launch_pages_free(const PagesArgs &a, int32_t *length, const uint8_t *ends, int32_t window, int32_t sinks, void *stream);
+int launch_pages_fork(const PagesArgs &a, void *stream);
+int launch_pages_compact(const PagesArgs &a, void *stream);
+constexpr int kCopyPools = 128;  // pools of one launch: K and V of 64 layers
+struct CopyArgs {
+    const int32_t *copies;
+    int *err;
+    int64_t block_bytes;
+    int32_t num_copies, num_blocks, pools;
+    void *pool[kCopyPools];
+};
+int launch_copy_blocks(const CopyArgs &a, void *stream);
+
 // A sliding window (size 0: none): a query at position p sees keys p - size + 1 .. p
 // and the first `sinks` of its sequence.
 struct Window {
