@@ -8,10 +8,8 @@ int shape_ok(const fnpu_beam_desc *d) {
     if (!d || d->num_groups < 0 || d->num_beams < 1 || d->vocab < 1 || d->num_select < 1) return FNPU_EINVAL;
     if ((d->dtype != FNPU_LOGITS_BF16 && d->dtype != FNPU_LOGITS_FP32) || d->end_token < -1 || d->end_token >= d->vocab) return FNPU_EINVAL;
     if (d->num_beams > 128 || d->num_select > 64 || d->vocab > (1 << 24)) return FNPU_EUNSUPPORTED;
-    int values, slices;
-    beam_split(d, &values, &slices);
     // (the grid and each row's parent are 32-bit)
-    return static_cast<int64_t>(d->num_groups) * d->num_beams * slices > INT32_MAX ? FNPU_EUNSUPPORTED : FNPU_OK;
+    return static_cast<int64_t>(d->num_groups) * d->num_beams * beam_slices(d) > INT32_MAX ? FNPU_EUNSUPPORTED : FNPU_OK;
 }
 
 // Bytes of the slices' parts (8 each), then of their lists.
@@ -19,8 +17,7 @@ int64_t parts_bytes(const fnpu_beam_desc *d, int slices) {
     return (static_cast<int64_t>(d->num_groups) * d->num_beams * slices * 8 + 15) / 16 * 16;
 }
 int64_t workspace_bytes_of(const fnpu_beam_desc *d) {
-    int values, slices;
-    beam_split(d, &values, &slices);
+    const int slices = beam_slices(d);
     return parts_bytes(d, slices) + static_cast<int64_t>(d->num_groups) * d->num_beams * slices * d->num_select * 8;
 }
 
@@ -52,9 +49,8 @@ int fnpu_beam_select(const fnpu_beam_desc *desc, const void *logits, int64_t row
         (reinterpret_cast<uintptr_t>(workspace) & 15u))
         return FNPU_EINVAL;
     if (workspace_bytes < workspace_bytes_of(desc)) return FNPU_EINVAL;
-    int values;
     BeamArgs a = {};
-    beam_split(desc, &values, &a.slices);
+    a.slices = beam_slices(desc);
     a.logits = logits;
     a.stride = row_stride;
     a.scores = scores;
@@ -69,7 +65,7 @@ int fnpu_beam_select(const fnpu_beam_desc *desc, const void *logits, int64_t row
     a.vocab = desc->vocab;
     a.select = desc->num_select;
     a.end_token = desc->end_token;
-    return launch_beam_select(a, values, fp32, stream);
+    return launch_beam_select(a, fp32, stream);
 }
 
 }  // extern "C"

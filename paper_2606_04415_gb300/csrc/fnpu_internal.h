@@ -177,8 +177,8 @@ struct BeamArgs {
     int32_t *out_parents, *out_tokens;
     int32_t groups, beams, vocab, select, end_token, slices;
 };
-void beam_split(const fnpu_beam_desc *d, int *values, int *slices);
-int launch_beam_select(const BeamArgs &a, int values, bool fp32, void *stream);
+int beam_slices(const fnpu_beam_desc *d);
+int launch_beam_select(const BeamArgs &a, bool fp32, void *stream);
 
 // Page operations (pages.cu); see fnpu.h. Workspace pieces are laid out by the host.
 constexpr int32_t kPagesChunk = 8192;    // counts that a CTA looks through
