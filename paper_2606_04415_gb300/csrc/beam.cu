@@ -6,19 +6,24 @@
 //   * A CTA of the first takes a slice of a row and leaves its maximum, the sum of
 //     exp(x - max) and its best num_select values in order. Within a row the order
 //     of the totals is the order of the logits, ties to the lower token, so candidates
-//     need no normalisation. Each warp streams a part of the slice by itself: a value
-//     costs a conversion, half a paired multiply-add, an exponential and half a paired
-//     addition, and bf16 maxima go in pairs; a reference that all of a warp's sums share moves only when
-//     a tile has a value 2^8 above it. Candidates are what reaches a bound: the
-//     K-th largest of the maxima of 64 subsets of what the warp has seen, which at least
-//     K values reach. It is formed anew after 1, 2, 4, .. tiles, so that some K log n
-//     values become candidates; a list that fills up is cut to its best K.
+//     need no normalisation. A value costs a conversion, half a paired multiply-add,
+//     an exponential and half a paired addition, and bf16 maxima go in pairs; a
+//     reference that all of a warp's sums share moves only when a tile has a value 2^8
+//     above it. Candidates are chunks of 16 bytes whose maximum reaches a bound: the
+//     K-th largest of the maxima of 64 subsets of what the CTA has seen, which at least
+//     K values reach. It is formed anew after 1, 4, 16, .. tiles, so only some
+//     K log n chunks are noted (4 bytes each, their values read again at the
+//     end); a warp's list that fills up is cut to the chunks of its best K values.
+//     Slices, chunks and the order of the sums go by token numbers, wherever a row
+//     starts in memory: beams with equal logits have equal sums to the last bit.
 //   * A CTA of the second takes a group: the rows' log-sum-exps from their slices',
-//     then the best of all slices' lists by the total in 64 bits. Totals of
-//     different beams may lie closer than an fp32 score of some hundred resolves
-//     (3e-5); fp64 is slow on this device, so only what an fp32 total with its error
-//     cannot rule out is added in 64 bits, and order-preserving integers are compared.
+//     then the best of all slices' lists by the total. Totals of different beams
+//     may lie closer than an fp32 score of some hundred resolves (3e-5), and fp64 is slow
+//     on this device (a warp's instruction takes some 60 cycles), so totals are
+//     unevaluated sums of two floats (Dekker 1971), compared as order-preserving integers.
 #include <float.h>
+
+#include <algorithm>
 
 #include "common.cuh"
 
@@ -30,7 +35,8 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kLoads = 4;           // 16-byte loads of a lane in a tile
 constexpr int kMergeThreads = 256;  // of the second
 constexpr int kSubsets = 64;        // (num_select is at most as many)
-constexpr int kWarpList = 384;      // candidates of a warp: 64, and 256 of one load
+constexpr int kMergeSubsets = 128;  // (two threads count for each)
+constexpr int kWarpList = 512;      // chunks that a warp notes
 constexpr int kList = 512;          // candidates of a CTA
 
 // Order-preserving bits of a float, and back.
@@ -105,48 +111,102 @@ struct Pack<float> {
 // NaN counts as -inf, +inf as the largest finite value.
 __device__ __forceinline__ float clean(float x) { return fminf(fmaxf(x, -INFINITY), FLT_MAX); }
 
-// The K-th largest of a warp's 64 values, two a lane (order bits).
-__device__ __forceinline__ uint32_t kth_of_64(uint32_t a, uint32_t b, int K, int lane) {
-    const bool low = K > 32;  // from the other end: the (65 - K)-th smallest
-    const int n = low ? 65 - K : K;
-    if (low) {
-        a = ~a;
-        b = ~b;
-    }
+// The K-th largest of a warp's 64 values, two a lane (order bits, of which the
+// `kBits` highest differ).
+template <int kBits>
+__device__ __forceinline__ uint32_t kth_of_64(uint32_t a, uint32_t b, int K) {
     uint32_t top = 0u;
-    for (int r = 0; r < n; ++r) {
-        top = __reduce_max_sync(0xffffffffu, max(a, b));
-        const uint32_t who = __ballot_sync(0xffffffffu, a == top || b == top);
-        if (lane == __ffs(who) - 1) {  // one of them goes (0 is below every value's bits, and above none's)
-            if (a == top) a = 0u;
-            else b = 0u;
-        }
+#pragma unroll
+    for (int i = 31; i >= 32 - kBits; --i) {
+        const uint32_t t = top | 1u << i;
+        if (__popc(__ballot_sync(0xffffffffu, a >= t)) + __popc(__ballot_sync(0xffffffffu, b >= t)) >= K) top = t;
     }
-    return low ? ~top : top;
+    // (of a negative value the bits below are ones)
+    return kBits < 32 && !(top >> 31) ? top | 0xFFFFu : top;
 }
 
-// The best K of a warp's list, in its first K places; returns the K-th.
-__device__ __noinline__ uint64_t cut_list(uint64_t *list, int n, int K) {
-    const int lane = threadIdx.x & 31;
-    uint64_t keep0 = 0, keep1 = 0, last = ~0ull;
-    __syncwarp();
-    for (int r = 0; r < K; ++r) {
-        uint64_t k = 0;
-        for (int i = lane; i < n; i += 32) {
-            const uint64_t e = list[i];
-            if (e < last) k = max(k, e);
+// A row as chunks of 16 bytes from its first token on; past its end there is -inf.
+// Where its rows do not start on 16 bytes a chunk is cut from two neighbouring ones.
+template <typename T, bool kAligned>
+struct Row {
+    static constexpr int kV = Pack<T>::kN;
+    const T *src;
+    const uint4 *base;  // 16-byte boundary at or before the row
+    int vocab, head;    // values between `base` and the row
+
+    __device__ __forceinline__ Row(const void *logits, int64_t at, int n) : src(static_cast<const T *>(logits) + at), vocab(n) {
+        head = kAligned ? 0 : static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15u) / sizeof(T));
+        base = reinterpret_cast<const uint4 *>(src - head);
+    }
+    __device__ __forceinline__ uint4 chunk(int c) const {
+        const int first = c * kV;
+        if (kAligned || head == 0) {
+            if (first + kV <= vocab) return __ldcs(base + c);
+        } else if (first >= head && first + 2 * kV - head <= vocab) {  // (both boundaries' chunks are the row's)
+            uint4 l = __ldcs(base + c), h = __ldcs(base + c + 1);
+            const int s = head * static_cast<int>(sizeof(T));  // bytes to leave out
+            if (s & 8) {
+                l = make_uint4(l.z, l.w, h.x, h.y);
+                h.x = h.z;
+                h.y = h.w;
+            }
+            if (s & 4) {
+                l = make_uint4(l.y, l.z, l.w, h.x);
+                h.x = h.y;
+            }
+            if (sizeof(T) == 2 && (s & 2))
+                l = make_uint4(__funnelshift_r(l.x, l.y, 16), __funnelshift_r(l.y, l.z, 16), __funnelshift_r(l.z, l.w, 16),
+                               __funnelshift_r(l.w, h.x, 16));
+            return l;
         }
-        last = warp_max(k);
-        if (lane == (r & 31)) {
-            if (r < 32) keep0 = last;
-            else keep1 = last;
+        uint4 v = make_uint4(Pack<T>::kNone, Pack<T>::kNone, Pack<T>::kNone, Pack<T>::kNone);
+        T *t = reinterpret_cast<T *>(&v);
+#pragma unroll
+        for (int j = 0; j < kV; ++j)
+            if (first + j < vocab) t[j] = src[first + j];
+        return v;
+    }
+    // f(key) of every value of a chunk that may be a candidate
+    template <typename F>
+    __device__ __forceinline__ void keys(int c, F f) const {
+        const uint4 v = chunk(c);
+#pragma unroll
+        for (int j = 0; j < kV; ++j) {
+            const float x = clean(Pack<T>::get(v, j));
+            if (x > -INFINITY) f(row_key(x, c * kV + j));
         }
     }
+};
+
+// Cuts a warp's list of n chunks (K or more, each with a candidate) to those of its best
+// K values, in place; returns the last of these and how many chunks there are.
+struct Cut {
+    uint64_t last;
+    int len;
+};
+template <typename T, bool kAligned>
+__device__ __noinline__ Cut cut_list(const void *logits, int64_t at, int vocab, int *list, int n, int K) {
+    const Row<T, kAligned> row(logits, at, vocab);
+    const int lane = threadIdx.x & 31;
+    uint64_t last = ~0ull;
     __syncwarp();
-    if (lane < K) list[lane] = keep0;
-    if (lane + 32 < K) list[lane + 32] = keep1;
+    for (int r = 0; r < K; ++r) {
+        uint64_t k = 0ull;
+        for (int i = lane; i < n; i += 32) row.keys(list[i], [&](uint64_t e) { if (e < last) k = max(k, e); });
+        last = warp_max(k);
+    }
+    int kept = 0;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int c = i0 + lane < n ? list[i0 + lane] : -1;
+        bool in = false;
+        if (c >= 0) row.keys(c, [&](uint64_t e) { in |= e >= last; });
+        __syncwarp();  // (all have read before any write, which is no further than they have read)
+        const uint32_t who = __ballot_sync(0xffffffffu, in);
+        if (in) list[kept + __popc(who & ((1u << lane) - 1))] = c;
+        kept += __popc(who);
+    }
     __syncwarp();
-    return last;
+    return Cut{last, kept};
 }
 
 // The maximum and sum of a slice again, value by value, where NaN or an infinity is among them.
@@ -174,56 +234,66 @@ __device__ __noinline__ float2 clean_sum(const T *src, int e0, int e1, float *s_
     return make_float2(m, block(z, true));
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 6) beam_slice_kernel(const BeamArgs a) {
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs a) {
     typedef Pack<T> P;
-    constexpr int kV = P::kN;
-    __shared__ uint64_t s_lists[kWarps][kWarpList];
+    constexpr int kV = P::kN, kBits = 8 * sizeof(T), kStep = 32 * kWarps;  // chunks of a load of the CTA
+    __shared__ int s_chunks[kWarps][kWarpList];
     __shared__ uint64_t s_list[kList];
-    __shared__ float s_ref[kWarps], s_sum[kWarps], s_bound[kWarps], s_part[kWarps];
+    __shared__ uint32_t s_seen[kWarps][kSubsets];
+    __shared__ float s_ref[kWarps], s_sum[kWarps], s_cut[kWarps], s_part[kWarps];
     __shared__ uint64_t s_best[kWarps];
-    __shared__ int s_len[kWarps], s_count;
+    __shared__ int s_count;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices;
+    const int r = blockIdx.x / a.slices, slice = blockIdx.x - r * a.slices;
     const int K = a.select;
     pdl_trigger();
     pdl_wait();  // the logits and scores of the kernel before, and the last call's reads of the workspace
-    if (row_closed(a, row)) return;
+    if (row_closed(a, r)) return;
     if (tid == 0) s_count = 0;
 
-    // 16-byte chunks of memory; the row's first and last may hold neighbours' values
-    const T *src = static_cast<const T *>(a.logits) + static_cast<int64_t>(row) * a.stride;
-    const int head = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15u) / sizeof(T));
-    const uint4 *base = reinterpret_cast<const uint4 *>(src - head);
-    const int chunks = (head + a.vocab + kV - 1) / kV;
-    const int per = (chunks + a.slices - 1) / a.slices;
+    const Row<T, kAligned> row(a.logits, static_cast<int64_t>(r) * a.stride, a.vocab);
+    const int chunks = (a.vocab + kV - 1) / kV, per = (chunks + a.slices - 1) / a.slices;
     const int c0 = min(chunks, slice * per), c1 = min(chunks, c0 + per);
-    // (whole loads of a warp to each warp)
-    const int wper = ((c1 - c0 + kWarps - 1) / kWarps + 31) / 32 * 32;
-    const int w0 = min(c1, c0 + warp * wper), w1 = min(c1, w0 + wper);
-    auto load = [&](int c) -> uint4 {
-        const int first = c * kV - head;
-        if (c < w1 && first >= 0 && first + kV <= a.vocab) return __ldcs(base + c);
-        uint4 v = make_uint4(P::kNone, P::kNone, P::kNone, P::kNone);
-        if (c < w1) {  // the row's first or last chunk
-            T *t = reinterpret_cast<T *>(&v);
-#pragma unroll
-            for (int j = 0; j < kV; ++j)
-                if (first + j >= 0 && first + j < a.vocab) t[j] = src[first + j];
-        }
-        return v;
-    };
+    const int tiles = (c1 - c0 + kStep * kLoads - 1) / (kStep * kLoads);
+    const uint4 none = make_uint4(P::kNone, P::kNone, P::kNone, P::kNone);
+    auto load = [&](int c) { return c < c1 ? row.chunk(c) : none; };
 
-    uint64_t *list = s_lists[warp];
+    int *list = s_chunks[warp];
     int len = 0;
-    typename P::Max seen = P::none();           // maxima of the lane's two subsets
-    float bound = -INFINITY, reach = -FLT_MAX;  // K values of the list reach `bound`; candidates reach `reach`
-    float ref = -INFINITY, c = 0.f;             // the sums' reference, and ref log2(e) as fp32 has it
+    typename P::Max seen = P::none();  // maxima of the lane's two subsets
+    float reach = -FLT_MAX;            // what a chunk's maximum has to reach to be noted
+    float cut = -INFINITY;             // K values of the warp's list reach it
+    float ref = -INFINITY, c = 0.f;    // the sums' reference, and ref log2(e) as fp32 has it
     uint64_t z0 = f2_pack(0.f, 0.f), z1 = z0;
-    for (int t = 0, at = w0; at < w1; ++t, at += 32 * kLoads) {
+    // The K-th largest of the maxima of the CTA's subsets. (Every warp comes here after
+    // the same tiles, so what the bound goes by has lower tokens than all later tiles.)
+    auto bound = [&]() {
+        s_seen[warp][lane] = order_bits(P::lo(seen));
+        s_seen[warp][lane + 32] = order_bits(P::hi(seen));
+        __syncthreads();
+        uint32_t x = s_seen[0][lane], y = s_seen[0][lane + 32];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+            x = max(x, s_seen[w][lane]);
+            y = max(y, s_seen[w][lane + 32]);
+        }
+        return clean(from_order(max(kth_of_64<kBits>(x, y, K), order_bits(-INFINITY))));
+    };
+    uint4 next[kLoads];
+    int at = c0 + warp * 32 + lane;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) next[i] = load(at + i * kStep);
+    for (int t = 0, renew = 0; t < tiles; ++t) {
         uint4 v[kLoads];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) v[i] = load(at + 32 * i + lane);
+        for (int i = 0; i < kLoads; ++i) v[i] = next[i];
+        const int here = at;
+        at += kLoads * kStep;
+        if (t + 1 < tiles) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) next[i] = load(at + i * kStep);
+        }
         typename P::Max mx[kLoads], all = P::none();
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -245,7 +315,8 @@ __global__ void __launch_bounds__(kThreads, 6) beam_slice_kernel(const BeamArgs 
         if (ref > -INFINITY) {
             const uint64_t l2 = f2_pack(kLog2e, kLog2e), c2 = f2_pack(-c, -c);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
+            for (int i = 0; i < kLoads; ++i) {
+                if (here - lane + i * kStep >= c1) break;
 #pragma unroll
                 for (int j = 0; j < kV; j += 2) {
                     float x, y;
@@ -254,36 +325,33 @@ __global__ void __launch_bounds__(kThreads, 6) beam_slice_kernel(const BeamArgs 
                     if (j & 2) z1 = f2_add(z1, e);
                     else z0 = f2_add(z0, e);
                 }
-        }
-        const bool renew = (t & (t + 1)) == 0;
-        if (renew) {
-            const uint32_t k = kth_of_64(order_bits(P::lo(seen)), order_bits(P::hi(seen)), K, lane);
-            const float b = fminf(from_order(k), FLT_MAX);
-            if (b > bound) {
-                bound = b;
-                reach = fmaxf(reach, b);
             }
+        }
+        const bool now = t == renew;
+        float b = -INFINITY;
+        if (now) {
+            renew = 4 * renew + 3;
+            b = bound();
+            reach = fmaxf(reach, b);
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            if (!__any_sync(0xffffffffu, fmaxf(P::lo(mx[i]), P::hi(mx[i])) >= reach)) continue;
-            if (len > kWarpList - 32 * kV) {
-                const float b = key_value(cut_list(list, len, K));
-                len = K;
-                bound = fmaxf(bound, b);
-                reach = fmaxf(reach, from_order(order_bits(b) + 1));  // (later equals are higher tokens)
+            const bool in = fmaxf(P::lo(mx[i]), P::hi(mx[i])) >= reach;
+            const uint32_t who = __ballot_sync(0xffffffffu, in);
+            if (who == 0u) continue;
+            if (len > kWarpList - 32) {
+                const Cut k = cut_list<T, kAligned>(a.logits, static_cast<int64_t>(r) * a.stride, a.vocab, list, len, K);
+                len = k.len;
+                cut = key_value(k.last);
+                // (the list's values have lower tokens than all that follow)
+                reach = fmaxf(reach, from_order(order_bits(cut) + 1));
             }
-#pragma unroll
-            for (int j = 0; j < kV; ++j) {
-                const float x = P::get(v[i], j);
-                const bool in = x >= reach;
-                const uint32_t who = __ballot_sync(0xffffffffu, in);
-                if (in) list[len + __popc(who & ((1u << lane) - 1))] = row_key(fminf(x, FLT_MAX), (at + 32 * i + lane) * kV - head + j);
-                len += __popc(who);
-            }
+            if (in) list[len + __popc(who & ((1u << lane) - 1))] = here + i * kStep;
+            len += __popc(who);
         }
-        // from the next tile on, equals of the bound are higher tokens than K that are in the list
-        if (renew && bound > -INFINITY) reach = fmaxf(reach, from_order(order_bits(bound) + 1));
+        // from the next tile on, equals of the bound are higher tokens than K that reach it
+        if (b > -INFINITY) reach = fmaxf(reach, from_order(order_bits(b) + 1));
+        if (now && t + 1 < tiles) __syncthreads();  // (s_seen is written again)
     }
     {
         float x, y;
@@ -294,68 +362,90 @@ __global__ void __launch_bounds__(kThreads, 6) beam_slice_kernel(const BeamArgs 
         if (lane == 0) {
             s_ref[warp] = ref;
             s_sum[warp] = z;
-            s_bound[warp] = bound;
-            s_len[warp] = len;
+            s_cut[warp] = cut;
         }
     }
     __syncthreads();
+    float floor = bound();
     // the slice's sum over 2^c, c = max log2(e) rounded, then over e^max: the rounding of c is taken out
-    float m = s_ref[0], floor = s_bound[0], z = 0.f;
+    float m = s_ref[0], z = 0.f;
+    floor = fmaxf(floor, s_cut[0]);
 #pragma unroll
     for (int i = 1; i < kWarps; ++i) {
         m = fmaxf(m, s_ref[i]);
-        floor = fmaxf(floor, s_bound[i]);
+        floor = fmaxf(floor, s_cut[i]);
     }
+    // the values that reach the bound, and the bounds of the warps' cuts
+    auto values = [&](auto f) {
+        for (int i = lane; i < len; i += 32) row.keys(list[i], f);
+    };
+    values([&](uint64_t key) {
+        if (key_value(key) < floor) return;
+        const int n = atomicAdd(&s_count, 1);
+        if (n < kList) s_list[n] = key;
+    });
     c = m * kLog2e;
     for (int i = 0; i < kWarps; ++i)
         if (s_ref[i] > -INFINITY) z += s_sum[i] * fast_exp2(s_ref[i] * kLog2e - c);
     z -= z * fmaf(m, kLog2e, -c) * kLn2;
     float2 part = make_float2(m, z);
-    if (m > -INFINITY && !(z < INFINITY)) {  // NaN or +inf among the values
-        const int e0 = max(0, c0 * kV - head), e1 = min(a.vocab, c1 * kV - head);
-        part = clean_sum(src, e0, e1, s_part);
-    }
+    if (m > -INFINITY && !(z < INFINITY)) part = clean_sum(row.src, c0 * kV, min(a.vocab, c1 * kV), s_part);  // NaN or +inf among them
     if (tid == 0) a.parts[blockIdx.x] = part;
-    // what reaches the best of the warps' bounds (K values of that warp do)
-    for (int i0 = 0; i0 < len; i0 += 32) {
-        const uint64_t key = i0 + lane < len ? list[i0 + lane] : 0ull;
-        const bool in = key != 0ull && key_value(key) >= floor;
-        const uint32_t who = __ballot_sync(0xffffffffu, in);
-        int n = 0;
-        if (lane == 0 && who) n = atomicAdd(&s_count, __popc(who));
-        n = __shfl_sync(0xffffffffu, n, 0) + __popc(who & ((1u << lane) - 1));
-        if (in && n < kList) s_list[n] = key;
-    }
     __syncthreads();
     const int n = s_count;
     uint64_t *keys = a.keys + static_cast<int64_t>(blockIdx.x) * K;
     if (n <= kList) {
         for (int i = tid; i < n; i += kThreads) {
             const uint64_t key = s_list[i];
-            int r = 0;
-            for (int j = 0; j < n; ++j) r += s_list[j] > key;
-            if (r < K) keys[r] = key;
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += s_list[j] > key;
+            if (rank < K) keys[rank] = key;
         }
         for (int i = n + tid; i < K; i += kThreads) keys[i] = 0ull;
         return;
     }
     uint64_t last = ~0ull;  // K rounds of a maximum over the warps' lists
-    for (int r = 0; r < K; ++r) {
+    for (int i = 0; i < K; ++i) {
         uint64_t k = 0ull;
-        for (int i = lane; i < len; i += 32)
-            if (list[i] < last) k = max(k, list[i]);
+        values([&](uint64_t key) { if (key < last) k = max(k, key); });
         k = warp_max(k);
         __syncthreads();
         if (lane == 0) s_best[warp] = k;
         __syncthreads();
         last = s_best[0];
 #pragma unroll
-        for (int i = 1; i < kWarps; ++i) last = max(last, s_best[i]);
-        if (tid == 0) keys[r] = last;  // (0 once there are none left)
+        for (int w = 1; w < kWarps; ++w) last = max(last, s_best[w]);
+        if (tid == 0) keys[i] = last;  // (0 once there are none left)
     }
 }
 
-// A candidate of a group: a larger total (order-preserving bits of a double) is
+// Unevaluated sums of two floats, the second at most half a step of the first.
+struct Two {
+    float hi, lo;
+};
+__device__ __forceinline__ Two two_sum(float a, float b) {  // exact
+    const float s = a + b, t = s - a;
+    return Two{s, (a - (s - t)) + (b - t)};
+}
+__device__ __forceinline__ Two two_norm(float hi, float lo) {
+    const float s = hi + lo;
+    return fabsf(s) < INFINITY ? Two{s + 0.f, (lo - (s - hi)) + 0.f} : Two{s, 0.f};  // (no zero is negative)
+}
+// ln z, z of 1 or more (but for rounding): z = 2^e f, ln f = 2 atanh((f - 1) / (f + 1))
+// by its series. Off by some 1e-9.
+__device__ Two two_log(float z) {
+    const int bits = __float_as_int(z), e = (bits - __float_as_int(0.70710678f)) >> 23;
+    const float f = __int_as_float(bits - (e << 23)), n = f - 1.f;  // (exact: f is 0.7 .. 1.42)
+    const Two d = two_sum(f, 1.f);
+    const float q = n / d.hi, q1 = (fmaf(-q, d.hi, n) - q * d.lo) / d.hi, s = q * q;
+    const float p = s * fmaf(s, fmaf(s, fmaf(s, fmaf(s, 1.f / 11, 1.f / 9), 1.f / 7), 1.f / 5), 1.f / 3);
+    constexpr float kHi = 45426.f / 65536.f;  // (16 bits of ln 2: e kHi is exact)
+    constexpr float kLo = static_cast<float>(0.69314718055994530942 - 45426.0 / 65536.0);
+    const Two t = two_sum(e * kHi, 2.f * q);
+    return two_norm(t.hi, t.lo + fmaf(static_cast<float>(e), kLo, 2.f * fmaf(q, p, q1)));
+}
+
+// A candidate of a group: a larger total (order-preserving bits of its two floats) is
 // better, ties to the lower beam and token.
 struct Cand {
     uint64_t total;
@@ -365,35 +455,39 @@ __device__ __forceinline__ Cand no_cand() { return Cand{0ull, INT64_MAX}; }
 __device__ __forceinline__ bool better(const Cand &a, const Cand &b) {
     return a.total > b.total || (a.total == b.total && a.tie < b.tie);
 }
-__device__ __forceinline__ uint64_t order_bits64(double x) {
-    const uint64_t b = static_cast<uint64_t>(__double_as_longlong(x));
-    return b ^ ((b >> 63) ? ~0ull : 1ull << 63);
-}
-__device__ __forceinline__ double from_order64(uint64_t o) {
-    return __longlong_as_double(static_cast<long long>(o ^ ((o >> 63) ? 1ull << 63 : ~0ull)));
-}
+__device__ __forceinline__ uint64_t order_bits2(Two x) { return static_cast<uint64_t>(order_bits(x.hi)) << 32 | order_bits(x.lo); }
 
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
-    // of the group's beams: maximum logit, score - log sum exp(x - maximum), and both in fp32
-    double *s_max = reinterpret_cast<double *>(smem), *s_off = s_max + a.beams;
-    float *s_maxf = reinterpret_cast<float *>(s_off + a.beams), *s_offf = s_maxf + a.beams;
-    int *s_open = reinterpret_cast<int *>(s_offf + a.beams);
+    // of the group's beams: maximum logit, and score - log sum exp(x - maximum)
+    Two *s_off = reinterpret_cast<Two *>(smem);
+    float *s_max = reinterpret_cast<float *>(s_off + a.beams);
+    int *s_open = reinterpret_cast<int *>(s_max + a.beams);
     __shared__ Cand s_best[kMergeThreads];
-    __shared__ Cand s_sub[kSubsets];
     __shared__ Cand s_list[kList];
-    __shared__ Cand s_bound;
+    __shared__ __align__(16) uint64_t s_sub[kMergeSubsets];
+    __shared__ uint64_t s_bound;
     __shared__ int s_count;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = blockIdx.x, W = a.beams, S = a.slices, K = a.select;
     pdl_trigger();
     pdl_wait();
-    if (tid == 0) s_count = 0;
+    if (tid == 0) {
+        s_count = 0;
+        s_bound = 0ull;
+    }
+    // what a thread looks at below, on its way before the sums are known (a closed
+    // beam's lists are not written; they are not looked at either)
+    const uint64_t *keys = a.keys + static_cast<int64_t>(g) * W * S * K;
+    // (the lists' heads, and where there are few lists what is next in them)
+    const int deep = min(K, (kMergeSubsets + W * S - 1) / (W * S));
+    const uint64_t head0 = tid < W * S * deep ? keys[tid % (W * S) * K + tid / (W * S)] : 0ull;
+    const uint64_t key0 = tid < W * S * K ? keys[tid] : 0ull;
+    const uint64_t key1 = tid + kMergeThreads < W * S * K ? keys[tid + kMergeThreads] : 0ull;
     for (int w = warp; w < W; w += kMergeThreads / 32) {
         const int row = g * W + w;
         const bool open = !row_closed(a, row);
-        float m = -INFINITY;
-        double z = 0.0;
+        float m = -INFINITY, z = 0.f;
         if (open) {
             const float2 *part = a.parts + static_cast<int64_t>(row) * S;
             for (int s = lane; s < S; s += 32) m = fmaxf(m, part[s].x);
@@ -401,91 +495,71 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
             for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
             for (int s = lane; s < S; s += 32) {
                 const float2 p = part[s];
-                if (p.x > -INFINITY) z += static_cast<double>(p.y * expf(p.x - m));
+                if (p.x > -INFINITY) z += p.y * expf(p.x - m);
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
         }
         if (lane == 0) {
-            s_max[w] = s_maxf[w] = m;
-            s_off[w] = z;
+            s_max[w] = m;
             s_open[w] = open && m > -INFINITY;
+            if (s_open[w]) {
+                const Two l = two_log(z), o = two_sum(a.scores[row], -l.hi);
+                s_off[w] = two_norm(o.hi, o.lo - l.lo);
+            }
         }
     }
     __syncthreads();
-    for (int w = tid; w < W; w += kMergeThreads) {  // (one warp's logarithms cost as much as one lane's)
-        s_off[w] = s_open[w] ? static_cast<double>(a.scores[g * W + w]) - log(s_off[w]) : 0.0;
-        s_offf[w] = static_cast<float>(s_off[w]);
-    }
-    __syncthreads();
-    const uint64_t *keys = a.keys + static_cast<int64_t>(g) * W * S * K;
     auto cand = [&](int w, uint64_t key) {
-        return Cand{order_bits64((static_cast<double>(key_value(key)) - s_max[w]) + s_off[w]),
+        const Two d = two_sum(key_value(key), -s_max[w]), off = s_off[w], t = two_sum(d.hi, off.hi);
+        return Cand{order_bits2(two_norm(t.hi, t.lo + (d.lo + off.lo))),
                     static_cast<int64_t>(w) * a.vocab + static_cast<int64_t>(0xFFFFFFFFu - static_cast<uint32_t>(key))};
     };
     auto end_of = [&](int w) {  // the one continuation of a finished beam
         const int row = g * W + w;
         const float s = a.scores[row];
         if (a.finished == nullptr || a.finished[row] == 0 || a.end_token < 0 || !(s > -INFINITY)) return no_cand();
-        return Cand{order_bits64(static_cast<double>(s)), static_cast<int64_t>(w) * a.vocab + a.end_token};
+        return Cand{order_bits2(two_norm(s, 0.f)), static_cast<int64_t>(w) * a.vocab + a.end_token};
     };
-    // each thread's best of the lists' heads, and the K-th best of the subsets of threads
-    Cand best = no_cand();
-    for (int l = tid; l < W * S; l += kMergeThreads) {
-        const int w = l / S;
-        const uint64_t key = s_open[w] ? keys[static_cast<int64_t>(l) * K] : 0ull;
-        if (key != 0ull) {
-            const Cand c = cand(w, key);
-            if (better(c, best)) best = c;
+    // the K-th best of the subsets' bests (threads t and t + kMergeSubsets), which K candidates reach
+    uint64_t best = 0ull;
+    for (int i = tid; i < W * S * deep; i += kMergeThreads) {
+        const int l = i % (W * S), w = l / S;
+        const uint64_t key = !s_open[w] ? 0ull : i == tid ? head0 : keys[l * K + i / (W * S)];
+        if (key != 0ull) best = max(best, cand(w, key).total);
+    }
+    for (int w = tid; w < W; w += kMergeThreads) best = max(best, end_of(w).total);
+    if (tid >= kMergeSubsets) s_best[tid].total = best;
+    __syncthreads();
+    if (tid < kMergeSubsets) s_sub[tid] = max(best, s_best[tid + kMergeSubsets].total);
+    __syncthreads();
+    {
+        const uint64_t mine = s_sub[tid / 2];
+        int above = 0, reach = 0;
+#pragma unroll 8
+        for (int i = tid % 2; i < kMergeSubsets / 2; i += 2) {
+            const ulonglong2 o = reinterpret_cast<const ulonglong2 *>(s_sub)[i];
+            above += (o.x > mine) + (o.y > mine);
+            reach += (o.x >= mine) + (o.y >= mine);
         }
-    }
-    for (int w = tid; w < W; w += kMergeThreads) {
-        const Cand c = end_of(w);
-        if (better(c, best)) best = c;
-    }
-    s_best[tid] = best;
-    __syncthreads();
-    if (tid < kSubsets) {
-#pragma unroll
-        for (int i = 1; i < kMergeThreads / kSubsets; ++i)
-            if (better(s_best[tid + kSubsets * i], best)) best = s_best[tid + kSubsets * i];
-        s_sub[tid] = best;
+        above += __shfl_xor_sync(0xffffffffu, above, 1);
+        reach += __shfl_xor_sync(0xffffffffu, reach, 1);
+        if (above < K && K <= reach) s_bound = mine;  // (all that get here have the same)
     }
     __syncthreads();
-    {  // four threads a subset count the better ones (of equal ones, which are none, those before)
-        const int s = tid / 4;
-        const Cand mine = s_sub[s];
-        int r = 0;
-#pragma unroll 4
-        for (int i = tid % 4; i < kSubsets; i += 4) {
-            const Cand o = s_sub[i];
-            r += better(o, mine) || (o.total == mine.total && o.tie == mine.tie && i < s);
-        }
-        r += __shfl_xor_sync(0xffffffffu, r, 1);
-        r += __shfl_xor_sync(0xffffffffu, r, 2);
-        if (r == K - 1 && tid % 4 == 0) s_bound = mine;
-    }
-    __syncthreads();
-    const Cand bound = s_bound;
-    const bool all = bound.total == 0ull;
-    const float bound_f = all ? -INFINITY : __double2float_rd(from_order64(bound.total));
+    const uint64_t bound = s_bound;  // (0: there are fewer)
     auto take = [&](const Cand &c) {
-        if (c.total == 0ull || (!all && better(bound, c))) return;
+        if (c.total == 0ull || c.total < bound) return;
         const int n = atomicAdd(&s_count, 1);
         if (n < kList) s_list[n] = c;
     };
-    // Visits every candidate of the thread that may reach the bound.
+    // Visits every candidate of the thread.
     auto visit = [&](auto f) {
         for (int i = tid; i < W * S * K; i += kMergeThreads) {
             const int w = i / (S * K);
             if (!s_open[w]) continue;
-            const uint64_t key = keys[i];
-            if (key == 0ull) continue;
-            if (!all) {  // ruled out in fp32: the sums round twice, the offset once
-                const float d = key_value(key) - s_maxf[w], o = s_offf[w];
-                if (d + o + 4e-7f * (fabsf(d) + fabsf(o)) < bound_f) continue;
-            }
-            f(cand(w, key));
+            const uint64_t key = i == tid ? key0 : i == tid + kMergeThreads ? key1 : keys[i];
+            if (key != 0ull) f(cand(w, key));
         }
         for (int w = tid; w < W; w += kMergeThreads) f(end_of(w));
     };
@@ -496,7 +570,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
         const int64_t o = static_cast<int64_t>(g) * K + r;
         const bool none = c.total == 0ull;
         const int w = none ? 0 : static_cast<int>(c.tie / a.vocab);
-        a.out_scores[o] = none ? -INFINITY : static_cast<float>(from_order64(c.total));
+        a.out_scores[o] = none ? -INFINITY : from_order(static_cast<uint32_t>(c.total >> 32));
         a.out_parents[o] = none ? -1 : g * W + w;
         a.out_tokens[o] = none ? -1 : static_cast<int32_t>(c.tie - static_cast<int64_t>(w) * a.vocab);
     };
@@ -532,25 +606,36 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
     }
 }
 
-// 16-byte chunks of a row that starts anywhere (one more than its bytes fill)
-int64_t most_chunks(int64_t vocab, bool fp32) { return fp32 ? (vocab + 3) / 4 + 1 : (vocab + 7) / 8 + 1; }
-
 }  // namespace
 
-// Slices a row: as many CTAs as fit the SMs at once, of a load for each lane at least.
+// Slices a row: those with which the SMs are done first, where a CTA's fixed cost is some
+// kFixed chunks' time and it takes three CTAs to keep an SM's loads in flight.
 int beam_slices(const fnpu_beam_desc *d) {
+    constexpr int64_t kSms = 152, kFixed = 512, kMost = 12;
     const int64_t rows = static_cast<int64_t>(d->num_groups) * d->num_beams;
-    const int64_t chunks = most_chunks(d->vocab, d->dtype == FNPU_LOGITS_FP32);
-    const int64_t fit = rows > 0 ? 6 * 152 / rows : 1, most = (chunks + kThreads - 1) / kThreads;
-    return static_cast<int>(fit < 1 ? 1 : fit < most ? fit : most);
+    const int64_t chunks = d->dtype == FNPU_LOGITS_FP32 ? (static_cast<int64_t>(d->vocab) + 3) / 4 : (static_cast<int64_t>(d->vocab) + 7) / 8;
+    const int64_t most = (chunks + kThreads - 1) / kThreads;  // (a chunk a thread at least)
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t n = 1; n <= kMost && rows > 0; ++n) {
+        const int64_t s = std::min(most, std::max<int64_t>(1, kSms * n / rows));
+        const int64_t ctas = (rows * s + kSms - 1) / kSms, cost = std::max<int64_t>(ctas, 3) * ((chunks + s - 1) / s + kFixed);
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return static_cast<int>(best);
 }
 
 int launch_beam_select(const BeamArgs &a, bool fp32, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t grid = static_cast<int64_t>(a.groups) * a.beams * a.slices;
-    auto kernel = fp32 ? beam_slice_kernel<float> : beam_slice_kernel<__nv_bfloat16>;
+    const bool aligned = (reinterpret_cast<uintptr_t>(a.logits) & 15u) == 0 &&
+                         (a.groups * a.beams == 1 || a.stride % (fp32 ? 4 : 8) == 0);
+    auto kernel = fp32 ? (aligned ? beam_slice_kernel<float, true> : beam_slice_kernel<float, false>)
+                       : (aligned ? beam_slice_kernel<__nv_bfloat16, true> : beam_slice_kernel<__nv_bfloat16, false>);
     FNPU_CUDA_TRY(launch_ex(kernel, static_cast<unsigned>(grid), kThreads, 0, st, true, nullptr, a));
-    const size_t smem = static_cast<size_t>(a.beams) * (2 * sizeof(double) + 2 * sizeof(float) + sizeof(int));
+    const size_t smem = static_cast<size_t>(a.beams) * (sizeof(Two) + sizeof(float) + sizeof(int));
     FNPU_CUDA_TRY(launch_ex(beam_merge_kernel, static_cast<unsigned>(a.groups), kMergeThreads, smem, st, true, nullptr, a));
     return FNPU_OK;
 }
