@@ -627,9 +627,16 @@ def _int32(x, name: str, *shape):
     """Address of a contiguous int32 tensor of that shape (None: any extent)."""
     if x.dtype is not (_dtypes or _types())[1]:
         raise TypeError(f"{name} is int32")
-    if x.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, x.shape)):
-        raise ValueError(f"expected {name} of shape {shape}, not {tuple(x.shape)}")
-    return _tptr(x)
+    have = x.shape
+    if have != shape and (len(have) != len(shape) or any(n is not None and n != m for n, m in zip(shape, have))):
+        raise ValueError(f"expected {name} of shape {shape}, not {tuple(have)}")
+    return x.data_ptr() if x.is_cuda and x.is_contiguous() else _dptr(x)
+
+
+@functools.lru_cache(maxsize=16)
+def _pointers(n: int):
+    """The type of an array of n addresses (making one takes longer than a launch)."""
+    return ctypes.c_void_p * n
 
 
 def window_decode(desc: AttnDesc, window: int, sinks: int, context_len, block_table, max_context_len: int, q, k_cache, v_cache, out,
@@ -765,10 +772,10 @@ def kv_copy_blocks(desc: AttnDesc, copies, k_pools, v_pools=None, kv_format: int
     n = len(k_pools)
     if v_pools is not None and len(v_pools) != n:
         raise ValueError("as many V pools as K pools")
-    kv = [_pool_addresses(pools, k, v) for k, v in zip(k_pools, v_pools if v_pools is not None else [None] * n)]
-    ptrs = ctypes.c_void_p * n
+    kv = [_pool_addresses(pools, k, v) for k, v in zip(k_pools, [None] * n if v_pools is None else v_pools)]
+    ptrs = _pointers(n)
     rc = (_lib or load()).fnpu_kv_copy_blocks(ctypes.byref(desc), int(kv_format), _int32(copies, "copies", None, 2), copies.shape[0],
-                                              ptrs(*(k for k, _ in kv)), None if v_pools is None else ptrs(*(v for _, v in kv)), n,
+                                              ptrs(*[k for k, _ in kv]), None if v_pools is None else ptrs(*[v for _, v in kv]), n,
                                               _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_kv_copy_blocks")

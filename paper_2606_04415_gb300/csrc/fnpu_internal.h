@@ -181,7 +181,8 @@ int beam_slices(const fnpu_beam_desc *d);
 int launch_beam_select(const BeamArgs &a, bool fp32, void *stream);
 
 // Page operations (pages.cu); see fnpu.h. Workspace pieces are laid out by the host.
-constexpr int32_t kPagesChunk = 8192;    // counts that a CTA looks through
+constexpr int32_t kPagesChunk = 2048;    // counts that a CTA looks through at a time
+constexpr int32_t kPagesMostChunks = 2048;
 constexpr int32_t kPagesMaxRows = 8192;
 struct PagesArgs {
     int32_t *table;             // rows x width (fork: the old one, read only)
@@ -190,12 +191,12 @@ struct PagesArgs {
     int32_t *refs;
     int32_t *new_table, *new_length, *copies, *stats, *remap;
     int64_t *slots;
-    // workspace: free or live blocks of each chunk; of each new row: length, last page if
+    // workspace: live blocks of each chunk; of each new row: length, last page if
     // partly filled (-1: none, -2: the row cannot grow), its count; of each block: rows
     // whose last page it is, the lowest of them (fork) or the free and moving blocks' places (compact)
     int32_t *chunk_count, *row_length, *row_tail, *row_refs, *block_a, *block_b;
     int *err;                   // the library-wide error flag
-    int32_t block_size, num_blocks, rows, width, new_rows, grow, max_copies, chunks;
+    int32_t block_size, num_blocks, rows, width, new_rows, grow, max_copies, chunks, chunk;
 };
 int launch_pages_free(const PagesArgs &a, int32_t *length, const uint8_t *ends, int32_t window, int32_t sinks, void *stream);
 int launch_pages_fork(const PagesArgs &a, void *stream);

@@ -4,7 +4,9 @@
 //
 // The tables are small (some MB at most), so what bounds these calls is the chain
 // of dependent steps: counts before free blocks, free blocks before their rows. Each
-// step is a kernel over all SMs and a dependent launch of the one before. Every
+// step is a kernel over all SMs and a dependent launch of the one before; where a step is a
+// matter of some rows and one chunk of counts, all steps are one kernel of one CTA, a
+// warp a row (launches of 3 steps take 8 us, 6 of them the host's). Every
 // result is independent of the order of the atomics: counts are sums, the lowest row
 // of a page a minimum, and the k-th block that is taken is the k-th free one by id, by a
 // prefix sum over chunks of counts that each CTA forms for itself.
@@ -16,8 +18,9 @@ namespace fnpu {
 namespace {
 
 constexpr int kRowThreads = 256;    // kernels over rows
-constexpr int kScanThreads = 512;   // kernels over chunks of counts
+constexpr int kScanThreads = 512;   // kernels over chunks of counts, and those of one CTA
 constexpr int kPer = kPagesChunk / kScanThreads;
+constexpr int64_t kSmallEntries = 16384;  // of the tables that one CTA goes through
 
 // States of a new row, where its last page is full or there is none to write to.
 constexpr int kRowFull = -1;   // goes on with new blocks
@@ -101,16 +104,50 @@ __global__ void __launch_bounds__(kRowThreads) pages_free_kernel(const PagesArgs
     }
 }
 
-// Fork, first step. CTAs 0 .. new_rows - 1: a new row's entries. The others: an old
+// The sum over a row's threads: a warp or the CTA.
+template <int kGroup>
+__device__ __forceinline__ int group_sum(int v, int *s) {
+    if constexpr (kGroup == 32) return __reduce_add_sync(0xffffffffu, v);
+    else return block_sum<kGroup>(v, s);
+}
+// The counts of a thread's kPer neighbours from `id0` on that are above zero, as bits.
+__device__ __forceinline__ uint32_t live_bits(const PagesArgs &a, int id0) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (id0 + i < a.num_blocks && a.refs[id0 + i] > 0) bits |= 1u << i;
+    return bits;
+}
+// How many of a chunk's counts are above zero.
+__device__ __forceinline__ int live_in_chunk(const PagesArgs &a, int chunk, int *s) {
+    int n = 0;
+    for (int i = 0; i < a.chunk; i += kScanThreads) {
+        const int id = chunk * a.chunk + i + static_cast<int>(threadIdx.x);
+        n += id < a.num_blocks && a.refs[id] > 0;
+    }
+    return block_sum<kScanThreads>(n, s);
+}
+// Of all chunks' live counts: the sum, and that of the chunks before `chunk`.
+__device__ __forceinline__ int live_before(const PagesArgs &a, int chunk, int *s, int *all) {
+    int before = 0, sum = 0;
+    for (int c = threadIdx.x; c < a.chunks; c += kScanThreads) {
+        const int n = a.chunk_count[c];
+        sum += n;
+        if (c < chunk) before += n;
+    }
+    *all = block_sum<kScanThreads>(sum, s);
+    return block_sum<kScanThreads>(before, s);
+}
+
+// Fork, first step. Units 0 .. new_rows - 1: a new row's entries. The others: an old
 // row's pages get as many holders more as rows continue it, less the one that it was
 // (nothing to do where one row does, the usual case late in a search).
-__global__ void __launch_bounds__(kRowThreads) fork_rows_kernel(const PagesArgs a) {
-    __shared__ int s_sum[kRowThreads / 32];
-    pdl_trigger();
-    pdl_wait();
-    const int tid = threadIdx.x, bs = a.block_size;
-    if (static_cast<int>(blockIdx.x) < a.new_rows) {
-        const int r = blockIdx.x;
+template <int kGroup>
+__device__ __forceinline__ void fork_row(const PagesArgs &a, int unit, int *s_sum) {
+    constexpr int kLoads = 4;  // entries in flight
+    const int tid = threadIdx.x % kGroup, bs = a.block_size;
+    if (unit < a.new_rows) {
+        const int r = unit;
         const int p = a.parents ? a.parents[r] : r;
         bool ok = p >= 0 && p < a.rows;
         if (p >= a.rows && tid == 0) atomicOr(a.err, 1);
@@ -119,20 +156,25 @@ __global__ void __launch_bounds__(kRowThreads) fork_rows_kernel(const PagesArgs 
         const int held = ok ? entries(n, bs) : 0;
         const int32_t *from = a.table + static_cast<int64_t>(ok ? p : 0) * a.width;
         int32_t *to = a.new_table + static_cast<int64_t>(r) * a.width;
-        for (int c = tid; c < a.width; c += kRowThreads) {
-            int e = c < held ? from[c] : -1;
-            if (e >= a.num_blocks) atomicOr(a.err, 1);
-            if (e < 0 || e >= a.num_blocks) e = -1;
-            to[c] = e;
+        int tail = kRowFull;
+        if (!ok) tail = kRowEmpty;
+        else if (a.grow > 0 && static_cast<int64_t>(n) + a.grow > static_cast<int64_t>(a.width) * bs) tail = kRowStuck;
+        else if (a.grow > 0 && n % bs != 0) {
+            const int e = from[n / bs];
+            tail = e >= 0 && e < a.num_blocks ? e : kRowStuck;
+        }
+        for (int c0 = tid; c0 < a.width; c0 += kLoads * kGroup) {
+            int e[kLoads];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) e[i] = c0 + i * kGroup < held ? from[c0 + i * kGroup] : -1;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if (c0 + i * kGroup >= a.width) break;
+                if (e[i] >= a.num_blocks) atomicOr(a.err, 1);
+                to[c0 + i * kGroup] = e[i] < 0 || e[i] >= a.num_blocks ? -1 : e[i];
+            }
         }
         if (tid == 0) {
-            int tail = kRowFull;
-            if (!ok) tail = kRowEmpty;
-            else if (a.grow > 0 && static_cast<int64_t>(n) + a.grow > static_cast<int64_t>(a.width) * bs) tail = kRowStuck;
-            else if (a.grow > 0 && n % bs != 0) {
-                const int e = from[n / bs];
-                tail = e >= 0 && e < a.num_blocks ? e : kRowStuck;
-            }
             a.row_length[r] = ok ? n : 0;
             a.row_tail[r] = tail;
             if (tail >= 0) {  // (the same for every row with this page)
@@ -142,7 +184,7 @@ __global__ void __launch_bounds__(kRowThreads) fork_rows_kernel(const PagesArgs 
         }
         return;
     }
-    const int p = static_cast<int>(blockIdx.x) - a.new_rows;
+    const int p = unit - a.new_rows;
     const int n = a.length[p];
     if (!length_ok(a, n)) {
         if (tid == 0) atomicOr(a.err, 1);
@@ -151,39 +193,27 @@ __global__ void __launch_bounds__(kRowThreads) fork_rows_kernel(const PagesArgs 
     int next = a.new_rows > 0 ? 1 : 0;  // (no new rows: nobody continues any)
     if (a.parents) {
         int mine = 0;
-        for (int r = tid; r < a.new_rows; r += kRowThreads) mine += a.parents[r] == p;
-        next = block_sum<kRowThreads>(mine, s_sum);
+        for (int r = tid; r < a.new_rows; r += kGroup) mine += a.parents[r] == p;
+        next = group_sum<kGroup>(mine, s_sum);
     }
     const int32_t *row = a.table + static_cast<int64_t>(p) * a.width;
-    for (int c = tid; c < entries(n, bs); c += kRowThreads) {
-        const int e = row[c];
-        if (e >= a.num_blocks) atomicOr(a.err, 1);
-        if (e < 0 || e >= a.num_blocks || next == 1) continue;
-        if (next > 1) atomicAdd(a.refs + e, next - 1);
-        else drop(a, e);
+    const int held = entries(n, bs);
+    for (int c0 = tid; c0 < held; c0 += kLoads * kGroup) {
+        int e[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) e[i] = c0 + i * kGroup < held ? row[c0 + i * kGroup] : -1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (e[i] >= a.num_blocks) atomicOr(a.err, 1);
+            if (e[i] < 0 || e[i] >= a.num_blocks || next == 1) continue;
+            if (next > 1) atomicAdd(a.refs + e[i], next - 1);
+            else drop(a, e[i]);
+        }
     }
 }
 
-// Second step: the free blocks of each chunk, and the rows of each last page.
-__global__ void __launch_bounds__(kScanThreads) fork_count_kernel(const PagesArgs a) {
-    __shared__ int s_sum[kScanThreads / 32];
-    pdl_trigger();
-    pdl_wait();
-    const int tid = threadIdx.x;
-    if (static_cast<int>(blockIdx.x) < a.chunks) {
-        int n = 0;
-        const int c0 = blockIdx.x * kPagesChunk;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int id = c0 + i * kScanThreads + tid;
-            n += id < a.num_blocks && a.refs[id] <= 0;
-        }
-        n = block_sum<kScanThreads>(n, s_sum);
-        if (tid == 0) a.chunk_count[blockIdx.x] = n;
-        return;
-    }
-    const int r = (static_cast<int>(blockIdx.x) - a.chunks) * kScanThreads + tid;
-    if (r >= a.new_rows) return;
+// Second step: the rows of each last page (and the live blocks of each chunk).
+__device__ __forceinline__ void fork_tail(const PagesArgs &a, int r) {
     const int tail = a.row_tail[r];
     if (tail < 0) return;
     atomicAdd(a.block_a + tail, 1);
@@ -191,38 +221,36 @@ __global__ void __launch_bounds__(kScanThreads) fork_count_kernel(const PagesArg
     a.row_refs[r] = a.refs[tail];
 }
 
-// Third step: a CTA a chunk. Each forms the rows' needs and their prefix sums, and
-// hands its own free blocks to the rows whose turn they are; CTA 0 does what is
-// left of every row.
-__global__ void __launch_bounds__(kScanThreads) fork_take_kernel(const PagesArgs a) {
-    extern __shared__ int s_off[];  // [new_rows + 1]: blocks that the rows before need * 2 + (it copies)
-    __shared__ int s_sum[kScanThreads / 32];
-    pdl_trigger();
-    pdl_wait();
+// Third step, a chunk each CTA. All form the rows' needs and their prefix sums; a CTA
+// hands its own free blocks to the rows whose turn they are, and that of chunk 0 does what
+// is left of every row.
+struct ForkShared {
+    int sum[kScanThreads / 32];
+    int free[kPagesChunk];
+};
+__device__ __forceinline__ void fork_take(const PagesArgs &a, int chunk, ForkShared *s, int *s_off) {
     const int tid = threadIdx.x, bs = a.block_size, R = a.new_rows;
-    int before = 0, all = 0;
-    for (int c = tid; c < a.chunks; c += kScanThreads) {
-        const int n = a.chunk_count[c];
-        all += n;
-        if (c < static_cast<int>(blockIdx.x)) before += n;
-    }
-    before = block_sum<kScanThreads>(before, s_sum);
-    const int free_blocks = block_sum<kScanThreads>(all, s_sum);
-    auto need_of = [&](int r, bool *copy) {
+    const int first = chunk * a.chunk;
+    uint32_t live = live_bits(a, first + tid * kPer);
+    // s_off[r]: blocks that row r needs, then that the rows before it do, * 2 + (it copies)
+    for (int r = tid; r < R; r += kScanThreads) {
         const int tail = a.row_tail[r], n = a.row_length[r];
-        *copy = tail >= 0 && (a.block_b[tail] != r || a.row_refs[r] > a.block_a[tail]);
-        return tail < kRowFull ? 0 : (*copy ? 1 : 0) + entries(n + a.grow, bs) - entries(n, bs);
-    };
+        const bool copy = tail >= 0 && (a.block_b[tail] != r || a.row_refs[r] > a.block_a[tail]);
+        s_off[r] = tail < kRowFull ? 0 : 2 * ((copy ? 1 : 0) + entries(n + a.grow, bs) - entries(n, bs)) + (copy ? 1 : 0);
+    }
+    int live_blocks;
+    const int live_chunks = live_before(a, chunk, s->sum, &live_blocks);  // (and s_off is written)
+    const int free_blocks = a.num_blocks - live_blocks;
+    int before = first - live_chunks;  // free ones of the chunks before
     const int per = (R + kScanThreads - 1) / kScanThreads;
     int mine = 0;
-    bool copy;
-    for (int r = tid * per; r < min(R, (tid + 1) * per); ++r) mine += need_of(r, &copy);
+    for (int r = tid * per; r < min(R, (tid + 1) * per); ++r) mine += s_off[r] >> 1;
     int needed;
-    int off = block_before<kScanThreads>(mine, s_sum, &needed);
+    int off = block_before<kScanThreads>(mine, s->sum, &needed);
     for (int r = tid * per; r < min(R, (tid + 1) * per); ++r) {
-        const int n = need_of(r, &copy);
-        s_off[r] = 2 * off + (copy ? 1 : 0);
-        off += n;
+        const int v = s_off[r];
+        s_off[r] = 2 * off + (v & 1);
+        off += v >> 1;
     }
     if (tid == 0) s_off[R] = 2 * needed;
     __syncthreads();
@@ -230,18 +258,20 @@ __global__ void __launch_bounds__(kScanThreads) fork_take_kernel(const PagesArgs
         const int o = s_off[r] >> 1, e = s_off[r + 1] >> 1;
         return e == o || e <= free_blocks;
     };
-    if (before < needed) {
-        // the chunk's free blocks in order, `kPer` neighbours a thread
-        const int id0 = blockIdx.x * kPagesChunk + tid * kPer;
-        uint32_t is_free = 0;
+    for (int c = 0; c < a.chunk && before < needed; c += kPagesChunk) {
+        // free blocks in order, kPer neighbours a thread
+        const int id0 = first + c + tid * kPer;
+        if (c > 0) live = live_bits(a, id0);
+        uint32_t is_free = ~live & ((1u << kPer) - 1);
+        if (id0 + kPer > a.num_blocks) is_free &= id0 < a.num_blocks ? (1u << (a.num_blocks - id0)) - 1 : 0u;
+        int here;
+        int f = block_before<kScanThreads>(__popc(is_free), s->sum, &here);  // (and the last round's ids are read)
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
-            if (id0 + i < a.num_blocks && a.refs[id0 + i] <= 0) is_free |= 1u << i;
-        int unused;
-        int f = before + block_before<kScanThreads>(__popc(is_free), s_sum, &unused);  // (and all have read before any writes)
-        for (int i = 0; i < kPer && f < needed; ++i) {
-            if (!(is_free >> i & 1u)) continue;
-            const int id = id0 + i, turn = f++;
+            if (is_free >> i & 1u) s->free[f++] = id0 + i;
+        __syncthreads();
+        for (int j = tid; j < min(here, needed - before); j += kScanThreads) {
+            const int id = s->free[j], turn = before + j;
             int lo = 0, hi = R - 1;  // the last row whose blocks begin at `turn` or before
             while (lo < hi) {
                 const int mid = (lo + hi + 1) / 2;
@@ -265,8 +295,9 @@ __global__ void __launch_bounds__(kScanThreads) fork_take_kernel(const PagesArgs
             for (int g = max(0, col * bs - n); g < g1; ++g)
                 a.slots[static_cast<int64_t>(r) * a.grow + g] = static_cast<int64_t>(id) * bs + (n + g) % bs;
         }
+        before += here;
     }
-    if (blockIdx.x != 0) return;
+    if (chunk != 0) return;
     int taken = 0, unserved = 0, copied = 0;
     for (int r = tid; r < R; r += kScanThreads) {
         const int tail = a.row_tail[r], n = a.row_length[r];
@@ -285,9 +316,9 @@ __global__ void __launch_bounds__(kScanThreads) fork_take_kernel(const PagesArgs
         unserved += !ok && tail != kRowEmpty;
         copied += ok && copies;
     }
-    taken = block_sum<kScanThreads>(taken, s_sum);
-    unserved = block_sum<kScanThreads>(unserved, s_sum);
-    copied = block_sum<kScanThreads>(copied, s_sum);
+    taken = block_sum<kScanThreads>(taken, s->sum);
+    unserved = block_sum<kScanThreads>(unserved, s->sum);
+    copied = block_sum<kScanThreads>(copied, s->sum);
     if (tid == 0) {
         a.stats[0] = free_blocks - taken;
         a.stats[1] = taken;
@@ -296,108 +327,167 @@ __global__ void __launch_bounds__(kScanThreads) fork_take_kernel(const PagesArgs
     }
 }
 
-// Compaction, first step: the live blocks of each chunk.
-__global__ void __launch_bounds__(kScanThreads) compact_count_kernel(const PagesArgs a) {
+__global__ void __launch_bounds__(kRowThreads) fork_rows_kernel(const PagesArgs a) {
+    __shared__ int s_sum[kRowThreads / 32];
+    pdl_trigger();
+    pdl_wait();
+    fork_row<kRowThreads>(a, blockIdx.x, s_sum);
+}
+__global__ void __launch_bounds__(kScanThreads) fork_count_kernel(const PagesArgs a) {
     __shared__ int s_sum[kScanThreads / 32];
     pdl_trigger();
     pdl_wait();
-    int n = 0;
-    const int c0 = blockIdx.x * kPagesChunk;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int id = c0 + i * kScanThreads + static_cast<int>(threadIdx.x);
-        n += id < a.num_blocks && a.refs[id] > 0;
+    if (static_cast<int>(blockIdx.x) < a.chunks) {
+        const int n = live_in_chunk(a, blockIdx.x, s_sum);
+        if (threadIdx.x == 0) a.chunk_count[blockIdx.x] = n;
+        return;
     }
-    n = block_sum<kScanThreads>(n, s_sum);
-    if (threadIdx.x == 0) a.chunk_count[blockIdx.x] = n;
+    const int r = (static_cast<int>(blockIdx.x) - a.chunks) * kScanThreads + static_cast<int>(threadIdx.x);
+    if (r < a.new_rows) fork_tail(a, r);
+}
+__global__ void __launch_bounds__(kScanThreads) fork_take_kernel(const PagesArgs a) {
+    extern __shared__ int s_off[];  // [new_rows + 1]
+    __shared__ ForkShared s;
+    pdl_trigger();
+    pdl_wait();
+    fork_take(a, blockIdx.x, &s, s_off);
+}
+// All three steps, of one chunk.
+__global__ void __launch_bounds__(kScanThreads) fork_small_kernel(const PagesArgs a) {
+    extern __shared__ int s_off[];
+    __shared__ ForkShared s;
+    pdl_trigger();
+    pdl_wait();
+    for (int u = threadIdx.x / 32; u < a.new_rows + a.rows; u += kScanThreads / 32) fork_row<32>(a, u, nullptr);
+    __syncthreads();
+    for (int r = threadIdx.x; r < a.new_rows; r += kScanThreads) fork_tail(a, r);
+    const int n = live_in_chunk(a, 0, s.sum);
+    if (threadIdx.x == 0) a.chunk_count[0] = n;
+    __syncthreads();
+    fork_take(a, 0, &s, s_off);
 }
 
-// Second step: with `live` live blocks, the i-th free id below it (block_a[i]) and, of
-// each live id from there on, how many are above it (block_b[id]: its turn).
-__global__ void __launch_bounds__(kScanThreads) compact_rank_kernel(const PagesArgs a) {
-    __shared__ int s_sum[kScanThreads / 32];
-    pdl_trigger();
-    pdl_wait();
+// Compaction, second step (after the live blocks of each chunk): with `live` live
+// blocks, the i-th free id below it (block_a[i]) and, of each live id from there on, how
+// many are above it (block_b[id]: its turn).
+__device__ __forceinline__ void compact_rank(const PagesArgs &a, int chunk, int *s_sum) {
     const int tid = threadIdx.x;
-    int before = 0, live = 0;
-    for (int c = tid; c < a.chunks; c += kScanThreads) {
-        const int n = a.chunk_count[c];
-        live += n;
-        if (c < static_cast<int>(blockIdx.x)) before += n;
-    }
-    before = block_sum<kScanThreads>(before, s_sum);
-    live = block_sum<kScanThreads>(live, s_sum);
-    const int id0 = blockIdx.x * kPagesChunk + tid * kPer;
-    uint32_t is_live = 0;
+    int live;
+    int base = live_before(a, chunk, s_sum, &live);
+    for (int c = 0; c < a.chunk; c += kPagesChunk) {
+        const int id0 = chunk * a.chunk + c + tid * kPer;
+        const uint32_t is_live = live_bits(a, id0);
+        int here;
+        int before = base + block_before<kScanThreads>(__popc(is_live), s_sum, &here);
+        base += here;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-        if (id0 + i < a.num_blocks && a.refs[id0 + i] > 0) is_live |= 1u << i;
-    int unused;
-    before += block_before<kScanThreads>(__popc(is_live), s_sum, &unused);
-    for (int i = 0; i < kPer && id0 + i < a.num_blocks; ++i) {
-        const int id = id0 + i;
-        const bool is = is_live >> i & 1u;
-        if (id == live) a.row_length[1] = live - before;  // as many are free below it as are live from it on
-        if (id < live) {
-            a.remap[id] = is ? id : -1;
-            if (!is) a.block_a[id - before] = id;
-        } else {  // (INT_MAX: no page; an entry that names it has no count)
-            a.block_b[id] = is ? live - 1 - before : INT_MAX;
+        for (int i = 0; i < kPer; ++i) {
+            const int id = id0 + i;
+            if (id >= a.num_blocks) break;
+            const bool is = is_live >> i & 1u;
+            if (id == live) a.row_length[1] = live - before;  // as many are free below it as are live from it on
+            if (id < live) {
+                a.remap[id] = is ? id : -1;
+                if (!is) a.block_a[id - before] = id;
+            } else {  // (INT_MAX: no page; an entry that names it has no count)
+                a.block_b[id] = is ? live - 1 - before : INT_MAX;
+            }
+            before += is;
         }
-        before += is;
     }
-    if (blockIdx.x == 0 && tid == 0) {
+    if (chunk == 0 && tid == 0) {
         a.row_length[0] = live;
         if (live >= a.num_blocks) a.row_length[1] = 0;
     }
 }
 
-// Third step. CTAs 0 .. chunks - 1: the moving blocks' pairs, counts and new places, and
-// the unused end of the list; the others: rows of the table.
-__global__ void __launch_bounds__(kScanThreads) compact_move_kernel(const PagesArgs a) {
-    pdl_trigger();
-    pdl_wait();
-    const int tid = threadIdx.x, live = a.row_length[0], moves = min(a.row_length[1], a.max_copies);
-    if (static_cast<int>(blockIdx.x) < a.chunks) {
+// Third step: the moving blocks' pairs, counts and new places, and the unused end of
+// the list;
+__device__ __forceinline__ void compact_move(const PagesArgs &a, int chunk, int live, int moves) {
+    const int tid = threadIdx.x;
+    for (int c = 0; c < a.chunk; c += kPagesChunk) {
+        int id[kPer];
+        int turn[kPer];
+#pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int id = blockIdx.x * kPagesChunk + i * kScanThreads + tid;
-            if (id >= a.num_blocks) break;
-            if (id < live) continue;
-            const int64_t turn = a.block_b[id];
-            if (turn < moves) {
-                const int to = a.block_a[turn];
-                a.remap[id] = to;
-                a.refs[to] = a.refs[id];
-                a.refs[id] = 0;
-                a.copies[2 * turn] = id;
-                a.copies[2 * turn + 1] = to;
+            id[i] = chunk * a.chunk + c + i * kScanThreads + tid;
+            turn[i] = id[i] >= live && id[i] < a.num_blocks ? a.block_b[id[i]] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (turn[i] < 0) continue;
+            if (turn[i] < moves) {
+                const int to = a.block_a[turn[i]];
+                a.remap[id[i]] = to;
+                a.refs[to] = a.refs[id[i]];
+                a.refs[id[i]] = 0;
+                a.copies[2ll * turn[i]] = id[i];
+                a.copies[2ll * turn[i] + 1] = to;
             } else {
-                a.remap[id] = turn == INT_MAX ? -1 : id;
+                a.remap[id[i]] = turn[i] == INT_MAX ? -1 : id[i];
             }
         }
-        for (int64_t i = moves + static_cast<int64_t>(blockIdx.x) * kScanThreads + tid; i < a.max_copies;
-             i += static_cast<int64_t>(a.chunks) * kScanThreads)
-            a.copies[2 * i] = a.copies[2 * i + 1] = -1;
-        if (blockIdx.x == 0 && tid == 0) {
-            a.stats[0] = live;
-            a.stats[1] = moves;
-        }
-        return;
     }
-    const int r = static_cast<int>(blockIdx.x) - a.chunks;
+    for (int64_t i = moves + static_cast<int64_t>(chunk) * kScanThreads + tid; i < a.max_copies;
+         i += static_cast<int64_t>(a.chunks) * kScanThreads)
+        a.copies[2 * i] = a.copies[2 * i + 1] = -1;
+    if (chunk == 0 && tid == 0) {
+        a.stats[0] = live;
+        a.stats[1] = moves;
+    }
+}
+// and a row of the table.
+template <int kGroup>
+__device__ __forceinline__ void compact_row(const PagesArgs &a, int r, int live, int moves) {
+    const int tid = threadIdx.x % kGroup;
     const int n = a.length[r];
     if (!length_ok(a, n)) {
         if (tid == 0) atomicOr(a.err, 1);
         return;
     }
     int32_t *row = a.table + static_cast<int64_t>(r) * a.width;
-    for (int c = tid; c < entries(n, a.block_size); c += kScanThreads) {
+    for (int c = tid; c < entries(n, a.block_size); c += kGroup) {
         const int e = row[c];
         if (e < live) continue;
         const int turn = e < a.num_blocks ? a.block_b[e] : INT_MAX;
         if (turn == INT_MAX) atomicOr(a.err, 1);
         else if (turn < moves) row[c] = a.block_a[turn];
     }
+}
+
+__global__ void __launch_bounds__(kScanThreads) compact_count_kernel(const PagesArgs a) {
+    __shared__ int s_sum[kScanThreads / 32];
+    pdl_trigger();
+    pdl_wait();
+    const int n = live_in_chunk(a, blockIdx.x, s_sum);
+    if (threadIdx.x == 0) a.chunk_count[blockIdx.x] = n;
+}
+__global__ void __launch_bounds__(kScanThreads) compact_rank_kernel(const PagesArgs a) {
+    __shared__ int s_sum[kScanThreads / 32];
+    pdl_trigger();
+    pdl_wait();
+    compact_rank(a, blockIdx.x, s_sum);
+}
+__global__ void __launch_bounds__(kScanThreads) compact_move_kernel(const PagesArgs a) {
+    pdl_trigger();
+    pdl_wait();
+    const int live = a.row_length[0], moves = min(a.row_length[1], a.max_copies);
+    if (static_cast<int>(blockIdx.x) < a.chunks) compact_move(a, blockIdx.x, live, moves);
+    else compact_row<kScanThreads>(a, static_cast<int>(blockIdx.x) - a.chunks, live, moves);
+}
+// All three steps, of one chunk.
+__global__ void __launch_bounds__(kScanThreads) compact_small_kernel(const PagesArgs a) {
+    __shared__ int s_sum[kScanThreads / 32];
+    pdl_trigger();
+    pdl_wait();
+    const int n = live_in_chunk(a, 0, s_sum);
+    if (threadIdx.x == 0) a.chunk_count[0] = n;
+    __syncthreads();
+    compact_rank(a, 0, s_sum);
+    __syncthreads();
+    const int live = a.row_length[0], moves = min(a.row_length[1], a.max_copies);
+    compact_move(a, 0, live, moves);
+    for (int r = threadIdx.x / 32; r < a.rows; r += kScanThreads / 32) compact_row<32>(a, r, live, moves);
 }
 
 // Copies of blocks in every pool. A unit is one pool's part of a pair, up to 16 KB; the
@@ -458,17 +548,26 @@ int launch_pages_free(const PagesArgs &a, int32_t *length, const uint8_t *ends, 
 
 int launch_pages_fork(const PagesArgs &a, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (a.new_rows + a.rows > 0)
-        FNPU_CUDA_TRY(launch_ex(fork_rows_kernel, static_cast<unsigned>(a.new_rows + a.rows), kRowThreads, 0, st, true, nullptr, a));
+    const size_t smem = sizeof(int) * (a.new_rows + 1);
+    const int64_t rows = static_cast<int64_t>(a.new_rows) + a.rows;
+    if (a.chunks == 1 && a.chunk == kPagesChunk && rows <= 4 * (kScanThreads / 32) && rows * a.width <= kSmallEntries) {
+        FNPU_CUDA_TRY(launch_ex(fork_small_kernel, 1u, kScanThreads, smem, st, true, nullptr, a));
+        return FNPU_OK;
+    }
+    if (rows > 0) FNPU_CUDA_TRY(launch_ex(fork_rows_kernel, static_cast<unsigned>(rows), kRowThreads, 0, st, true, nullptr, a));
     const int row_ctas = (a.new_rows + kScanThreads - 1) / kScanThreads;
     FNPU_CUDA_TRY(launch_ex(fork_count_kernel, static_cast<unsigned>(a.chunks + row_ctas), kScanThreads, 0, st, true, nullptr, a));
-    FNPU_CUDA_TRY(launch_ex(fork_take_kernel, static_cast<unsigned>(a.chunks), kScanThreads, sizeof(int) * (a.new_rows + 1), st, true,
-                            nullptr, a));
+    FNPU_CUDA_TRY(launch_ex(fork_take_kernel, static_cast<unsigned>(a.chunks), kScanThreads, smem, st, true, nullptr, a));
     return FNPU_OK;
 }
 
 int launch_pages_compact(const PagesArgs &a, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a.chunks == 1 && a.chunk == kPagesChunk && a.rows <= 4 * (kScanThreads / 32) &&
+        static_cast<int64_t>(a.rows) * a.width <= kSmallEntries) {
+        FNPU_CUDA_TRY(launch_ex(compact_small_kernel, 1u, kScanThreads, 0, st, true, nullptr, a));
+        return FNPU_OK;
+    }
     FNPU_CUDA_TRY(launch_ex(compact_count_kernel, static_cast<unsigned>(a.chunks), kScanThreads, 0, st, true, nullptr, a));
     FNPU_CUDA_TRY(launch_ex(compact_rank_kernel, static_cast<unsigned>(a.chunks), kScanThreads, 0, st, true, nullptr, a));
     FNPU_CUDA_TRY(launch_ex(compact_move_kernel, static_cast<unsigned>(a.chunks + a.rows), kScanThreads, 0, st, true, nullptr, a));

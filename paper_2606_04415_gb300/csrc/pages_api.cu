@@ -13,7 +13,13 @@ int pages_ok(const fnpu_pages_desc *d, int64_t rows, int64_t width) {
     return width * d->block_size > INT32_MAX - (1 << 17) ? FNPU_EUNSUPPORTED : FNPU_OK;
 }
 
-int32_t chunks_of(const fnpu_pages_desc *d) { return (d->num_blocks + kPagesChunk - 1) / kPagesChunk; }
+// Blocks of a CTA's chunk: kPagesChunk, or as many of them as leave kPagesMostChunks chunks
+// (each CTA adds up all chunks' counts).
+int32_t chunk_of(const fnpu_pages_desc *d) {
+    constexpr int32_t kAll = kPagesChunk * kPagesMostChunks;
+    return kPagesChunk * ((d->num_blocks - 1) / kAll + 1);
+}
+int32_t chunks_of(const fnpu_pages_desc *d) { return (d->num_blocks - 1) / chunk_of(d) + 1; }
 
 // Workspace, in int32: chunk counts, three values a row (two at least), two a block.
 int64_t words(const fnpu_pages_desc *d, int32_t rows) {
@@ -22,6 +28,7 @@ int64_t words(const fnpu_pages_desc *d, int32_t rows) {
 
 void place(const fnpu_pages_desc *d, int32_t rows, void *workspace, PagesArgs *a) {
     a->chunks = chunks_of(d);
+    a->chunk = chunk_of(d);
     a->block_size = d->block_size;
     a->num_blocks = d->num_blocks;
     a->chunk_count = static_cast<int32_t *>(workspace);

@@ -92,6 +92,24 @@ def test_large_values_in_few_threads(dtype, period):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("g,b,v,off", [(1, 4, 50257, 0), (3, 5, 5003, 3), (40, 8, 9999, 1), (2, 3, 13, 5)])
+def test_equal_beams_tie_wherever_their_rows_start(g, b, v, off, dtype):
+    """Beams of equal logits and scores have equal totals: the lowest beam's come first, token by token."""
+    x, _ = _logits(31, 1, 1, v, dtype)
+    buf = torch.zeros(g * b * v + off, dtype=dtype, device="cuda")
+    rows = buf[off:].view(g, b, v)
+    rows.copy_(x.expand(g, b, v))
+    s = torch.full((g, b), -1.5, device="cuda")
+    k = min(12, b * v)
+    got = _run(rows, s, k)
+    flat = x[0, 0].tolist()
+    best = sorted(range(v), key=lambda t: (-flat[t], t))[:k]
+    want = sorted(((w, t) for t in best for w in range(b)), key=lambda p: (-flat[p[1]], p))  # (equal logits: beams before tokens)
+    for i in range(g):
+        assert list(zip((got[1][i] - i * b).tolist(), got[2][i].tolist())) == want[:k]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("off,stride", [(0, 5003), (1, 5003), (3, 6007), (5, 8192)])
 def test_rows_that_start_anywhere(dtype, off, stride):
     """Slices of a larger buffer whose other values are NaN."""

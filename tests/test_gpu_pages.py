@@ -208,6 +208,45 @@ def test_compact_of_full_and_empty_pools():
         assert remap.tolist() == (list(range(9000)) if refs[0] else [-1] * 9000)
 
 
+@pytest.mark.parametrize("blocks", [2048, 2049, 2048 * 2048 + 4097])
+def test_pools_of_any_size(blocks):
+    """Pools of one chunk of counts, of two, and of so many that a chunk is longer."""
+    import paper_2606_04415_gb300 as fnpu
+    rng = np.random.default_rng([47, blocks])
+    refs = (rng.random(blocks) < 0.5).astype(np.int32)
+    refs[:100], refs[-50:] = 1, 1
+    live, d, rows = np.flatnonzero(refs), fnpu.make_pages(1, blocks), 40
+    table = np.full((rows, 600), -1, np.int32)
+    table[:, :3] = live[:rows * 3].reshape(rows, 3)
+    table[0, 2], table[1, 1] = live[-1], live[-2]
+    n, ws = np.full(rows, 3, np.int32), torch.full((fnpu.pages_workspace(d, rows),), 0xFF, dtype=torch.uint8, device="cuda")
+    # full pages only: each row takes the next 7 free ids (the pool has some at both ends of every chunk)
+    r, got = _dev(refs, np.int32), [torch.full(s, 77, dtype=t, device="cuda") for s, t in
+                                    (((rows, 600), torch.int32), ((rows,), torch.int32), ((rows, 7), torch.int64), ((rows, 2), torch.int32), ((4,), torch.int32))]
+    fnpu.pages_fork(d, _dev(table, np.int32), _dev(n, np.int32), r, *got, ws)
+    free = np.flatnonzero(refs == 0)
+    taken = free[:rows * 7].reshape(rows, 7)
+    want = refs.copy()
+    want[taken] = 1
+    assert np.array_equal(got[0].cpu().numpy()[:, 3:10], taken) and np.array_equal(got[2].cpu().numpy(), taken)
+    assert got[4].tolist() == [len(free) - rows * 7, rows * 7, 0, 0] and np.array_equal(r.cpu().numpy(), want)
+    # compaction: the i-th highest live page to the i-th lowest free place
+    refs[live] = rng.integers(1, 9, len(live))
+    r, moves = _dev(refs, np.int32), int((live >= len(live)).sum())
+    copies, remap, stats = (torch.full(s, 77, dtype=torch.int32, device="cuda") for s in ((moves + 3, 2), (blocks,), (2,)))
+    t = _dev(table, np.int32)
+    fnpu.pages_compact(d, t, _dev(n, np.int32), r, copies, remap, stats, ws)
+    src, dst = live[live >= len(live)][::-1], free[free < len(live)]
+    where = np.where(refs > 0, np.arange(blocks), -1)
+    where[src] = dst
+    assert stats.tolist() == [len(live), moves] and np.array_equal(copies.cpu().numpy()[:moves], np.stack([src, dst], 1))
+    assert copies[moves:].eq(-1).all() and np.array_equal(remap.cpu().numpy(), where)
+    want = np.zeros_like(refs)
+    want[where[live]] = refs[live]
+    assert np.array_equal(r.cpu().numpy(), want)
+    assert np.array_equal(t.cpu().numpy()[:, :3], where[table[:, :3]]) and fnpu.check() == 0
+
+
 # ---------------------------------------------------------------- copies
 
 def _pools(fnpu, kind, layers, blocks=37):
