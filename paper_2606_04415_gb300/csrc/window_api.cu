@@ -57,9 +57,16 @@ int window_split(const fnpu_attn_desc *d, int32_t window, int32_t sinks, int32_t
     int64_t sk = split_keys;
     constexpr int64_t kSms = 152;
     if (sk == 0) {
-        sk = 512;
-        if (items(128) <= 2 * kSms) sk = 128;
-        else if (items(256) <= 2 * kSms || items(512) > 3 * kSms) sk = 256;
+        // the shortest whose items fit the device at once (three CTAs an SM); where none does, 256.
+        // us a call, kv heads x rows, window: 4 x 4, 1024: 64 keys 11.1, 128 13.2; 4 x 64, 1024:
+        // 128 keys 36.5, 192 29.8, 256 31.2; 8 x 16, 1024: 64 18.3, 128 14.9; 8 x 24, 4096: 256
+        // 71.1, 512 67.8; 4 x 64, 4096 (none fits): 256 99.5, 512 110.3
+        sk = 256;
+        for (int64_t k : {64, 128, 192, 256, 512})
+            if (items(k) <= 3 * kSms) {
+                sk = k;
+                break;
+            }
     }
     sk = std::max<int64_t>(sk, (keys + 256 * 64 - 1) / (256 * 64) * 64);  // at most 256 splits of a sequence
     out->keys = static_cast<int32_t>(std::min<int64_t>(sk, 1 << 30));
