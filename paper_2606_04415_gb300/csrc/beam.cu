@@ -9,11 +9,11 @@
 //     need no normalisation. A value costs a conversion, half a paired multiply-add,
 //     an exponential and half a paired addition, and bf16 maxima go in pairs; a
 //     reference that all of a warp's sums share moves only when a tile has a value 2^8
-//     above it. Candidates are chunks of 16 bytes whose maximum reaches a bound: the
-//     K-th largest of the maxima of 64 subsets of what the CTA has seen, which at least
-//     K values reach. It is formed anew after 1, 4, 16, .. tiles, so only some
-//     K log n chunks are noted (4 bytes each, their values read again at the
-//     end); a warp's list that fills up is cut to the chunks of its best K values.
+//     above it. Each thread keeps its tiles' maxima in shared memory. Once the slice is
+//     read, the K-th largest of the maxima of 64 subsets of it is a bound that K
+//     values reach; only the tiles that reach it, some K of them, are read again (from
+//     L2) for their values. (A bound that follows the reading, with a list of chunks
+//     that reach it, costs a fifth more: 512 rows of 151936, 43 us against XX.)
 //     Slices, chunks and the order of the sums go by token numbers, wherever a row
 //     starts in memory: beams with equal logits have equal sums to the last bit.
 //   * A CTA of the second takes a group: the rows' log-sum-exps from their slices',
@@ -36,7 +36,8 @@ constexpr int kLoads = 4;           // 16-byte loads of a lane in a tile
 constexpr int kMergeThreads = 256;  // of the second
 constexpr int kSubsets = 64;        // (num_select is at most as many)
 constexpr int kMergeSubsets = 128;  // (two threads count for each)
-constexpr int kWarpList = 512;      // chunks that a warp notes
+constexpr int kTops = 32;           // tiles' maxima that a thread keeps (of several tiles each where there are more)
+constexpr int kHits = 256;          // of them that reach the bound
 constexpr int kList = 512;          // candidates of a CTA
 
 // Order-preserving bits of a float, and back.
@@ -117,9 +118,14 @@ template <int kBits>
 __device__ __forceinline__ uint32_t kth_of_64(uint32_t a, uint32_t b, int K) {
     uint32_t top = 0u;
 #pragma unroll
-    for (int i = 31; i >= 32 - kBits; --i) {
-        const uint32_t t = top | 1u << i;
-        if (__popc(__ballot_sync(0xffffffffu, a >= t)) + __popc(__ballot_sync(0xffffffffu, b >= t)) >= K) top = t;
+    for (int i = 30; i >= 32 - kBits; i -= 2) {  // two bits a step: the three thresholds' votes are independent
+        uint32_t next = top;
+#pragma unroll
+        for (uint32_t j = 1; j < 4; ++j) {
+            const uint32_t t = top | j << i;
+            if (__popc(__ballot_sync(0xffffffffu, a >= t)) + __popc(__ballot_sync(0xffffffffu, b >= t)) >= K) next = t;
+        }
+        top = next;
     }
     // (of a negative value the bits below are ones)
     return kBits < 32 && !(top >> 31) ? top | 0xFFFFu : top;
@@ -178,37 +184,6 @@ struct Row {
     }
 };
 
-// Cuts a warp's list of n chunks (K or more, each with a candidate) to those of its best
-// K values, in place; returns the last of these and how many chunks there are.
-struct Cut {
-    uint64_t last;
-    int len;
-};
-template <typename T, bool kAligned>
-__device__ __noinline__ Cut cut_list(const void *logits, int64_t at, int vocab, int *list, int n, int K) {
-    const Row<T, kAligned> row(logits, at, vocab);
-    const int lane = threadIdx.x & 31;
-    uint64_t last = ~0ull;
-    __syncwarp();
-    for (int r = 0; r < K; ++r) {
-        uint64_t k = 0ull;
-        for (int i = lane; i < n; i += 32) row.keys(list[i], [&](uint64_t e) { if (e < last) k = max(k, e); });
-        last = warp_max(k);
-    }
-    int kept = 0;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const int c = i0 + lane < n ? list[i0 + lane] : -1;
-        bool in = false;
-        if (c >= 0) row.keys(c, [&](uint64_t e) { in |= e >= last; });
-        __syncwarp();  // (all have read before any write, which is no further than they have read)
-        const uint32_t who = __ballot_sync(0xffffffffu, in);
-        if (in) list[kept + __popc(who & ((1u << lane) - 1))] = c;
-        kept += __popc(who);
-    }
-    __syncwarp();
-    return Cut{last, kept};
-}
-
 // The maximum and sum of a slice again, value by value, where NaN or an infinity is among them.
 template <typename T>
 __device__ __noinline__ float2 clean_sum(const T *src, int e0, int e1, float *s_part) {
@@ -237,71 +212,64 @@ __device__ __noinline__ float2 clean_sum(const T *src, int e0, int e1, float *s_
 template <typename T, bool kAligned>
 __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs a) {
     typedef Pack<T> P;
-    constexpr int kV = P::kN, kBits = 8 * sizeof(T), kStep = 32 * kWarps;  // chunks of a load of the CTA
-    __shared__ int s_chunks[kWarps][kWarpList];
-    __shared__ uint64_t s_list[kList];
+    constexpr int kV = P::kN, kBits = 8 * sizeof(T);
+    constexpr int kMore = kSubsets + kThreads * kV;  // candidates kept, and those of a chunk a thread
+    __shared__ union {
+        float tops[kTops][kThreads];
+        struct {
+            uint64_t list[kList];
+            int hits[kHits];
+        } few;  // (tops are read before)
+        uint64_t more[kMore];
+    } u;
     __shared__ uint32_t s_seen[kWarps][kSubsets];
-    __shared__ float s_ref[kWarps], s_sum[kWarps], s_cut[kWarps], s_part[kWarps];
+    __shared__ float s_ref[kWarps], s_sum[kWarps], s_part[kWarps];
     __shared__ uint64_t s_best[kWarps];
-    __shared__ int s_count;
+    __shared__ float s_bound;
+    __shared__ int s_hits, s_count;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int r = blockIdx.x / a.slices, slice = blockIdx.x - r * a.slices;
     const int K = a.select;
     pdl_trigger();
     pdl_wait();  // the logits and scores of the kernel before, and the last call's reads of the workspace
     if (row_closed(a, r)) return;
-    if (tid == 0) s_count = 0;
+    if (tid == 0) s_hits = s_count = 0;
 
     const Row<T, kAligned> row(a.logits, static_cast<int64_t>(r) * a.stride, a.vocab);
     const int chunks = (a.vocab + kV - 1) / kV, per = (chunks + a.slices - 1) / a.slices;
     const int c0 = min(chunks, slice * per), c1 = min(chunks, c0 + per);
-    const int tiles = (c1 - c0 + kStep * kLoads - 1) / (kStep * kLoads);
+    const int tiles = (c1 - c0 + kThreads * kLoads - 1) / (kThreads * kLoads), run = (tiles + kTops - 1) / kTops;
     const uint4 none = make_uint4(P::kNone, P::kNone, P::kNone, P::kNone);
     auto load = [&](int c) { return c < c1 ? row.chunk(c) : none; };
 
-    int *list = s_chunks[warp];
-    int len = 0;
-    typename P::Max seen = P::none();  // maxima of the lane's two subsets
-    float reach = -FLT_MAX;            // what a chunk's maximum has to reach to be noted
-    float cut = -INFINITY;             // K values of the warp's list reach it
+    typename P::Max seen = P::none();  // maxima of the thread's two subsets
     float ref = -INFINITY, c = 0.f;    // the sums' reference, and ref log2(e) as fp32 has it
     uint64_t z0 = f2_pack(0.f, 0.f), z1 = z0;
-    // The K-th largest of the maxima of the CTA's subsets. (Every warp comes here after
-    // the same tiles, so what the bound goes by has lower tokens than all later tiles.)
-    auto bound = [&]() {
-        s_seen[warp][lane] = order_bits(P::lo(seen));
-        s_seen[warp][lane + 32] = order_bits(P::hi(seen));
-        __syncthreads();
-        uint32_t x = s_seen[0][lane], y = s_seen[0][lane + 32];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) {
-            x = max(x, s_seen[w][lane]);
-            y = max(y, s_seen[w][lane + 32]);
-        }
-        return clean(from_order(max(kth_of_64<kBits>(x, y, K), order_bits(-INFINITY))));
-    };
     uint4 next[kLoads];
-    int at = c0 + warp * 32 + lane;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) next[i] = load(at + i * kStep);
-    for (int t = 0, renew = 0; t < tiles; ++t) {
+    for (int i = 0; i < kLoads; ++i) next[i] = load(c0 + i * kThreads + tid);
+    float run_top = -INFINITY;
+    for (int t = 0, in_run = 0, at = c0; t < tiles; ++t) {
         uint4 v[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) v[i] = next[i];
         const int here = at;
-        at += kLoads * kStep;
+        at += kLoads * kThreads;
         if (t + 1 < tiles) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) next[i] = load(at + i * kStep);
+            for (int i = 0; i < kLoads; ++i) next[i] = load(at + i * kThreads + tid);
         }
-        typename P::Max mx[kLoads], all = P::none();
+        typename P::Max all = P::max_of(v[0]);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            mx[i] = P::max_of(v[i]);
-            all = P::join(all, mx[i]);
-        }
+        for (int i = 1; i < kLoads; ++i) all = P::join(all, P::max_of(v[i]));
         seen = P::join(seen, all);
         const float top = fmaxf(P::lo(all), P::hi(all));
+        run_top = fmaxf(run_top, top);
+        if (++in_run == run || t + 1 == tiles) {
+            u.tops[t / run][tid] = run_top;
+            run_top = -INFINITY;
+            in_run = 0;
+        }
         if (__any_sync(0xffffffffu, top > ref + 5.5f)) {  // (e^5.5 < 2^8)
             const float m = fminf(from_order(__reduce_max_sync(0xffffffffu, order_bits(fmaxf(top, ref)))), FLT_MAX);
             const float cn = m * kLog2e;
@@ -316,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
             const uint64_t l2 = f2_pack(kLog2e, kLog2e), c2 = f2_pack(-c, -c);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                if (here - lane + i * kStep >= c1) break;
+                if (here + i * kThreads >= c1) break;
 #pragma unroll
                 for (int j = 0; j < kV; j += 2) {
                     float x, y;
@@ -327,31 +295,6 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
                 }
             }
         }
-        const bool now = t == renew;
-        float b = -INFINITY;
-        if (now) {
-            renew = 4 * renew + 3;
-            b = bound();
-            reach = fmaxf(reach, b);
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const bool in = fmaxf(P::lo(mx[i]), P::hi(mx[i])) >= reach;
-            const uint32_t who = __ballot_sync(0xffffffffu, in);
-            if (who == 0u) continue;
-            if (len > kWarpList - 32) {
-                const Cut k = cut_list<T, kAligned>(a.logits, static_cast<int64_t>(r) * a.stride, a.vocab, list, len, K);
-                len = k.len;
-                cut = key_value(k.last);
-                // (the list's values have lower tokens than all that follow)
-                reach = fmaxf(reach, from_order(order_bits(cut) + 1));
-            }
-            if (in) list[len + __popc(who & ((1u << lane) - 1))] = here + i * kStep;
-            len += __popc(who);
-        }
-        // from the next tile on, equals of the bound are higher tokens than K that reach it
-        if (b > -INFINITY) reach = fmaxf(reach, from_order(order_bits(b) + 1));
-        if (now && t + 1 < tiles) __syncthreads();  // (s_seen is written again)
     }
     {
         float x, y;
@@ -362,28 +305,25 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
         if (lane == 0) {
             s_ref[warp] = ref;
             s_sum[warp] = z;
-            s_cut[warp] = cut;
         }
+        s_seen[warp][lane] = order_bits(P::lo(seen));
+        s_seen[warp][lane + 32] = order_bits(P::hi(seen));
     }
     __syncthreads();
-    float floor = bound();
+    if (warp == 0) {  // the bound: by one warp, the issue slots go to the SM's other CTAs
+        uint32_t x = s_seen[0][lane], y = s_seen[0][lane + 32];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+            x = max(x, s_seen[w][lane]);
+            y = max(y, s_seen[w][lane + 32]);
+        }
+        x = kth_of_64<kBits>(x, y, K);
+        if (lane == 0) s_bound = fmaxf(clean(from_order(max(x, order_bits(-INFINITY)))), -FLT_MAX);
+    }
     // the slice's sum over 2^c, c = max log2(e) rounded, then over e^max: the rounding of c is taken out
     float m = s_ref[0], z = 0.f;
-    floor = fmaxf(floor, s_cut[0]);
 #pragma unroll
-    for (int i = 1; i < kWarps; ++i) {
-        m = fmaxf(m, s_ref[i]);
-        floor = fmaxf(floor, s_cut[i]);
-    }
-    // the values that reach the bound, and the bounds of the warps' cuts
-    auto values = [&](auto f) {
-        for (int i = lane; i < len; i += 32) row.keys(list[i], f);
-    };
-    values([&](uint64_t key) {
-        if (key_value(key) < floor) return;
-        const int n = atomicAdd(&s_count, 1);
-        if (n < kList) s_list[n] = key;
-    });
+    for (int i = 1; i < kWarps; ++i) m = fmaxf(m, s_ref[i]);
     c = m * kLog2e;
     for (int i = 0; i < kWarps; ++i)
         if (s_ref[i] > -INFINITY) z += s_sum[i] * fast_exp2(s_ref[i] * kLog2e - c);
@@ -392,30 +332,86 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
     if (m > -INFINITY && !(z < INFINITY)) part = clean_sum(row.src, c0 * kV, min(a.vocab, c1 * kV), s_part);  // NaN or +inf among them
     if (tid == 0) a.parts[blockIdx.x] = part;
     __syncthreads();
-    const int n = s_count;
-    uint64_t *keys = a.keys + static_cast<int64_t>(blockIdx.x) * K;
-    if (n <= kList) {
-        for (int i = tid; i < n; i += kThreads) {
-            const uint64_t key = s_list[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += s_list[j] > key;
-            if (rank < K) keys[rank] = key;
-        }
-        for (int i = n + tid; i < K; i += kThreads) keys[i] = 0ull;
-        return;
+    const float bound = s_bound;
+    uint32_t reach = 0u;  // the thread's runs of tiles that reach the bound
+    for (int i = 0; i * run < tiles; ++i) reach |= (u.tops[i][tid] >= bound ? 1u : 0u) << i;
+    __syncthreads();
+    while (reach) {
+        const int i = __ffs(reach) - 1, n = atomicAdd(&s_hits, 1);
+        reach &= reach - 1;
+        if (n < kHits) u.few.hits[n] = i * kThreads + tid;
     }
-    uint64_t last = ~0ull;  // K rounds of a maximum over the warps' lists
-    for (int i = 0; i < K; ++i) {
-        uint64_t k = 0ull;
-        values([&](uint64_t key) { if (key < last) k = max(k, key); });
-        k = warp_max(k);
+    __syncthreads();
+    const int hits = s_hits;
+    uint64_t *keys = a.keys + static_cast<int64_t>(blockIdx.x) * K;
+    if (hits <= kHits) {
+        const int loads = run * kLoads;  // of a hit
+        for (int i = tid; i < hits * loads; i += kThreads) {
+            const int hit = u.few.hits[i / loads], at = c0 + (hit / kThreads * loads + i % loads) * kThreads + hit % kThreads;
+            if (at < c1)
+                row.keys(at, [&](uint64_t key) {
+                    if (key_value(key) < bound) return;
+                    const int n = atomicAdd(&s_count, 1);
+                    if (n < kList) u.few.list[n] = key;
+                });
+        }
         __syncthreads();
-        if (lane == 0) s_best[warp] = k;
+        const int n = s_count;
+        if (n <= kList) {
+            for (int i = tid; i < n; i += kThreads) {
+                const uint64_t key = u.few.list[i];
+                int rank = 0;
+                for (int j = 0; j < n; ++j) rank += u.few.list[j] > key;
+                if (rank < K) keys[rank] = key;
+            }
+            for (int i = n + tid; i < K; i += kThreads) keys[i] = 0ull;
+            return;
+        }
+    }
+    // Many values reach the bound (equals of it, or large values in few subsets): the
+    // slice again, a chunk a thread, whose candidates are cut to the best K each time.
+    __syncthreads();
+    if (tid == 0) s_count = 0;
+    __syncthreads();
+    uint64_t worst = 0ull;  // of K kept ones; the later tokens of equals are worse
+    for (int at = c0; at < c1; at += kThreads) {
+        if (at + tid < c1)
+            row.keys(at + tid, [&](uint64_t key) {
+                if (key > worst && key_value(key) >= bound) u.more[atomicAdd(&s_count, 1)] = key;
+            });
         __syncthreads();
-        last = s_best[0];
+        const int n = s_count;
+        if (n > K) {
+            uint64_t last = ~0ull, mine = 0ull;
+            for (int i = 0; i < K; ++i) {
+                uint64_t k = 0ull;
+                for (int j = tid; j < n; j += kThreads)
+                    if (u.more[j] < last) k = max(k, u.more[j]);
+                k = warp_max(k);
+                if (lane == 0) s_best[warp] = k;
+                __syncthreads();
+                last = s_best[0];
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) last = max(last, s_best[w]);
-        if (tid == 0) keys[i] = last;  // (0 once there are none left)
+                for (int w = 1; w < kWarps; ++w) last = max(last, s_best[w]);
+                if (tid == i) mine = last;
+                __syncthreads();
+            }
+            if (tid < K) u.more[tid] = mine;
+            if (tid == 0) s_count = K;
+            worst = last;
+        }
+        __syncthreads();
+    }
+    for (int i = tid; i < K; i += kThreads) {
+        // (cut lists are in order; one that never was is ranked)
+        const int n = s_count;
+        int rank = i;
+        uint64_t key = i < n ? u.more[i] : 0ull;
+        if (i < n) {
+            rank = 0;
+            for (int j = 0; j < n; ++j) rank += u.more[j] > key;
+        }
+        keys[rank] = key;
     }
 }
 
@@ -449,7 +445,7 @@ __device__ Two two_log(float z) {
 // better, ties to the lower beam and token.
 struct Cand {
     uint64_t total;
-    int64_t tie;  // beam * vocab + token
+    int64_t tie;  // beam * 2^32 + token
 };
 __device__ __forceinline__ Cand no_cand() { return Cand{0ull, INT64_MAX}; }
 __device__ __forceinline__ bool better(const Cand &a, const Cand &b) {
@@ -486,15 +482,17 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
     const uint64_t key1 = tid + kMergeThreads < W * S * K ? keys[tid + kMergeThreads] : 0ull;
     for (int w = warp; w < W; w += kMergeThreads / 32) {
         const int row = g * W + w;
+        const float2 *part = a.parts + static_cast<int64_t>(row) * S;
+        const float2 first = lane < S ? part[lane] : make_float2(-INFINITY, 0.f);  // (with the score's load; not used of a closed row)
         const bool open = !row_closed(a, row);
         float m = -INFINITY, z = 0.f;
         if (open) {
-            const float2 *part = a.parts + static_cast<int64_t>(row) * S;
-            for (int s = lane; s < S; s += 32) m = fmaxf(m, part[s].x);
+            m = first.x;
+            for (int s = lane + 32; s < S; s += 32) m = fmaxf(m, part[s].x);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
             for (int s = lane; s < S; s += 32) {
-                const float2 p = part[s];
+                const float2 p = s == lane ? first : part[s];
                 if (p.x > -INFINITY) z += p.y * expf(p.x - m);
             }
 #pragma unroll
@@ -513,13 +511,13 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
     auto cand = [&](int w, uint64_t key) {
         const Two d = two_sum(key_value(key), -s_max[w]), off = s_off[w], t = two_sum(d.hi, off.hi);
         return Cand{order_bits2(two_norm(t.hi, t.lo + (d.lo + off.lo))),
-                    static_cast<int64_t>(w) * a.vocab + static_cast<int64_t>(0xFFFFFFFFu - static_cast<uint32_t>(key))};
+                    static_cast<int64_t>(w) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(key))};
     };
     auto end_of = [&](int w) {  // the one continuation of a finished beam
         const int row = g * W + w;
         const float s = a.scores[row];
         if (a.finished == nullptr || a.finished[row] == 0 || a.end_token < 0 || !(s > -INFINITY)) return no_cand();
-        return Cand{order_bits2(two_norm(s, 0.f)), static_cast<int64_t>(w) * a.vocab + a.end_token};
+        return Cand{order_bits2(two_norm(s, 0.f)), static_cast<int64_t>(w) << 32 | a.end_token};
     };
     // the K-th best of the subsets' bests (threads t and t + kMergeSubsets), which K candidates reach
     uint64_t best = 0ull;
@@ -569,10 +567,9 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
     auto put = [&](int r, const Cand &c) {
         const int64_t o = static_cast<int64_t>(g) * K + r;
         const bool none = c.total == 0ull;
-        const int w = none ? 0 : static_cast<int>(c.tie / a.vocab);
         a.out_scores[o] = none ? -INFINITY : from_order(static_cast<uint32_t>(c.total >> 32));
-        a.out_parents[o] = none ? -1 : g * W + w;
-        a.out_tokens[o] = none ? -1 : static_cast<int32_t>(c.tie - static_cast<int64_t>(w) * a.vocab);
+        a.out_parents[o] = none ? -1 : g * W + static_cast<int>(c.tie >> 32);
+        a.out_tokens[o] = none ? -1 : static_cast<int32_t>(c.tie);
     };
     if (n <= kList) {
         for (int i = tid; i < n; i += kMergeThreads) {
