@@ -602,8 +602,9 @@ int fnpu_window_decode(const fnpu_attn_desc *desc, int32_t window, int32_t sinks
  * largest finite value, and a beam whose score is -inf or NaN has no continuation
  * (the idle beams of a first step). Where a group has fewer than num_select, the
  * rest come out with score -inf, parent -1 and token -1.
- * Exponentials are summed in fp32 a slice of a row and combined in 64 bits, and
- * totals are compared in 64 bits.
+ * Exponentials are summed in fp32; logarithms, totals and their comparison have 48
+ * bits (pairs of fp32). Rows are cut by token numbers, so beams of equal logits and
+ * scores tie exactly, wherever their rows start. Scores are finite, -inf or NaN.
  *   logits        device, row_stride values between rows (>= vocab; the start of a
  *                 row needs the alignment of its type only)
  *   scores        device fp32 [num_groups, num_beams]

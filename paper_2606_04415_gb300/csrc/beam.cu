@@ -182,7 +182,7 @@ struct Row {
     }
 };
 
-// The maximum and sum of a slice again, value by value, where NaN or an infinity is among them.
+// The maximum and sum of a slice again, value by value.
 template <typename T>
 __device__ __noinline__ float2 clean_sum(const T *src, int e0, int e1, float *s_part) {
     const int tid = threadIdx.x;
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
 
     typename P::Max seen = P::none();  // maxima of the thread's two subsets
     float ref = -INFINITY, c = 0.f;    // the sums' reference, and ref log2(e) as fp32 has it
-    uint64_t z0 = f2_pack(0.f, 0.f), z1 = z0;
+    uint64_t z = f2_pack(0.f, 0.f);    // (a tile's values are added up first: rounding errors grow with the tiles alone)
     uint4 next[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) next[i] = load(c0 + i * kThreads + tid);
@@ -270,16 +270,15 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
         }
         if (__any_sync(0xffffffffu, top > ref + 5.5f)) {  // (e^5.5 < 2^8)
             const float m = fminf(from_order(__reduce_max_sync(0xffffffffu, order_bits(fmaxf(top, ref)))), FLT_MAX);
-            const float cn = m * kLog2e;
+            const float cn = __fmul_rn(m, kLog2e);  // (rounded wherever it is used, never part of a multiply-add)
             const float f = ref > -INFINITY ? fast_exp2(c - cn) : 0.f;
-            const uint64_t f2 = f2_pack(f, f), o2 = f2_pack(0.f, 0.f);
-            z0 = f2_fma(z0, f2, o2);
-            z1 = f2_fma(z1, f2, o2);
+            z = f2_fma(z, f2_pack(f, f), f2_pack(0.f, 0.f));
             ref = m;
             c = cn;
         }
         if (ref > -INFINITY) {
             const uint64_t l2 = f2_pack(kLog2e, kLog2e), c2 = f2_pack(-c, -c);
+            uint64_t z0 = f2_pack(0.f, 0.f), z1 = z0;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 if (here + i * kThreads >= c1) break;
@@ -292,17 +291,18 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
                     else z0 = f2_add(z0, e);
                 }
             }
+            z = f2_add(z, f2_add(z0, z1));
         }
     }
     {
         float x, y;
-        f2_unpack(f2_add(z0, z1), x, y);
-        float z = x + y;
+        f2_unpack(z, x, y);
+        x += y;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
         if (lane == 0) {
             s_ref[warp] = ref;
-            s_sum[warp] = z;
+            s_sum[warp] = x;
         }
         s_seen[warp][lane] = order_bits(P::lo(seen));
         s_seen[warp][lane + 32] = order_bits(P::hi(seen));
@@ -319,15 +319,16 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
         if (lane == 0) s_bound = fmaxf(clean(from_order(max(x, order_bits(-INFINITY)))), -FLT_MAX);
     }
     // the slice's sum over 2^c, c = max log2(e) rounded, then over e^max: the rounding of c is taken out
-    float m = s_ref[0], z = 0.f;
+    float m = s_ref[0], sum = 0.f;
 #pragma unroll
     for (int i = 1; i < kWarps; ++i) m = fmaxf(m, s_ref[i]);
-    c = m * kLog2e;
+    c = __fmul_rn(m, kLog2e);
     for (int i = 0; i < kWarps; ++i)
-        if (s_ref[i] > -INFINITY) z += s_sum[i] * fast_exp2(s_ref[i] * kLog2e - c);
-    z -= z * fmaf(m, kLog2e, -c) * kLn2;
-    float2 part = make_float2(m, z);
-    if (m > -INFINITY && !(z < INFINITY)) part = clean_sum(row.src, c0 * kV, min(a.vocab, c1 * kV), s_part);  // NaN or +inf among them
+        if (s_ref[i] > -INFINITY) sum += s_sum[i] * fast_exp2(__fmul_rn(s_ref[i], kLog2e) - c);
+    sum -= sum * fmaf(m, kLog2e, -c) * kLn2;
+    float2 part = make_float2(m, sum);
+    // (NaN or an infinity among them, or a maximum whose product with log2(e) overflows; else the maximum gives 1)
+    if (m > -INFINITY && !(sum > 0.5f && sum < INFINITY)) part = clean_sum(row.src, c0 * kV, min(a.vocab, c1 * kV), s_part);
     if (tid == 0) a.parts[blockIdx.x] = part;
     __syncthreads();
     const float bound = s_bound;
@@ -422,8 +423,9 @@ __device__ __forceinline__ Two two_sum(float a, float b) {  // exact
     return Two{s, (a - (s - t)) + (b - t)};
 }
 __device__ __forceinline__ Two two_norm(float hi, float lo) {
+    if (!(fabsf(hi) < INFINITY)) return Two{hi, 0.f};  // (`lo` is NaN then)
     const float s = hi + lo;
-    return fabsf(s) < INFINITY ? Two{s + 0.f, (lo - (s - hi)) + 0.f} : Two{s, 0.f};  // (no zero is negative)
+    return Two{s + 0.f, (lo - (s - hi)) + 0.f};  // (no zero is negative)
 }
 // ln z, z of 1 or more (but for rounding): z = 2^e f, ln f = 2 atanh((f - 1) / (f + 1))
 // by its series. Off by some 1e-9.

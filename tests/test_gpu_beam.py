@@ -131,6 +131,18 @@ def test_scores_far_apart_and_near_each_other():
     _check(x, s, 3, _run(x, s, 3))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_logits_near_the_ends_of_their_type(dtype):
+    """Finite logits whose multiple in base 2 is not, alone and beside ordinary ones."""
+    x, s = _logits(13, 4, 2, 3001, dtype)
+    x[0, 0, 5], x[0, 0, 2900] = 3e38, 2.5e38
+    x[0, 1], x[0, 1, 17:19] = -3e38, -2.9e38
+    x[1, 0], x[1, 0, 2000] = -3.3e38, 3.3e38
+    x[2, 0, 7], x[2, 0, 8] = float("inf"), 3e38
+    x[3, 1] = 3e38
+    _check(x, s, 2, _run(x, s, 2))
+
+
 def test_captured_and_on_other_streams():
     x, s = _logits(21, 2, 4, 20000, torch.bfloat16)
     import paper_2606_04415_gb300 as fnpu
@@ -148,6 +160,22 @@ def test_captured_and_on_other_streams():
             g.replay()
         torch.cuda.synchronize()
         _check(x, s, 8, out)
+
+
+@pytest.mark.parametrize("run", [1, 2])
+def test_long_slices(run):
+    """Rows in one slice each of so many tiles that a thread keeps maxima of several; the reference on the device."""
+    g, b, v, k = 61, 5, 130000 * run, 20
+    x = torch.randn((g, b, v), device="cuda", generator=torch.Generator(device="cuda").manual_seed(run)) * 3
+    s = -10 * torch.rand((g, b), device="cuda", generator=torch.Generator(device="cuda").manual_seed(9))
+    got = _run(x, s, k)
+    for i in range(0, g, 6):
+        total = (s[i].double()[:, None] + torch.log_softmax(x[i].double(), -1)).flatten()
+        best = torch.sort(total, descending=True, stable=True)
+        assert (got[1][i].long() - i * b).tolist() == (best.indices[:k] // v).tolist()
+        assert got[2][i].tolist() == (best.indices[:k] % v).tolist()
+        ref = best.values[:k]
+        assert ((got[0][i].double() - ref).abs() <= ref.abs() * 2.0 ** -24 + 2.0 ** -20).all()
 
 
 def test_binding_checks():
