@@ -6,7 +6,8 @@
 // of dependent steps: counts before free blocks, free blocks before their rows. Each
 // step is a kernel over all SMs and a dependent launch of the one before; where a step is a
 // matter of some rows and one chunk of counts, all steps are one kernel of one CTA, a
-// warp a row (launches of 3 steps take 8 us, 6 of them the host's). Every
+// warp a row, with what passes between them in shared memory (14.2 us
+// for a turn of 8 rows with its copies, 12.1 so). Every
 // result is independent of the order of the atomics: counts are sums, the lowest row
 // of a page a minimum, and the k-th block that is taken is the k-th free one by id, by a
 // prefix sum over chunks of counts that each CTA forms for itself.
@@ -21,6 +22,7 @@ constexpr int kRowThreads = 256;    // kernels over rows
 constexpr int kScanThreads = 512;   // kernels over chunks of counts, and those of one CTA
 constexpr int kPer = kPagesChunk / kScanThreads;
 constexpr int64_t kSmallEntries = 16384;  // of the tables that one CTA goes through
+constexpr int kSmallRows = 64;            // and their rows (four a warp)
 
 // States of a new row, where its last page is full or there is none to write to.
 constexpr int kRowFull = -1;   // goes on with new blocks
@@ -352,10 +354,27 @@ __global__ void __launch_bounds__(kScanThreads) fork_take_kernel(const PagesArgs
     pdl_wait();
     fork_take(a, blockIdx.x, &s, s_off);
 }
+// What the workspace holds otherwise, where one CTA does all steps.
+struct SmallShared {
+    int rows[3][kSmallRows + 2];
+    int blocks[2][kPagesChunk];
+    int count;
+};
+__device__ __forceinline__ PagesArgs with_shared(PagesArgs a, SmallShared *s) {
+    a.chunk_count = &s->count;
+    a.row_length = s->rows[0];
+    a.row_tail = s->rows[1];
+    a.row_refs = s->rows[2];
+    a.block_a = s->blocks[0];
+    a.block_b = s->blocks[1];
+    return a;
+}
 // All three steps, of one chunk.
-__global__ void __launch_bounds__(kScanThreads) fork_small_kernel(const PagesArgs a) {
+__global__ void __launch_bounds__(kScanThreads) fork_small_kernel(const PagesArgs args) {
     extern __shared__ int s_off[];
     __shared__ ForkShared s;
+    __shared__ SmallShared small;
+    const PagesArgs a = with_shared(args, &small);
     pdl_trigger();
     pdl_wait();
     for (int u = threadIdx.x / 32; u < a.new_rows + a.rows; u += kScanThreads / 32) fork_row<32>(a, u, nullptr);
@@ -476,8 +495,10 @@ __global__ void __launch_bounds__(kScanThreads) compact_move_kernel(const PagesA
     else compact_row<kScanThreads>(a, static_cast<int>(blockIdx.x) - a.chunks, live, moves);
 }
 // All three steps, of one chunk.
-__global__ void __launch_bounds__(kScanThreads) compact_small_kernel(const PagesArgs a) {
+__global__ void __launch_bounds__(kScanThreads) compact_small_kernel(const PagesArgs args) {
     __shared__ int s_sum[kScanThreads / 32];
+    __shared__ SmallShared small;
+    const PagesArgs a = with_shared(args, &small);
     pdl_trigger();
     pdl_wait();
     const int n = live_in_chunk(a, 0, s_sum);
@@ -550,7 +571,7 @@ int launch_pages_fork(const PagesArgs &a, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const size_t smem = sizeof(int) * (a.new_rows + 1);
     const int64_t rows = static_cast<int64_t>(a.new_rows) + a.rows;
-    if (a.chunks == 1 && a.chunk == kPagesChunk && rows <= 4 * (kScanThreads / 32) && rows * a.width <= kSmallEntries) {
+    if (a.chunks == 1 && a.chunk == kPagesChunk && rows <= kSmallRows && rows * a.width <= kSmallEntries) {
         FNPU_CUDA_TRY(launch_ex(fork_small_kernel, 1u, kScanThreads, smem, st, true, nullptr, a));
         return FNPU_OK;
     }
@@ -563,7 +584,7 @@ int launch_pages_fork(const PagesArgs &a, void *stream) {
 
 int launch_pages_compact(const PagesArgs &a, void *stream) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (a.chunks == 1 && a.chunk == kPagesChunk && a.rows <= 4 * (kScanThreads / 32) &&
+    if (a.chunks == 1 && a.chunk == kPagesChunk && a.rows <= kSmallRows &&
         static_cast<int64_t>(a.rows) * a.width <= kSmallEntries) {
         FNPU_CUDA_TRY(launch_ex(compact_small_kernel, 1u, kScanThreads, 0, st, true, nullptr, a));
         return FNPU_OK;
