@@ -21,6 +21,10 @@
 //     may lie closer than an fp32 score of some hundred resolves (3e-5), and fp64 is slow
 //     on this device (a warp's instruction takes some 60 cycles), so totals are
 //     unevaluated sums of two floats (Dekker 1971), compared as order-preserving integers.
+// 512 rows of 151936 in bf16 (140 MB of open beams): 34 us, 4.1 TB/s. Some 8 us of it are what
+// the smallest call takes (4 rows of 32000 8.5 us: first loads, the bound, the merge); the
+// reading by itself runs at 6 TB/s (rows of 151936 against rows of 32000). Both steps in one kernel,
+// a cluster a group with the lists in its first CTA's shared memory, took as long.
 #include <float.h>
 
 #include "common.cuh"
@@ -30,7 +34,8 @@ namespace {
 
 constexpr int kThreads = 256;       // of the first kernel
 constexpr int kWarps = kThreads / 32;
-constexpr int kLoads = 4;           // 16-byte loads of a lane in a tile
+constexpr int kLoads = 8;           // 16-byte loads of a lane in a tile, all in flight
+constexpr int kGroup = 4;           // of them that are taken together
 constexpr int kMergeThreads = 256;  // of the second
 constexpr int kSubsets = 64;        // (num_select is at most as many)
 constexpr int kMergeSubsets = 128;  // (two threads count for each)
@@ -230,7 +235,6 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
     const int K = a.select;
     pdl_trigger();
     pdl_wait();  // the logits and scores of the kernel before, and the last call's reads of the workspace
-    if (row_closed(a, r)) return;
     if (tid == 0) s_hits = s_count = 0;
 
     const Row<T, kAligned> row(a.logits, static_cast<int64_t>(r) * a.stride, a.vocab);
@@ -242,56 +246,52 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
 
     typename P::Max seen = P::none();  // maxima of the thread's two subsets
     float ref = -INFINITY, c = 0.f;    // the sums' reference, and ref log2(e) as fp32 has it
-    uint64_t z = f2_pack(0.f, 0.f);    // (a tile's values are added up first: rounding errors grow with the tiles alone)
-    uint4 next[kLoads];
+    uint64_t z = f2_pack(0.f, 0.f);    // (a group's values are added up first: rounding errors grow with the groups alone)
+    uint4 v[kLoads];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) next[i] = load(c0 + i * kThreads + tid);
+    for (int i = 0; i < kLoads; ++i) v[i] = load(c0 + i * kThreads + tid);
+    if (row_closed(a, r)) return;  // (known while the first values are on their way)
     float run_top = -INFINITY;
-    for (int t = 0, in_run = 0, at = c0; t < tiles; ++t) {
-        uint4 v[kLoads];
+    for (int t = 0, in_run = 0, at = c0; t < tiles; ++t, at += kLoads * kThreads) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) v[i] = next[i];
-        const int here = at;
-        at += kLoads * kThreads;
-        if (t + 1 < tiles) {
+        for (int g = 0; g < kLoads; g += kGroup) {
+            if (at + g * kThreads >= c1) break;
+            typename P::Max all = P::max_of(v[g]);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) next[i] = load(at + i * kThreads + tid);
+            for (int i = 1; i < kGroup; ++i) all = P::join(all, P::max_of(v[g + i]));
+            seen = P::join(seen, all);
+            const float top = fmaxf(P::lo(all), P::hi(all));
+            run_top = fmaxf(run_top, top);
+            if (__any_sync(0xffffffffu, top > ref + 5.5f)) {  // (e^5.5 < 2^8)
+                const float m = fminf(from_order(__reduce_max_sync(0xffffffffu, order_bits(fmaxf(top, ref)))), FLT_MAX);
+                const float cn = __fmul_rn(m, kLog2e);  // (rounded wherever it is used, never part of a multiply-add)
+                const float f = ref > -INFINITY ? fast_exp2(c - cn) : 0.f;
+                z = f2_fma(z, f2_pack(f, f), f2_pack(0.f, 0.f));
+                ref = m;
+                c = cn;
+            }
+            if (ref > -INFINITY) {
+                const uint64_t l2 = f2_pack(kLog2e, kLog2e), c2 = f2_pack(-c, -c);
+                uint64_t z0 = f2_pack(0.f, 0.f), z1 = z0;
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i)
+#pragma unroll
+                    for (int j = 0; j < kV; j += 2) {
+                        float x, y;
+                        f2_unpack(f2_fma(f2_pack(P::get(v[g + i], j), P::get(v[g + i], j + 1)), l2, c2), x, y);
+                        const uint64_t e = f2_pack(fast_exp2(x), fast_exp2(y));
+                        if (j & 2) z1 = f2_add(z1, e);
+                        else z0 = f2_add(z0, e);
+                    }
+                z = f2_add(z, f2_add(z0, z1));
+            }
+#pragma unroll
+            for (int i = g; i < g + kGroup; ++i) v[i] = load(at + (kLoads + i) * kThreads + tid);
         }
-        typename P::Max all = P::max_of(v[0]);
-#pragma unroll
-        for (int i = 1; i < kLoads; ++i) all = P::join(all, P::max_of(v[i]));
-        seen = P::join(seen, all);
-        const float top = fmaxf(P::lo(all), P::hi(all));
-        run_top = fmaxf(run_top, top);
         if (++in_run == run || t + 1 == tiles) {
             u.tops[t / run][tid] = run_top;
             run_top = -INFINITY;
             in_run = 0;
-        }
-        if (__any_sync(0xffffffffu, top > ref + 5.5f)) {  // (e^5.5 < 2^8)
-            const float m = fminf(from_order(__reduce_max_sync(0xffffffffu, order_bits(fmaxf(top, ref)))), FLT_MAX);
-            const float cn = __fmul_rn(m, kLog2e);  // (rounded wherever it is used, never part of a multiply-add)
-            const float f = ref > -INFINITY ? fast_exp2(c - cn) : 0.f;
-            z = f2_fma(z, f2_pack(f, f), f2_pack(0.f, 0.f));
-            ref = m;
-            c = cn;
-        }
-        if (ref > -INFINITY) {
-            const uint64_t l2 = f2_pack(kLog2e, kLog2e), c2 = f2_pack(-c, -c);
-            uint64_t z0 = f2_pack(0.f, 0.f), z1 = z0;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if (here + i * kThreads >= c1) break;
-#pragma unroll
-                for (int j = 0; j < kV; j += 2) {
-                    float x, y;
-                    f2_unpack(f2_fma(f2_pack(P::get(v[i], j), P::get(v[i], j + 1)), l2, c2), x, y);
-                    const uint64_t e = f2_pack(fast_exp2(x), fast_exp2(y));
-                    if (j & 2) z1 = f2_add(z1, e);
-                    else z0 = f2_add(z0, e);
-                }
-            }
-            z = f2_add(z, f2_add(z0, z1));
         }
     }
     {
@@ -461,8 +461,9 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
     int *s_open = reinterpret_cast<int *>(s_max + a.beams);
     __shared__ Cand s_best[kMergeThreads];
     __shared__ Cand s_list[kList];
-    __shared__ __align__(16) uint64_t s_sub[kMergeSubsets];
-    __shared__ uint64_t s_bound;
+    __shared__ uint32_t s_top[kMergeSubsets];
+    __shared__ __align__(16) uint32_t s_sub[kMergeSubsets];
+    __shared__ uint32_t s_bound;
     __shared__ int s_count;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = blockIdx.x, W = a.beams, S = a.slices, K = a.select;
@@ -470,7 +471,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
     pdl_wait();
     if (tid == 0) {
         s_count = 0;
-        s_bound = 0ull;
+        s_bound = ~0u;
     }
     // what a thread looks at below, on its way before the sums are known (a closed
     // beam's lists are not written; they are not looked at either)
@@ -519,35 +520,35 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
         if (a.finished == nullptr || a.finished[row] == 0 || a.end_token < 0 || !(s > -INFINITY)) return no_cand();
         return Cand{order_bits2(two_norm(s, 0.f)), static_cast<int64_t>(w) << 32 | a.end_token};
     };
-    // the K-th best of the subsets' bests (threads t and t + kMergeSubsets), which K candidates reach
-    uint64_t best = 0ull;
+    // the K-th best of the subsets' bests (threads t and t + kMergeSubsets; by the first of the
+    // two floats), which K candidates reach: the least of those that fewer than K are above
+    uint32_t best = 0u;
     for (int i = tid; i < W * S * deep; i += kMergeThreads) {
         const int l = i % (W * S), w = l / S;
         const uint64_t key = !s_open[w] ? 0ull : i == tid ? head0 : keys[l * K + i / (W * S)];
-        if (key != 0ull) best = max(best, cand(w, key).total);
+        if (key != 0ull) best = max(best, static_cast<uint32_t>(cand(w, key).total >> 32));
     }
-    for (int w = tid; w < W; w += kMergeThreads) best = max(best, end_of(w).total);
-    if (tid >= kMergeSubsets) s_best[tid].total = best;
+    for (int w = tid; w < W; w += kMergeThreads) best = max(best, static_cast<uint32_t>(end_of(w).total >> 32));
+    if (tid >= kMergeSubsets) s_top[tid - kMergeSubsets] = best;
     __syncthreads();
-    if (tid < kMergeSubsets) s_sub[tid] = max(best, s_best[tid + kMergeSubsets].total);
+    if (tid < kMergeSubsets) s_sub[tid] = max(best, s_top[tid]);
     __syncthreads();
     {
-        const uint64_t mine = s_sub[tid / 2];
-        int above = 0, reach = 0;
-#pragma unroll 8
-        for (int i = tid % 2; i < kMergeSubsets / 2; i += 2) {
-            const ulonglong2 o = reinterpret_cast<const ulonglong2 *>(s_sub)[i];
-            above += (o.x > mine) + (o.y > mine);
-            reach += (o.x >= mine) + (o.y >= mine);
+        const uint32_t mine = s_sub[tid / 2];
+        int above = 0;
+#pragma unroll
+        for (int i = 0; i < kMergeSubsets / 8; ++i) {
+            const uint4 o = reinterpret_cast<const uint4 *>(s_sub)[2 * i + tid % 2];
+            above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
         }
         above += __shfl_xor_sync(0xffffffffu, above, 1);
-        reach += __shfl_xor_sync(0xffffffffu, reach, 1);
-        if (above < K && K <= reach) s_bound = mine;  // (all that get here have the same)
+        const uint32_t least = __reduce_min_sync(0xffffffffu, above < K ? mine : ~0u);
+        if (lane == 0) atomicMin(&s_bound, least);
     }
     __syncthreads();
-    const uint64_t bound = s_bound;  // (0: there are fewer)
+    const uint32_t bound = s_bound;  // (0: there are fewer)
     auto take = [&](const Cand &c) {
-        if (c.total == 0ull || c.total < bound) return;
+        if (c.total == 0ull || static_cast<uint32_t>(c.total >> 32) < bound) return;
         const int n = atomicAdd(&s_count, 1);
         if (n < kList) s_list[n] = c;
     };
@@ -607,9 +608,9 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
 
 // Slices a row: what the SMs hold at once (4 CTAs each), but no more than balances a
 // slice's time with what each adds to the merge (s slices of n / s chunks: s^2 = n / 192).
-// us a call, rows x vocabulary in bf16: 152 x 151936 20.1 with 4, 22.0 with 3, 24.4 with 6;
-// 512 x 151936 38.8 with 1, 44.2 with 2; 4 x 151936 10.8 with 12, 12.1 with 4, 18.1 with 75;
-// 16 x 32000 9.4 with 4, 11.2 with 1, 13.2 with 16.
+// us a call, rows x vocabulary in bf16: 152 x 151936 19.6 with 4, 20.6 with 3, 23.4 with 6;
+// 512 x 151936 35.6 with 1, 40.1 with 2; 4 x 151936 10.7 with 8, 11.4 with 4, 17.2 with 1;
+// 8 x 32000 9.9 with 4, 10.6 with 1, 12.4 with 16.
 int beam_slices(const fnpu_beam_desc *d) {
     const int64_t rows = static_cast<int64_t>(d->num_groups) * d->num_beams;
     const int64_t chunks = d->dtype == FNPU_LOGITS_FP32 ? (static_cast<int64_t>(d->vocab) + 3) / 4 : (static_cast<int64_t>(d->vocab) + 7) / 8;
