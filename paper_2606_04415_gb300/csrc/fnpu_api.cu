@@ -1216,9 +1216,10 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
                 const int32_t rows = std::min(P2, q - r0);
                 int32_t ntiles = (prefix + r0 + rows + KT - 1) / KT;
                 if (windowed) {
-                    // virtual tiles: those between the sinks and the first row's window are
-                    // left out; a row may see no key of a split piece, so pieces start anywhere
-                    ntiles -= std::max(0, win.first_key(prefix + r0 + 1) / KT - win.sink_keys(KT) / KT);
+                    // whole blocks between the sinks and the first row's window are left
+                    // out; a row may see no key of a split piece, so pieces start anywhere
+                    const int32_t skip = std::max(0, win.first_key(prefix + r0 + 1) / bs * bs - win.sink_keys(bs));
+                    ntiles = (prefix + r0 + rows - skip + KT - 1) / KT;
                     for (int32_t kvh = 0; kvh < desc->num_kv_heads; ++kvh)
                         tc_units.push_back(TcUnit{s, kvh, r0, rows, ntiles, ntiles - 1, 0, ntiles});
                     continue;

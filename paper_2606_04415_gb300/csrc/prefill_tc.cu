@@ -45,14 +45,15 @@
 // TMEM (512 columns): S0 at 0, S1 at 128 (fp32, P over their first 64
 // columns); O0 at 256, O1 at 384.
 //
-// With a window and sinks (kWindow) an item's key tiles are virtual: those wholly
-// between the sinks and its first row's window are cut out, tile v of the item
-// being tile v below the sinks' end and v + skip from there on. Keys that no row
-// of the item sees are not loaded where their whole block is hidden (its page may
-// be gone: a box past the pool lands as zeros); the others' V rows are zeroed like
-// those past the context, in up to three tiles an item, so each V stage has a
-// barrier of its own for that. A row may see no key of a split piece, whose
-// partial result is then 0 with a log-sum-exp of -inf.
+// With a window and sinks (kWindow) an item's keys are virtual: the whole blocks
+// between the sinks' last and the one where its first row's window begins are cut out, and
+// positions, contexts and tiles are those of the shorter sequence (the mask's distances stay
+// what they were). A tile is read block by block, so it may hold the end of the sinks and the
+// begin of the window; tiles of 128 whole keys, the sinks in tiles of their own, took a
+// tile and a half more an item. Keys that no row of the item sees are left in at most two
+// blocks; their V rows are zeroed like those past the context, so each V stage has a
+// barrier of its own for that. A row may see no key of a split piece, whose partial
+// result is then 0 with a log-sum-exp of -inf.
 // Every mbarrier wait is bounded; a timeout raises the plan's error flag and
 // the CTA drains its tensor-core work and copies, frees its tensor memory and
 // exits. Launched as a programmatic dependent of the kernel before it (the step's
@@ -118,16 +119,13 @@ struct TcMaps {
 // dual: one Q tile, its even key tiles on tile 0's path and its odd ones on tile 1's
 template <bool kDual, bool kWindow = false>
 struct ItemGeomT {
-    int sink_tiles, skip, lo;  // window: tiles of the sinks, tiles left out behind them, first key of the first row's window
+    int skip, lo;  // window: keys left out behind the sinks' blocks, first key of the first row's window
     int kvh, p0, rows, prefix, ctx, kt0, ntiles, q_start, bt_row;
     int ns, split, pbase, cnt;  // key splits of the tile pair, this split, first partial, merge counter
     bool tail_fix;
     bool dual;
-    // the 128-key tile of the sequence that the item's i-th tile is
-    __device__ __forceinline__ int tile(int i) const {
-        const int v = kt0 + i;
-        return kWindow && v >= sink_tiles ? v + skip : v;
-    }
+    // the 128-key tile that the item's i-th tile is
+    __device__ __forceinline__ int tile(int i) const { return kt0 + i; }
     // hidden keys [a, b) of the 128 from k0 on, between the sinks and the first row's window
     __device__ __forceinline__ bool hidden(const AttnParams &p, int k0, int &a, int &b) const {
         a = p.sinks > k0 ? p.sinks - k0 : 0;
@@ -154,12 +152,15 @@ __device__ __forceinline__ ItemGeomT<kDual, kWindow> item_geom(const AttnParams 
     g.pbase = it.part_base;
     g.cnt = it.group;
     if constexpr (kWindow) {
-        const int first = it.prefix + it.row_begin;
-        g.lo = first >= p.window ? first - p.window + 1 : 0;
-        g.sink_tiles = (p.sinks + kKeys - 1) / kKeys;
-        g.skip = g.lo / kKeys > g.sink_tiles ? g.lo / kKeys - g.sink_tiles : 0;
+        const int first = it.prefix + it.row_begin, bs = p.block_size;
+        const int lo = first >= p.window ? first - p.window + 1 : 0;
+        const int skip = (lo - ((p.sinks + bs - 1) & -bs)) / bs * bs;
+        g.skip = skip > 0 ? skip : 0;
+        g.lo = lo - g.skip;
+        g.prefix -= g.skip;
+        g.ctx -= g.skip;
     } else {
-        g.lo = g.sink_tiles = g.skip = 0;
+        g.lo = g.skip = 0;
     }
     // (dual items have no window; the plain forms here and at the block ids keep
     // their kernel's registers as they were: 76 bytes of spills, else 84)
@@ -361,11 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int nblk_seq = (it.ctx + bs - 1) / bs;
             // block ids of the next tile, one per lane, loaded a tile ahead so
             // that the TMA issue never waits on a block-table read
-            // (window: a hidden block is read from past the pool, as zeros)
-            auto block_at = [&](int j) -> int {
-                if (kWindow && j * bs >= p.sinks && (j + 1) * bs <= it.lo) return p.num_blocks;
-                return __ldg(bt + j);
-            };
+            auto block_at = [&](int j) -> int { return __ldg(bt + (kWindow && j * bs >= p.sinks ? j + it.skip / bs : j)); };
             const int b00 = it.tile(0) * per_tile;
             int blk_next = (lane < per_tile && b00 + lane < nblk_seq) ? block_at(b00 + lane) : 0;
             bool ok = true;
