@@ -220,6 +220,48 @@ struct Window {
     // the sinks up to a whole tile of `tile` keys
     int32_t sink_keys(int32_t tile) const { return (sinks + tile - 1) / tile * tile; }
 };
+// Keys a split for windowed decodes whose items are more than fit the device at once
+// (window_api.cu). add(split, f) calls f(items, keys) for all items of `split` keys, then
+// for the shorter ones with their mean.
+template <typename Add>
+int32_t window_heavy_split(int64_t key_bytes, int32_t slots, Add add) {
+    // The CTAs of a round start together and share 7 TB/s, one by itself takes 30 GB/s, and a
+    // round's start and end are 2 us. A last round with few CTAs is what costs most, and rows
+    // under a window all have its length. Over 30 steps of 64 to 300 rows the choice was 1.3% (10% at
+    // most) longer than the best of 192 to 1024 keys, where 256 always is 7.8% (23%), and 512 6.2%.
+    constexpr double kAll = 7.0e6, kOne = 30e3, kRound = 2.0;  // bytes a us; us
+    double least = 0.0;
+    int32_t best = 0;
+    for (int32_t split : {256, 320, 384, 448, 512, 768, 1024}) {
+        double t = 0.0, longest = 0.0, open = 0.0;  // of the round that fills: its longest item, bytes
+        int64_t in_round = 0;
+        auto close = [&](double rounds) {
+            const double all = open / kAll, one = in_round < slots ? longest / kOne : 0.0;
+            t += rounds * (kRound + (all > one ? all : one));
+            open = longest = 0.0;
+            in_round = 0;
+        };
+        add(split, [&](int64_t items, double keys) {
+            const double bytes = keys * static_cast<double>(key_bytes);
+            while (items > 0) {
+                const bool whole = in_round == 0 && items >= slots;
+                const int64_t n = whole ? slots : items < slots - in_round ? items : slots - in_round;
+                in_round += n;
+                open += static_cast<double>(n) * bytes;
+                if (bytes > longest) longest = bytes;
+                const int64_t rounds = whole ? items / slots : 1;
+                items -= whole ? rounds * slots : n;
+                if (in_round == slots) close(static_cast<double>(rounds));
+            }
+        });
+        if (in_round > 0) close(1.0);
+        if (best == 0 || t < least) {
+            least = t;
+            best = split;
+        }
+    }
+    return best;
+}
 constexpr int32_t kMostSinks = INT32_MAX - 1024;  // (more see as much: room to round up)
 constexpr int kDecodeStageKeys = 16;              // keys of a stage of the TMA decode kernel
 

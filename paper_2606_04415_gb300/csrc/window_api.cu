@@ -57,16 +57,24 @@ int window_split(const fnpu_attn_desc *d, int32_t window, int32_t sinks, int32_t
     int64_t sk = split_keys;
     constexpr int64_t kSms = 152;
     if (sk == 0) {
-        // the shortest whose items fit the device at once (three CTAs an SM); where none does, 256.
+        // the shortest whose items fit the device at once (three CTAs an SM); where none does, by
+        // a model if the bound lies well past the window (rows of one length then), else 256.
         // us a call, kv heads x rows, window: 4 x 4, 1024: 64 keys 11.1, 128 13.2; 4 x 64, 1024:
         // 128 keys 36.5, 192 29.8, 256 31.2; 8 x 16, 1024: 64 18.3, 128 14.9; 8 x 24, 4096: 256
-        // 71.1, 512 67.8; 4 x 64, 4096 (none fits): 256 99.5, 512 110.3
-        sk = 256;
+        // 71.1, 512 67.8; 4 x 64, 4096 (none fits): 256 101.9, 512 110.7, 768 87.3
+        sk = 0;
         for (int64_t k : {64, 128, 192, 256, 512})
             if (items(k) <= 3 * kSms) {
                 sk = k;
                 break;
             }
+        if (sk == 0 && max_context_len < 2 * keys) sk = 256;
+        if (sk == 0)
+            sk = window_heavy_split(static_cast<int64_t>(std::min(hpi, Hkv)) * D * 4, 3 * kSms, [&](int32_t split, auto f) {
+                const int64_t rows = static_cast<int64_t>(num_seqs) * hgroups, whole = keys / split, rest = keys % split;
+                f(rows * whole, split);
+                if (rest > 0) f(rows, static_cast<double>(rest));
+            });
     }
     sk = std::max<int64_t>(sk, (keys + 256 * 64 - 1) / (256 * 64) * 64);  // at most 256 splits of a sequence
     out->keys = static_cast<int32_t>(std::min<int64_t>(sk, 1 << 30));
