@@ -1067,24 +1067,21 @@ int plan_fill(fnpu_plan *pl, const fnpu_attn_desc *desc, int32_t num_seqs, const
                 if (decode_queue(s)) items += static_cast<int64_t>((decode_keys(s) + split - 1) / split) * hgroups;
             if (items > 3LL * sms && items < 6LL * sms) split = 320;
         }
-        if (windowed && pl->use_dt) {
-            // (rows under a window are of one length, so items of a mean's keys are more
-            // rounds than theirs: 128 of 4096 keys, 8 kv heads, 354 us with 506 items, 314 with 1524)
-            int64_t items = 0;
-            for (int32_t s = 0; s < num_seqs; ++s)
-                if (decode_queue(s)) items += static_cast<int64_t>((decode_keys(s) + split - 1) / split) * hgroups;
-            if (num_dec == num_seqs && items > 3LL * sms)
-                split = window_heavy_split(static_cast<int64_t>(std::min(hpi, desc->num_kv_heads)) * desc->head_dim_qk * 4, 3 * sms,
-                                           [&](int32_t sk, auto f) {
-                                               int64_t whole = 0, rests = 0, rest = 0;
-                                               for (int32_t s = 0; s < num_seqs; ++s) {
-                                                   whole += decode_keys(s) / sk;
-                                                   rests += decode_keys(s) % sk > 0;
-                                                   rest += decode_keys(s) % sk;
-                                               }
-                                               f(whole * hgroups, sk);
-                                               if (rests > 0) f(rests * hgroups, static_cast<double>(rest) / static_cast<double>(rests));
-                                           });
+        // (rows under a window are of one length, so items of a mean's keys are more rounds
+        // than theirs: 128 of 4096 keys, 8 kv heads, 354 us with 506 items, 313 with 2284)
+        if (windowed && pl->use_dt && split >= 256 && num_dec == num_seqs) {
+            split = window_heavy_split(static_cast<int64_t>(std::min(hpi, desc->num_kv_heads)) * desc->head_dim_qk * 4, 3 * sms,
+                                       [&](int32_t sk, auto f) {
+                int64_t whole = 0, rests = 0, rest = 0;
+                for (int32_t s = 0; s < num_seqs; ++s) {
+                    const int32_t keys = decode_keys(s), n = keys / sk, left = keys - n * sk;
+                    whole += n;
+                    rests += left > 0;
+                    rest += left;
+                }
+                f(whole * hgroups, sk);
+                if (rests > 0) f(rests * hgroups, static_cast<double>(rest) / static_cast<double>(rests));
+            });
         }
     }
 

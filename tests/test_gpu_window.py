@@ -134,6 +134,28 @@ def test_mixed(window, sinks):
         assert first.shape == st.out.shape
 
 
+@pytest.mark.parametrize("flags,share", [(1, 0), (4, 0), (4, 40), (0, 10)])
+def test_mixed_in_every_way_of_running(flags, share):
+    """Both phases in launches of their own, in green contexts, and with a share that is asked for."""
+    import paper_2606_04415_gb300 as fnpu
+    st = Step((16, 8, 64), 32, [(90, 700, 0), (33, 33, 0), (200, 201, 0)] + [(1, c, 1) for c in (1, 40, 300, 777, 2000)], 130, 20, seed=flags + share)
+    st.run(st.plan(fnpu.PlanOpts(0, share, 0, flags)))
+    st.check()
+
+
+@pytest.mark.parametrize("n,ctx,window", [(120, 900, 800), (300, 700, 400)])
+def test_more_rows_than_fit_at_once(n, ctx, window):
+    """Items of more than a round, planned and not, lengths that vary past the window."""
+    rng = np.random.default_rng([53, n])
+    st = Step((8, 8, 64), 16, [(1, int(c), 1) for c in rng.integers(ctx, 3 * ctx, n)], window, 5, seed=n)
+    st.run(st.plan())
+    some = list(range(0, n, 17))
+    st.check(some)
+    st.out.fill_(7.0), st.lse.fill_(7.0)
+    _decode(st, *st.device(), int(st.ctx.max()), st.workspace())
+    st.check(some)
+
+
 @pytest.mark.parametrize("split", [16, 64, 1000])
 @pytest.mark.parametrize("window,sinks", [(300, 20), (64, 0)])
 def test_decode_splits(split, window, sinks):
