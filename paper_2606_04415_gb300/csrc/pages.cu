@@ -513,8 +513,10 @@ __global__ void __launch_bounds__(kScanThreads) compact_small_kernel(const Pages
 
 // Copies of blocks in every pool. A unit is one pool's part of a pair, up to 16 KB; the
 // units of all pairs go round the CTAs, a warp's lanes looking at 32 of a CTA's at
-// once, as most pairs of a fork's list are none.
-constexpr int kCopyThreads = 256, kCopyLoads = 4;
+// once, as most pairs of a fork's list are none. Many CTAs, each of a unit or two: which
+// of them take long is left to the hardware (1.33 GB read and written: with 8 CTAs of 256 threads
+// an SM 213 us, with up to 256 of 128 threads, 8 loads in flight each, 191: 7.0 TB/s).
+constexpr int kCopyThreads = 128, kCopyLoads = 8;
 constexpr int64_t kCopyPart = 16 * kCopyThreads * kCopyLoads;
 __global__ void __launch_bounds__(kCopyThreads) copy_blocks_kernel(const __grid_constant__ CopyArgs a) {
     pdl_trigger();
@@ -600,7 +602,7 @@ int launch_copy_blocks(const CopyArgs &a, void *stream) {
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return FNPU_ECUDA;
     const int64_t units = static_cast<int64_t>(a.num_copies) * a.pools * ((a.block_bytes + kCopyPart - 1) / kCopyPart);
-    const int64_t grid = units < 8ll * sms ? units : 8ll * sms;
+    const int64_t grid = units < 256ll * sms ? units : 256ll * sms;
     FNPU_CUDA_TRY(launch_ex(copy_blocks_kernel, static_cast<unsigned>(grid), kCopyThreads, 0, static_cast<cudaStream_t>(stream), true,
                             nullptr, a));
     return FNPU_OK;
