@@ -644,26 +644,26 @@ def window_decode(desc: AttnDesc, window: int, sinks: int, context_len, block_ta
     """One token a sequence under a window and sinks, with lengths and block table
     on the device (``fnpu_window_decode``); ``workspace``: a byte tensor of
     ``window_decode_workspace`` bytes, not shared by calls that may overlap."""
-    n = context_len.shape[0]
     bf16, _, fp32, _, _ = _dtypes or _types()
     hq, _, d, _, pools = _layout(bytes(desc), KV_BF16)
-    cp, bp = _int32(context_len, "context_len", None), _int32(block_table, "block_table", n, None)
-    for x in (q, out):
-        if x.dtype is not bf16 or x.shape != (n, hq, d):
-            raise ValueError("q and out are bf16 [rows, Hq, d]")
+    n, width = block_table.shape
+    shape = (n, hq, d)
+    if q.dtype is not bf16 or out.dtype is not bf16 or q.shape != shape or out.shape != shape:
+        raise ValueError("q and out are bf16 [rows, Hq, d]")
     if lse.dtype is not fp32 or lse.shape != (n, hq):
         raise ValueError("lse is fp32 [rows, Hq]")
     kp, vp = _pool_addresses(pools, k_cache, v_cache)
-    rc = (_lib or load()).fnpu_window_decode(ctypes.byref(desc), int(window), int(sinks), n, cp, bp, block_table.shape[1],
-                                             int(max_context_len), int(split_keys), _tptr(q), kp, vp, _tptr(out), _tptr(lse),
-                                             *_workspace(workspace), _stream(stream))
+    rc = (_lib or load()).fnpu_window_decode(ctypes.byref(desc), int(window), int(sinks), n, _int32(context_len, "context_len", n),
+                                             _int32(block_table, "block_table", n, width), width, int(max_context_len),
+                                             int(split_keys), _tptr(q), kp, vp, _tptr(out), _tptr(lse), *_workspace(workspace),
+                                             _stream(stream))
     if rc != FNPU_OK:
         raise FnpuError(rc, "fnpu_window_decode")
 
 
 def _workspace(x):
     """(address, bytes) of a workspace tensor or None."""
-    return (None, 0) if x is None else (_tptr(x), x.numel() * x.element_size())
+    return (None, 0) if x is None else (_tptr(x), x.nbytes)
 
 
 def beam_select_workspace(groups: int, beams: int, vocab: int, select: int, fp32: bool = True) -> int:
@@ -696,11 +696,14 @@ def beam_select(logits, scores, out_scores, out_parents, out_tokens, workspace, 
     if (sv != 1 and v > 1) or (g > 1 and sg != b * sb):
         raise ValueError("rows of logits are contiguous and equally far apart")
     k = out_scores.shape[-1]
-    for x, name, dtype, shape in ((scores, "scores", fp32, (g, b)), (out_scores, "out_scores", fp32, (g, k)),
-                                  (out_parents, "out_parents", int32, (g, k)), (out_tokens, "out_tokens", int32, (g, k)),
-                                  (finished, "finished", uint8, (g, b))):
-        if x is not None and (x.dtype is not dtype or x.shape != shape):
-            raise ValueError(f"{name} is {dtype} of shape {shape}")
+    beams, chosen = (g, b), (g, k)
+    if scores.dtype is not fp32 or scores.shape != beams:
+        raise ValueError("scores are fp32 [groups, beams]")
+    if finished is not None and (finished.dtype is not uint8 or finished.shape != beams):
+        raise ValueError("finished is uint8 [groups, beams]")
+    if (out_scores.dtype is not fp32 or out_parents.dtype is not int32 or out_tokens.dtype is not int32 or
+            out_scores.shape != chosen or out_parents.shape != chosen or out_tokens.shape != chosen):
+        raise ValueError("the outputs are fp32, int32 and int32 [groups, select]")
     d = BeamDesc(g, b, v, k, 0 if logits.dtype is bf16 else 1, int(end_token))
     rc = (_lib or load()).fnpu_beam_select(ctypes.byref(d), logits.data_ptr(), sb, _tptr(scores), _dptr(finished), _tptr(out_scores),
                                            _tptr(out_parents), _tptr(out_tokens), *_workspace(workspace), _stream(stream))

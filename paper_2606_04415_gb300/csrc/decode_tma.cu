@@ -713,8 +713,10 @@ int launch_dt(const AttnParams &p, cudaStream_t st, int grid, bool after_prev) {
     if (!encode_slot_major_map(&maps.k, p.k_cache, D, p.num_kv_heads, p.block_size, p.num_blocks) ||
         !encode_slot_major_map(&maps.v, p.v_cache, D, p.num_kv_heads, p.block_size, p.num_blocks))
         return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled (decode)");
-    const int rc = prepare_dt<D, kRagged, kStages, kNoPlan, kFineP, kWindow>();
-    if (rc != FNPU_OK) return rc;
+    if constexpr (!kNoPlan) {  // (calls without a plan have prepared all of theirs, once a device)
+        const int rc = prepare_dt<D, kRagged, kStages, kNoPlan, kFineP, kWindow>();
+        if (rc != FNPU_OK) return rc;
+    }
     FNPU_CUDA_TRY(launch_ex(kernel, grid, kThreads, Cfg::kSmemBytes, st, after_prev, nullptr, p, maps));
     return FNPU_OK;
 }
