@@ -244,6 +244,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
     const uint4 none = make_uint4(P::kNone, P::kNone, P::kNone, P::kNone);
     auto load = [&](int c) { return c < c1 ? row.chunk(c) : none; };
 
+    uint64_t *keys = a.keys + static_cast<int64_t>(blockIdx.x) * K;
     typename P::Max seen = P::none();  // maxima of the thread's two subsets
     float ref = -INFINITY, c = 0.f;    // the sums' reference, and ref log2(e) as fp32 has it
     uint64_t z = f2_pack(0.f, 0.f);    // (a group's values are added up first: rounding errors grow with the groups alone)
@@ -332,6 +333,21 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
     if (tid == 0) a.parts[blockIdx.x] = part;
     __syncthreads();
     const float bound = s_bound;
+    auto note = [&](uint64_t key) {
+        if (key_value(key) < bound) return;
+        const int n = atomicAdd(&s_count, 1);
+        if (n < kList) u.few.list[n] = key;
+    };
+    auto rank = [&](int n) {
+        for (int i = tid; i < n; i += kThreads) {
+            const uint64_t key = u.few.list[i];
+            int better = 0;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) better += u.few.list[j] > key;
+            if (better < K) keys[better] = key;
+        }
+        for (int i = n + tid; i < K; i += kThreads) keys[i] = 0ull;
+    };
     uint32_t reach = 0u;  // the thread's runs of tiles that reach the bound
     for (int i = 0; i * run < tiles; ++i) reach |= (u.tops[i][tid] >= bound ? 1u : 0u) << i;
     __syncthreads();
@@ -342,30 +358,14 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
     }
     __syncthreads();
     const int hits = s_hits;
-    uint64_t *keys = a.keys + static_cast<int64_t>(blockIdx.x) * K;
     if (hits <= kHits) {
         const int loads = run * kLoads;  // of a hit
         for (int i = tid; i < hits * loads; i += kThreads) {
             const int hit = u.few.hits[i / loads], at = c0 + (hit / kThreads * loads + i % loads) * kThreads + hit % kThreads;
-            if (at < c1)
-                row.keys(at, [&](uint64_t key) {
-                    if (key_value(key) < bound) return;
-                    const int n = atomicAdd(&s_count, 1);
-                    if (n < kList) u.few.list[n] = key;
-                });
+            if (at < c1) row.keys(at, note);
         }
         __syncthreads();
-        const int n = s_count;
-        if (n <= kList) {
-            for (int i = tid; i < n; i += kThreads) {
-                const uint64_t key = u.few.list[i];
-                int rank = 0;
-                for (int j = 0; j < n; ++j) rank += u.few.list[j] > key;
-                if (rank < K) keys[rank] = key;
-            }
-            for (int i = n + tid; i < K; i += kThreads) keys[i] = 0ull;
-            return;
-        }
+        if (s_count <= kList) return rank(s_count);
     }
     // Many values reach the bound (equals of it, or large values in few subsets): the
     // slice again, a chunk a thread, whose candidates are cut to the best K each time.
@@ -433,7 +433,7 @@ __device__ Two two_log(float z) {
     const int bits = __float_as_int(z), e = (bits - __float_as_int(0.70710678f)) >> 23;
     const float f = __int_as_float(bits - (e << 23)), n = f - 1.f;  // (exact: f is 0.7 .. 1.42)
     const Two d = two_sum(f, 1.f);
-    const float q = n / d.hi, q1 = (fmaf(-q, d.hi, n) - q * d.lo) / d.hi, s = q * q;
+    const float q = __fdividef(n, d.hi), q1 = __fdividef(fmaf(-q, d.hi, n) - q * d.lo, d.hi), s = q * q;  // (q1 takes q's error out)
     const float p = s * fmaf(s, fmaf(s, fmaf(s, fmaf(s, 1.f / 11, 1.f / 9), 1.f / 7), 1.f / 5), 1.f / 3);
     constexpr float kHi = 45426.f / 65536.f;  // (16 bits of ln 2: e kHi is exact)
     constexpr float kLo = static_cast<float>(0.69314718055994530942 - 45426.0 / 65536.0);
@@ -520,6 +520,39 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
         if (a.finished == nullptr || a.finished[row] == 0 || a.end_token < 0 || !(s > -INFINITY)) return no_cand();
         return Cand{order_bits2(two_norm(s, 0.f)), static_cast<int64_t>(w) << 32 | a.end_token};
     };
+    auto put = [&](int r, const Cand &c) {
+        const int64_t o = static_cast<int64_t>(g) * K + r;
+        const bool none = c.total == 0ull;
+        a.out_scores[o] = none ? -INFINITY : from_order(static_cast<uint32_t>(c.total >> 32));
+        a.out_parents[o] = none ? -1 : g * W + static_cast<int>(c.tie >> 32);
+        a.out_tokens[o] = none ? -1 : static_cast<int32_t>(c.tie);
+    };
+    if (W * S * K <= kMergeThreads / 4) {
+        // few: all are ranked, four threads each (4 rows of 4000, 16 chosen: 8.6 us with the bound
+        // below, 7.7 so; with 128 candidates, two threads each, it takes 0.9 us longer)
+        Cand c = no_cand();
+        if (tid < W * S * K) {
+            const int w = tid / (S * K);
+            if (s_open[w]) {
+                if (key0 != 0ull) c = cand(w, key0);
+            } else if (tid == w * S * K) {
+                c = end_of(w);
+            }
+            s_list[tid] = c;
+        }
+        const int n = __syncthreads_count(c.total != 0ull);
+        int r = 0;
+        c = tid / 4 < W * S * K ? s_list[tid / 4] : no_cand();
+        if (c.total != 0ull) {
+#pragma unroll 4
+            for (int i = tid % 4; i < W * S * K; i += 4) r += better(s_list[i], c);
+        }
+        r += __shfl_xor_sync(0xffffffffu, r, 1);
+        r += __shfl_xor_sync(0xffffffffu, r, 2);
+        if (tid % 4 == 0 && c.total != 0ull && r < K) put(r, c);
+        for (int i = n + tid; i < K; i += kMergeThreads) put(i, no_cand());
+        return;
+    }
     // the K-th best of the subsets' bests (threads t and t + kMergeSubsets; by the first of the
     // two floats), which K candidates reach: the least of those that fewer than K are above
     uint32_t best = 0u;
@@ -565,17 +598,11 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
     visit(take);
     __syncthreads();
     const int n = s_count;
-    auto put = [&](int r, const Cand &c) {
-        const int64_t o = static_cast<int64_t>(g) * K + r;
-        const bool none = c.total == 0ull;
-        a.out_scores[o] = none ? -INFINITY : from_order(static_cast<uint32_t>(c.total >> 32));
-        a.out_parents[o] = none ? -1 : g * W + static_cast<int>(c.tie >> 32);
-        a.out_tokens[o] = none ? -1 : static_cast<int32_t>(c.tie);
-    };
     if (n <= kList) {
         for (int i = tid; i < n; i += kMergeThreads) {
             const Cand c = s_list[i];
             int r = 0;
+#pragma unroll 4
             for (int j = 0; j < n; ++j) r += better(s_list[j], c);
             if (r < K) put(r, c);
         }
@@ -607,7 +634,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const BeamArg
 }  // namespace
 
 // Slices a row: what the SMs hold at once (4 CTAs each), but no more than balances a
-// slice's time with what each adds to the merge (s slices of n / s chunks: s^2 = n / 192).
+// slice's time with what each adds to the merge (s slices of n / s chunks: s^2 = n / 185).
 // us a call, rows x vocabulary in bf16: 152 x 151936 19.6 with 4, 20.6 with 3, 23.4 with 6;
 // 512 x 151936 35.6 with 1, 40.1 with 2; 4 x 151936 10.7 with 8, 11.4 with 4, 17.2 with 1;
 // 8 x 32000 9.9 with 4, 10.6 with 1, 12.4 with 16.
@@ -615,7 +642,7 @@ int beam_slices(const fnpu_beam_desc *d) {
     const int64_t rows = static_cast<int64_t>(d->num_groups) * d->num_beams;
     const int64_t chunks = d->dtype == FNPU_LOGITS_FP32 ? (static_cast<int64_t>(d->vocab) + 3) / 4 : (static_cast<int64_t>(d->vocab) + 7) / 8;
     int64_t s = 1;
-    while ((s + 1) * rows <= 4 * 152 && (s + 1) * (s + 1) * 192 <= chunks) ++s;
+    while ((s + 1) * rows <= 4 * 152 && (s + 1) * (s + 1) * 185 <= chunks) ++s;
     return static_cast<int>(s);
 }
 
