@@ -600,9 +600,33 @@ __global__ void __launch_bounds__(32 * kMergeWarps) split_merge_kernel(const Att
     pdl_trigger();  // (the next step's append may be placed; it waits for this grid to finish)
     pdl_wait();     // the partial results of the grid before
     if (wg >= p.num_mgroups * Hq) return;
+    const int h = wg % Hq;
     MergeGroup mg;
     if constexpr (kNoPlan) {
         mg.token = wg / Hq;
+        mg.part_base = mg.token * p.na_max_splits;
+        mg.num_splits = p.na_max_splits;  // (as many at most: there is scratch for all)
+    } else {
+        mg = p.mgroups[wg / Hq];
+    }
+    // the first log-sum-exps and rows together, and without a plan before the length
+    // is there: one memory round trip for what depends on nothing but the place
+    const int base = mg.part_base;
+    auto lse_of = [&](int split) { return __ldcg(p.part_lse + static_cast<int64_t>(base + split) * Hq + h); };
+    // lanes past the row (D = 64) read a duplicate column and drop it
+    const float4 *po = reinterpret_cast<const float4 *>(p.part_o) + (static_cast<int64_t>(base) * Hq + h) * kV + (lane & (kV < 32 ? kV - 1 : 31));
+    float4 v[kB][kC];
+    auto fetch = [&](int split, int n) {
+#pragma unroll
+        for (int u = 0; u < kB; ++u)
+            if (u < n) {
+#pragma unroll
+                for (int c = 0; c < kC; ++c) v[u][c] = __ldcg(po + static_cast<int64_t>(split + u) * Hq * kV + 32 * c);
+            }
+    };
+    float my = lane < mg.num_splits ? lse_of(lane) : -INFINITY;
+    fetch(0, mg.num_splits);
+    if constexpr (kNoPlan) {
         int ctx = p.na_ctx[mg.token];
         if (ctx > p.na_max_ctx) return;  // out of range: skipped
         if constexpr (kWindow) {
@@ -611,20 +635,16 @@ __global__ void __launch_bounds__(32 * kMergeWarps) split_merge_kernel(const Att
         }
         if (ctx <= p.na_split) return;  // one split: already written
         mg.num_splits = (ctx + p.na_split - 1) / p.na_split;
-        mg.part_base = mg.token * p.na_max_splits;
-    } else {
-        mg = p.mgroups[wg / Hq];
     }
-    const int h = wg % Hq;
-    const int ns = mg.num_splits, base = mg.part_base;
-    const float4 *po = reinterpret_cast<const float4 *>(p.part_o);
+    const int ns = mg.num_splits;
     float M = -INFINITY, L = 0.f;
     float4 acc[kC];
 #pragma unroll
     for (int c = 0; c < kC; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int c0 = 0; c0 < ns; c0 += 32) {
         const int nc = ns - c0 < 32 ? ns - c0 : 32;
-        const float my = lane < nc ? __ldcg(p.part_lse + static_cast<int64_t>(base + c0 + lane) * Hq + h) : -INFINITY;
+        if (c0 > 0) my = lane < nc ? lse_of(c0 + lane) : -INFINITY;
+        if (lane >= nc) my = -INFINITY;
         float cm = my;
 #pragma unroll
         for (int o2 = 16; o2 > 0; o2 >>= 1) cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, o2));
@@ -640,16 +660,8 @@ __global__ void __launch_bounds__(32 * kMergeWarps) split_merge_kernel(const Att
             acc[c].x *= a; acc[c].y *= a; acc[c].z *= a; acc[c].w *= a;
         }
         M = Mn;
-        // lanes past the row (D = 64) read a duplicate column and drop it
-        const float4 *row = po + (static_cast<int64_t>(base + c0) * Hq + h) * kV + (lane & (kV < 32 ? kV - 1 : 31));
         for (int j0 = 0; j0 < nc; j0 += kB) {
-            float4 v[kB][kC];
-#pragma unroll
-            for (int u = 0; u < kB; ++u)
-                if (j0 + u < nc) {
-#pragma unroll
-                    for (int c = 0; c < kC; ++c) v[u][c] = __ldcg(row + static_cast<int64_t>(j0 + u) * Hq * kV + 32 * c);
-                }
+            if (c0 + j0 > 0) fetch(c0 + j0, nc - j0);
 #pragma unroll
             for (int u = 0; u < kB; ++u) {
                 if (j0 + u < nc) {
