@@ -111,6 +111,7 @@ class BeamCache:
         pages_free(self.pages, self.table, self.length, self.refs, ends=rows)
 
     def compact(self) -> None:
-        """All live pages to the lowest ids; ``moved``: live blocks, blocks that moved."""
+        """All live pages to the lowest ids; ``moved``: live blocks, blocks that moved. After a
+        step's last layer: its ``slots`` and ``copies`` speak of the old places."""
         pages_compact(self.pages, self.table, self.length, self.refs, self.moves, self.remap, self.moved, self.page_space)
         kv_copy_blocks(self.desc, self.moves, self.k, self.v)
