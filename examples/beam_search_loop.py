@@ -87,21 +87,20 @@ def main(argv=None):
         cache.advance(row)
         logits.copy_(model(embed[tokens.view(-1).long().clamp(min=0)], cache.attend).view(G, W, a.vocab))
 
-    torch.cuda.synchronize()
-    t0 = time.perf_counter()
     for _ in range(2):
         step()
-    if a.eager:
-        for _ in range(a.tokens - 2):
-            step()
-    elif a.tokens > 2:
+    if a.tokens > 2 and not a.eager:
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             step()
             step()
-        torch.cuda.synchronize()
-        t0 = time.perf_counter()
-        for _ in range(a.tokens // 2 - 1):
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(a.tokens // 2 - 1):
+        if a.eager:
+            step()
+            step()
+        else:
             graph.replay()
     torch.cuda.synchronize()
     spent = time.perf_counter() - t0
@@ -115,7 +114,7 @@ def main(argv=None):
         row = parents[t].reshape(-1)[row]
     free, _, unserved, _ = cache.stats.tolist()
     print("%d requests x %d beams, %d tokens: %.1f us a step of %d layers; %d of %d blocks free, %d rows without one" % (
-        G, W, a.tokens, spent / max(1, a.tokens - (0 if a.eager else 2)) * 1e6, a.layers, free, blocks, unserved))
+        G, W, a.tokens, spent / max(1, a.tokens - 2) * 1e6, a.layers, free, blocks, unserved))
     return {"text": text, "scores": scores.cpu().numpy(), "cache": cache, "unserved": unserved}
 
 
