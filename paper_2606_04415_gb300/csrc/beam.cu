@@ -319,17 +319,23 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const BeamArgs 
         x = kth_of_64<kBits>(x, y, K);
         if (lane == 0) s_bound = fmaxf(clean(from_order(max(x, order_bits(-INFINITY)))), -FLT_MAX);
     }
-    // the slice's sum over 2^c, c = max log2(e) rounded, then over e^max: the rounding of c is taken out
+    // The slice's sum over 2^c, c = max log2(e) rounded, then over e^max: the rounding of c, d = max
+    // log2(e) - c (exact), is taken out as 2^-d = 1 + expm1(-d ln 2), which costs an ordinary row, whose
+    // d is next to nothing, no accuracy. From maxima of 1.5 10^6 on d may be 1/8 and more (0.5 at
+    // 10^7): the rounding of d ln 2 would count, and such slices are summed again.
     float m = s_ref[0], sum = 0.f;
 #pragma unroll
     for (int i = 1; i < kWarps; ++i) m = fmaxf(m, s_ref[i]);
     c = __fmul_rn(m, kLog2e);
     for (int i = 0; i < kWarps; ++i)
         if (s_ref[i] > -INFINITY) sum += s_sum[i] * fast_exp2(__fmul_rn(s_ref[i], kLog2e) - c);
-    sum -= sum * fmaf(m, kLog2e, -c) * kLn2;
+    const float d = fmaf(m, kLog2e, -c);
+    sum = fmaf(sum, expm1f(-d * kLn2), sum);
     float2 part = make_float2(m, sum);
-    // (NaN or an infinity among them, or a maximum whose product with log2(e) overflows; else the maximum gives 1)
-    if (m > -INFINITY && !(sum > 0.5f && sum < INFINITY)) part = clean_sum(row.src, c0 * kV, min(a.vocab, c1 * kV), s_part);
+    // (and those with NaN or an infinity among them, or a maximum whose product with log2(e) overflows;
+    // of others the reference, which some value was, gives 1)
+    if (m > -INFINITY && !(fabsf(d) < 0.125f && sum > 0.5f && sum < INFINITY))
+        part = clean_sum(row.src, c0 * kV, min(a.vocab, c1 * kV), s_part);
     if (tid == 0) a.parts[blockIdx.x] = part;
     __syncthreads();
     const float bound = s_bound;
