@@ -51,9 +51,10 @@ __device__ __forceinline__ uint32_t order_bits(float x) {
 __device__ __forceinline__ float from_order(uint32_t o) {
     return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
-// A candidate of a row: larger is better, ties to the lower token; 0 is none.
+// A candidate of a row: larger is better, ties to the lower token; 0 is none. (x + 0
+// makes a negative zero a positive one: they are equal, and their bits are not.)
 __device__ __forceinline__ uint64_t row_key(float x, int token) {
-    return (static_cast<uint64_t>(order_bits(x)) << 32) | (0xFFFFFFFFu - static_cast<uint32_t>(token));
+    return (static_cast<uint64_t>(order_bits(x + 0.f)) << 32) | (0xFFFFFFFFu - static_cast<uint32_t>(token));
 }
 __device__ __forceinline__ float key_value(uint64_t key) { return from_order(static_cast<uint32_t>(key >> 32)); }
 __device__ __forceinline__ uint64_t warp_max(uint64_t k) {

@@ -1,5 +1,5 @@
-"""Beam selection over logits of every size and sign against the fp64 reference: parents
-and tokens equal, scores within fp32.
+"""Beam selection over logits of every size and sign, zeros of both signs among them,
+against the fp64 reference: parents and tokens equal, scores within fp32.
 
 A row's total is exact where one logit leaves nothing of the others (the logarithm of
 1), and its sum of exponentials is good to 2^-20 otherwise, as for ordinary logits:
@@ -79,3 +79,30 @@ def test_every_size_beside_every_other(dtype):
     order = list(range(len(rows)))[::-1]
     assert got[1][0].tolist() == order and got[2][0].tolist() == [61 * b for b in order]
     assert np.abs(got[0][0] - s[0].numpy()[order]).max() <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("k", [1, 2, 16, 64])
+@pytest.mark.parametrize("v", [40, 3001, 200000])
+def test_zeros_of_both_signs_are_equal(v, k, dtype):
+    """Ties at zero go to the lowest token, and beams whose zeros have other signs tie."""
+    rng = np.random.default_rng([67, v, k])
+    x = np.full((3, 4, v), -1.0, np.float32)
+    at = np.sort(rng.permutation(v)[:min(v, 2 * k)])
+    x[:, :, at] = np.where(rng.random((3, 4, len(at))) < 0.5, np.float32(-0.0), np.float32(0.0))
+    x[0, 0, at], x[0, 0, at[-1]] = -0.0, 0.0     # the one that bits would put first stands last
+    x[2, :, at[0]] = 2.5                         # zeros below the largest
+    s = torch.tensor([[-1.5, -1.5, -1.5, -1.5], [-0.0, 0.0, -0.0, 0.0], [0.0, -0.0, 0.0, 0.0]])
+    from oracle import pages as P
+    t = torch.from_numpy(x).to(dtype)
+    got, ref = _run(t, s, k), P.beam_select(x, s.numpy(), None, k, -1)
+    assert np.array_equal(got[1], ref[1]) and np.array_equal(got[2], ref[2])
+    assert (np.abs(got[0] - ref[0]) <= np.abs(ref[0]) * 2.0 ** -24 + 2.0 ** -20).all()
+    assert not np.signbit(got[0][got[0] == 0]).any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_lower_zero_is_kept(dtype):
+    x = torch.full((1, 1, 64), -1.0)
+    x[0, 0, 3], x[0, 0, 9] = -0.0, 0.0
+    assert _run(x.to(dtype), torch.zeros(1, 1), 1)[2].tolist() == [[3]]
