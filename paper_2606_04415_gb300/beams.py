@@ -18,16 +18,18 @@ from . import (Plan, kv_append, kv_copy_blocks, make_desc, make_pages, mixed_att
 
 
 class BeamCache:
-    """``rows`` sequences of up to ``max_length`` tokens each over ``layers`` bf16
-    caches; ``window`` (None: every query sees all earlier keys) and ``sinks`` as in
-    ``window_attn_plan``."""
+    """``rows`` sequences over ``layers`` bf16 caches, of prompts of up to ``max_length``
+    tokens, and of as many in all as whole blocks of ``max_length`` hold (``room``); ``window``
+    (None: every query sees all earlier keys) and ``sinks`` as in ``window_attn_plan``."""
 
     def __init__(self, num_q_heads: int, num_kv_heads: int, head_dim: int, block_size: int, num_blocks: int, layers: int, rows: int,
                  max_length: int, window: Optional[int] = None, sinks: int = 0, device: str = "cuda"):
         import torch
         self.torch = torch
         self.heads, self.block_size, self.rows, self.max_length = (num_q_heads, num_kv_heads, head_dim), block_size, rows, max_length
-        self.freed_window, self.window, self.sinks = window or 0, window or max(1, max_length), sinks
+        width = -(-max_length // block_size)
+        self.room = width * block_size  # what pages_fork lets a row grow to
+        self.freed_window, self.window, self.sinks = window or 0, window or max(1, self.room), sinks
         self.desc = make_desc(num_q_heads, num_kv_heads, head_dim, head_dim, block_size, num_blocks)
         self.pages = make_pages(block_size, num_blocks)
         shape = (num_blocks, block_size, num_kv_heads, head_dim)
@@ -36,13 +38,12 @@ class BeamCache:
         def state(*shape, fill=0):
             return torch.full(shape, fill, dtype=torch.int32, device=device)
 
-        width = -(-max_length // block_size)
         self.tables, self.lengths = [state(rows, width, fill=-1) for _ in range(2)], [state(rows) for _ in range(2)]
         self.refs, self.now = state(num_blocks), 0
         self.copies, self.stats, self.slots = state(rows, 2), state(4), torch.full((rows, 1), -1, dtype=torch.int64, device=device)
         self.moves, self.remap, self.moved = state(num_blocks // 2, 2), state(num_blocks), state(2)
         self.page_space = torch.empty(pages_workspace(self.pages, rows), dtype=torch.uint8, device=device)
-        need = window_decode_workspace(self.desc, self.window, sinks, rows, max_length)
+        need = window_decode_workspace(self.desc, self.window, sinks, rows, self.room)
         self.decode_space = torch.empty(need, dtype=torch.uint8, device=device)
 
     @property
@@ -88,7 +89,7 @@ class BeamCache:
     def advance(self, parents) -> None:
         """Row r continues row parents[r] (int32 [rows] on the device; negative: an empty
         row), with room for its next token. ``stats`` then tells how many blocks are free,
-        and how many rows found none (their slot is -1 and their length is as before)."""
+        and how many rows found none or are at ``room`` (their slot is -1 and their length is as before)."""
         if self.freed_window:
             pages_free(self.pages, self.table, self.length, self.refs, window=self.freed_window, sinks=self.sinks)
         then = 1 - self.now
@@ -102,7 +103,7 @@ class BeamCache:
         keys and values (bf16 [rows, Hkv, d]) are stored first. An empty row's are 0 and -inf."""
         kv_append(self.desc, k, v, self.slots.view(-1), self.k[layer], self.v[layer])
         out, lse = self.torch.empty_like(q), self.torch.empty(q.shape[:2], dtype=self.torch.float32, device=q.device)
-        window_decode(self.desc, self.window, self.sinks, self.length, self.table, self.max_length, q, self.k[layer], self.v[layer], out,
+        window_decode(self.desc, self.window, self.sinks, self.length, self.table, self.room, q, self.k[layer], self.v[layer], out,
                       lse, self.decode_space)
         return out, lse
 
