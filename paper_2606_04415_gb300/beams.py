@@ -29,7 +29,10 @@ class BeamCache:
         self.heads, self.block_size, self.rows, self.max_length = (num_q_heads, num_kv_heads, head_dim), block_size, rows, max_length
         width = -(-max_length // block_size)
         self.room = width * block_size  # what pages_fork lets a row grow to
-        self.freed_window, self.window, self.sinks = window or 0, window or max(1, self.room), sinks
+        self.window, self.sinks = window or max(1, self.room), sinks
+        # A row that finds no block is attended at its old length, whose window begins one key
+        # earlier than its next token's: the page of that key stays for one step more.
+        self.freed_window = min(window, 2 ** 31 - 2) + 1 if window else 0
         self.desc = make_desc(num_q_heads, num_kv_heads, head_dim, head_dim, block_size, num_blocks)
         self.pages = make_pages(block_size, num_blocks)
         shape = (num_blocks, block_size, num_kv_heads, head_dim)

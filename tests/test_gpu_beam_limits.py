@@ -25,7 +25,7 @@ def _load(name, *path):
     return m
 
 
-@pytest.mark.parametrize("window,sinks", [(None, 0), (21, 3)])
+@pytest.mark.parametrize("window,sinks", [(None, 0), (21, 3), (33, 0)])
 @pytest.mark.parametrize("heads,bs,most", [((4, 2, 64), 16, 40), ((28, 4, 128), 16, 33), ((8, 8, 64), 32, 64), ((4, 2, 64), 16, 15)])
 def test_rows_grow_to_their_last_block(heads, bs, most, window, sinks):
     """Every step that gives a row a slot gives it an output too, up to whole blocks of
