@@ -74,7 +74,7 @@ def main(argv=None):
     space = torch.empty(fnpu.beam_select_workspace(G, W, a.vocab, W), dtype=torch.uint8, device="cuda")
     chosen = [torch.empty((G, W), dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32)]
     history = torch.zeros((2, a.tokens, G, W), dtype=torch.int32, device="cuda")  # parents and tokens of every step
-    at = torch.zeros((), dtype=torch.long, device="cuda")
+    at, short = torch.zeros((), dtype=torch.long, device="cuda"), torch.zeros((), dtype=torch.int32, device="cuda")
 
     def step():
         fnpu.beam_select(logits, scores, *chosen, space, finished=finished, end_token=END)
@@ -85,6 +85,7 @@ def main(argv=None):
         scores.copy_(best)
         finished.copy_((finished.view(-1)[row.long().clamp(min=0)].view(G, W) > 0) | (tokens == END))
         cache.advance(row)
+        short.add_(cache.stats[2])                         # rows without a block: their tokens are not stored
         logits.copy_(model(embed[tokens.view(-1).long().clamp(min=0)], cache.attend).view(G, W, a.vocab))
 
     for _ in range(2):
@@ -112,8 +113,8 @@ def main(argv=None):
     for t in range(a.tokens - 1, -1, -1):
         text[:, :, t] = tokens[t].reshape(-1)[row]
         row = parents[t].reshape(-1)[row]
-    free, _, unserved, _ = cache.stats.tolist()
-    print("%d requests x %d beams, %d tokens: %.1f us a step of %d layers; %d of %d blocks free, %d rows without one" % (
+    free, unserved = cache.stats[0].item(), short.item()
+    print("%d requests x %d beams, %d tokens: %.1f us a step of %d layers; %d of %d blocks free, %d times a row found none" % (
         G, W, a.tokens, spent / max(1, a.tokens - 2) * 1e6, a.layers, free, blocks, unserved))
     return {"text": text, "scores": scores.cpu().numpy(), "cache": cache, "unserved": unserved}
 

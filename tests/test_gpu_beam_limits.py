@@ -1,7 +1,8 @@
-"""A beam search that runs into its cache's limits: the longest rows."""
+"""A beam search that runs into its cache's limits: the longest rows, and pools that run out."""
 import importlib.util
 import os
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -51,3 +52,32 @@ def test_rows_grow_to_their_last_block(heads, bs, most, window, sinks):
         assert torch.isfinite(s.out[layer].float()).all() and torch.isfinite(s.lse[layer]).all()
         for r in range(3):                         # over the keys that they have
             s.check_row(r, layer, s.q[layer][r:r + 1], s.out[layer][r:r + 1], s.lse[layer][r:r + 1], room - 1)
+
+
+def test_example_counts_the_rows_of_every_step(monkeypatch):
+    """Rows that found no block in an early step are told, though later steps serve all."""
+    import paper_2606_04415_gb300.beams as beams
+    seen = []
+
+    class Tight(beams.BeamCache):
+        """A pool in which the first steps find no blocks: something else holds them until then."""
+
+        def admit(self, lengths):
+            got = super().admit(lengths)
+            self.kept = self.refs.eq(0)
+            self.refs[self.kept] = 1
+            return got
+
+        def advance(self, parents):
+            if len(seen) == 3:
+                self.refs[self.kept] -= 1
+            super().advance(parents)
+            seen.append(self.stats.clone())
+
+    monkeypatch.setattr(beams, "BeamCache", Tight)
+    got = _load("beam_search_loop", "examples", "beam_search_loop.py").main(
+        ["--heads", "8", "2", "64", "--requests", "2", "--beams", "3", "--prompt", "32", "--tokens", "8", "--window", "40", "--vocab", "503", "--eager"])
+    each = [int(x[2]) for x in seen]
+    assert each[-1] == 0 and sum(each) > 0, each
+    assert got["unserved"] == sum(each)
+    assert np.isfinite(got["scores"]).all()
