@@ -1664,7 +1664,7 @@ int fnpu_window_attn_plan(const fnpu_attn_desc *desc, int32_t window, int32_t si
                           const fnpu_plan_opts *opts, void *stream, fnpu_plan **out) {
     if (window < 1 || sinks < 0) return FNPU_EINVAL;
     return plan_new(desc, FNPU_KV_BF16, num_seqs, query_len, context_len, phase, block_table, block_table_stride, opts, stream, out,
-                    Window{window, std::min(sinks, kMostSinks)});
+                    make_window(window, sinks));
 }
 
 int fnpu_mixed_attn_replan(fnpu_plan *pl, int32_t num_seqs, const int32_t *query_len, const int32_t *context_len,

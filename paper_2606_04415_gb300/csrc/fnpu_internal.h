@@ -220,6 +220,13 @@ struct Window {
     // the sinks up to a whole tile of `tile` keys
     int32_t sink_keys(int32_t tile) const { return (sinks + tile - 1) / tile * tile; }
 };
+// The window of a call. Larger windows and sinks see as much, no context being longer; the
+// room left is for rounding sinks up and for a tile's distances from its rows, which lie up
+// to a tile below zero (2^31 - 1 taken from those would not fit).
+constexpr int32_t kMostSeen = INT32_MAX - 1024;
+inline Window make_window(int32_t size, int32_t sinks) {
+    return Window{size < kMostSeen ? size : kMostSeen, sinks < kMostSeen ? sinks : kMostSeen};
+}
 // Keys a split for windowed decodes whose items are more than fit the device at once
 // (window_api.cu). add(split, f) calls f(items, keys) for all items of `split` keys, then
 // for the shorter ones with their mean.
@@ -262,7 +269,6 @@ int32_t window_heavy_split(int64_t key_bytes, int32_t slots, Add add) {
     }
     return best;
 }
-constexpr int32_t kMostSinks = INT32_MAX - 1024;  // (more see as much: room to round up)
 constexpr int kDecodeStageKeys = 16;              // keys of a stage of the TMA decode kernel
 
 // cuTensorMapEncodeTiled, looked up once through the runtime's driver entry

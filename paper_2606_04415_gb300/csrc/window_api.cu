@@ -49,7 +49,7 @@ int window_split(const fnpu_attn_desc *d, int32_t window, int32_t sinks, int32_t
     if (Hq <= 0 || Hkv <= 0 || Hq % Hkv || D <= 0 || d->head_dim_v <= 0 || d->block_size <= 0 || d->num_blocks <= 0) return FNPU_EINVAL;
     if ((d->kv_fp8 != 0 && d->kv_fp8 != 1) || split_keys < 0 || split_keys % 64 != 0) return FNPU_EINVAL;
     if (d->v_in_k_latent || d->kv_fp8 || !decode_tma_supported(D, d->head_dim_v, Hq / Hkv, d->block_size)) return FNPU_EUNSUPPORTED;
-    const Window w{window, std::min(sinks, kMostSinks)};
+    const Window w = make_window(window, sinks);
     const int64_t seen = static_cast<int64_t>(w.sink_keys(kDecodeStageKeys)) + window + kDecodeStageKeys - 1;
     const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(max_context_len, seen));
     const int32_t hpi = decode_tma_heads_per_item(), hgroups = (Hkv + hpi - 1) / hpi;
@@ -147,7 +147,7 @@ int fnpu_window_decode(const fnpu_attn_desc *desc, int32_t window, int32_t sinks
     a.na_max_splits = s.most;
     a.num_ditems = static_cast<int32_t>(s.items);
     a.num_mgroups = num_seqs;
-    const Window w{window, std::min(sinks, kMostSinks)};
+    const Window w = make_window(window, sinks);
     a.window = w.size;
     a.sinks = w.sinks;
     a.sink_keys = w.sink_keys(kDecodeStageKeys);
