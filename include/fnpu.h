@@ -682,7 +682,8 @@ int fnpu_pages_free(const fnpu_pages_desc *desc, int32_t *table, int32_t *length
  *   - it holds its parent's pages, shared;
  *   - where the parent's last page is partly filled (length % bs != 0) and grow >= 1,
  *     the row is about to write to it: if other holders are counted than new rows whose last
- *     page it is, each of those rows takes a copy, else all but the lowest of them do.
+ *     page it is, each of those rows takes a copy, else all but the lowest of them do
+ *     (fewer holders counted than such rows: that raises the error flag, and the page keeps its count).
  *     A copy is a new block in the row's table and a pair (held block, new block) in `copies`;
  *   - then new blocks up to ceil((length + grow) / bs) entries.
  * Rows take their blocks in order; one whose blocks are not all there (or that would

@@ -289,7 +289,7 @@ __device__ __forceinline__ void fork_take(const PagesArgs &a, int chunk, ForkSha
             a.refs[id] = 1;
             if (copies && k == 0) {
                 const int tail = a.row_tail[r];
-                atomicSub(a.refs + tail, 1);  // (another row or holder keeps it)
+                if (a.row_refs[r] >= a.block_a[tail]) atomicSub(a.refs + tail, 1);  // (another row or holder keeps it: 1 at least is left)
                 a.copies[2 * r] = tail;
                 a.copies[2 * r + 1] = id;
             }
@@ -304,6 +304,9 @@ __device__ __forceinline__ void fork_take(const PagesArgs &a, int chunk, ForkSha
     for (int r = tid; r < R; r += kScanThreads) {
         const int tail = a.row_tail[r], n = a.row_length[r];
         const bool copies = s_off[r] & 1, ok = tail >= kRowFull && served(r);
+        // (fewer holders counted than rows that have it last: its count would end at 0 or below, or pass
+        // there while other CTAs look for free blocks; it stays)
+        if (tail >= 0 && a.row_refs[r] < a.block_a[tail]) atomicOr(a.err, 1);
         a.new_length[r] = n + (ok ? a.grow : 0);
         if (!ok || !copies) a.copies[2 * r] = a.copies[2 * r + 1] = -1;
         if (!ok) {
