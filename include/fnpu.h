@@ -648,9 +648,9 @@ int fnpu_beam_select(const fnpu_beam_desc *desc, const void *logits, int64_t row
  *           A block with none is free. Free blocks are taken lowest id first, in
  *           the order of the rows, so every result is determined by its inputs.
  * One table covers all layers: every layer's pool has a block of each id.
- * Ids >= num_blocks, lengths outside [0, width * bs], parents >= rows and counts
- * that would fall below zero raise the library-wide error flag (FNPU_EDEVICE_RANGE from
- * fnpu_check) and are skipped; nothing is read or written out of bounds. Calls on
+ * Ids >= num_blocks, lengths outside [0, width * bs] and parents >= rows raise the
+ * library-wide error flag (FNPU_EDEVICE_RANGE from fnpu_check) and are skipped; a count
+ * that would fall below zero raises it and is zero then. Nothing is read or written out of bounds. Calls on
  * the same state must be ordered by the caller (one stream, or events). All device
  * pointers need the alignment of their type, workspaces 16 bytes; inputs and outputs
  * must not overlap but for what is said. rows <= 8192 (FNPU_EUNSUPPORTED).

@@ -120,12 +120,19 @@ __device__ __forceinline__ uint32_t live_bits(const PagesArgs &a, int id0) {
         if (id0 + i < a.num_blocks && a.refs[id0 + i] > 0) bits |= 1u << i;
     return bits;
 }
-// How many of a chunk's counts are above zero.
+// How many of a chunk's counts are above zero. kFix: those below it, of more holders
+// given up than were counted, are flagged and become 0.
+template <bool kFix>
 __device__ __forceinline__ int live_in_chunk(const PagesArgs &a, int chunk, int *s) {
     int n = 0;
     for (int i = 0; i < a.chunk; i += kScanThreads) {
         const int id = chunk * a.chunk + i + static_cast<int>(threadIdx.x);
-        n += id < a.num_blocks && a.refs[id] > 0;
+        const int count = id < a.num_blocks ? a.refs[id] : 0;
+        n += count > 0;
+        if (kFix && count < 0) {
+            a.refs[id] = 0;
+            atomicOr(a.err, 1);
+        }
     }
     return block_sum<kScanThreads>(n, s);
 }
@@ -143,7 +150,8 @@ __device__ __forceinline__ int live_before(const PagesArgs &a, int chunk, int *s
 
 // Fork, first step. Units 0 .. new_rows - 1: a new row's entries. The others: an old
 // row's pages get as many holders more as rows continue it, less the one that it was
-// (nothing to do where one row does, the usual case late in a search).
+// (nothing to do where one row does, the usual case late in a search). Sums alone: whether a count
+// is below zero shows when all are in, whatever their order.
 template <int kGroup>
 __device__ __forceinline__ void fork_row(const PagesArgs &a, int unit, int *s_sum) {
     constexpr int kLoads = 4;  // entries in flight
@@ -208,8 +216,7 @@ __device__ __forceinline__ void fork_row(const PagesArgs &a, int unit, int *s_su
         for (int i = 0; i < kLoads; ++i) {
             if (e[i] >= a.num_blocks) atomicOr(a.err, 1);
             if (e[i] < 0 || e[i] >= a.num_blocks || next == 1) continue;
-            if (next > 1) atomicAdd(a.refs + e[i], next - 1);
-            else drop(a, e[i]);
+            atomicAdd(a.refs + e[i], next - 1);
         }
     }
 }
@@ -220,7 +227,7 @@ __device__ __forceinline__ void fork_tail(const PagesArgs &a, int r) {
     if (tail < 0) return;
     atomicAdd(a.block_a + tail, 1);
     atomicMin(a.block_b + tail, r);
-    a.row_refs[r] = a.refs[tail];
+    a.row_refs[r] = max(0, a.refs[tail]);  // (one below zero may become 0 meanwhile)
 }
 
 // Third step, a chunk each CTA. All form the rows' needs and their prefix sums; a CTA
@@ -343,7 +350,7 @@ __global__ void __launch_bounds__(kScanThreads) fork_count_kernel(const PagesArg
     pdl_trigger();
     pdl_wait();
     if (static_cast<int>(blockIdx.x) < a.chunks) {
-        const int n = live_in_chunk(a, blockIdx.x, s_sum);
+        const int n = live_in_chunk<true>(a, blockIdx.x, s_sum);
         if (threadIdx.x == 0) a.chunk_count[blockIdx.x] = n;
         return;
     }
@@ -383,7 +390,7 @@ __global__ void __launch_bounds__(kScanThreads) fork_small_kernel(const PagesArg
     for (int u = threadIdx.x / 32; u < a.new_rows + a.rows; u += kScanThreads / 32) fork_row<32>(a, u, nullptr);
     __syncthreads();
     for (int r = threadIdx.x; r < a.new_rows; r += kScanThreads) fork_tail(a, r);
-    const int n = live_in_chunk(a, 0, s.sum);
+    const int n = live_in_chunk<true>(a, 0, s.sum);
     if (threadIdx.x == 0) a.chunk_count[0] = n;
     __syncthreads();
     fork_take(a, 0, &s, s_off);
@@ -481,7 +488,7 @@ __global__ void __launch_bounds__(kScanThreads) compact_count_kernel(const Pages
     __shared__ int s_sum[kScanThreads / 32];
     pdl_trigger();
     pdl_wait();
-    const int n = live_in_chunk(a, blockIdx.x, s_sum);
+    const int n = live_in_chunk<false>(a, blockIdx.x, s_sum);
     if (threadIdx.x == 0) a.chunk_count[blockIdx.x] = n;
 }
 __global__ void __launch_bounds__(kScanThreads) compact_rank_kernel(const PagesArgs a) {
@@ -504,7 +511,7 @@ __global__ void __launch_bounds__(kScanThreads) compact_small_kernel(const Pages
     const PagesArgs a = with_shared(args, &small);
     pdl_trigger();
     pdl_wait();
-    const int n = live_in_chunk(a, 0, s_sum);
+    const int n = live_in_chunk<false>(a, 0, s_sum);
     if (threadIdx.x == 0) a.chunk_count[0] = n;
     __syncthreads();
     compact_rank(a, 0, s_sum);

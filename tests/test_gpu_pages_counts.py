@@ -77,3 +77,29 @@ def test_a_last_page_that_nobody_counts():
     flag, got, rows, lens, slots, copies, stats = _fork(table, [20], refs, None, 1)
     assert flag == fnpu.FNPU_EDEVICE_RANGE and rows == table and slots == [[9 * BS + 4]] and copies == [[-1, -1]]
     assert got == refs.tolist() and lens == [21] and stats == [11, 0, 0, 0]
+
+
+@pytest.mark.parametrize("blocks,width", [(300, 100), (9000, 500)])
+@pytest.mark.parametrize("count", [0, 1, 2, 5])
+def test_holders_come_and_go_in_one_sum(blocks, width, count):
+    """Pages of two rows, one given up and the other continued by three, with too low counts
+    among them: the new count is the old one and one, whichever row's comes first; where the
+    sum is below zero it is flagged and the count is zero."""
+    import paper_2606_04415_gb300 as fnpu
+    pages = np.arange(1, width + 1)
+    refs = np.zeros(blocks, np.int32)
+    refs[pages] = count
+    for _ in range(10):
+        for rows in (2, 40):                                   # (the first two rows' pages; those of the others are their own)
+            table = np.full((rows, width), -1, np.int32)
+            table[:2] = pages
+            n = np.array([width * BS] * 2 + [0] * (rows - 2), np.int32)
+            flag, got, new, lens, _, _, stats = _fork(table, n, refs, [1, 1, 1], 0)
+            assert flag == 0 and np.array_equal(got, np.where(refs + np.isin(np.arange(blocks), pages) > 0, count + 1, 0))
+            assert new == [pages.tolist()] * 3 and lens == [width * BS] * 3
+            live = width if count + 1 > 0 else 0
+            assert stats == [blocks - live, 0, 0, 0]
+            flag, got, new, *_ = _fork(table, n, refs, [-1], 0)
+            assert flag == (fnpu.FNPU_EDEVICE_RANGE if count < 2 else 0)
+            assert np.array_equal(got, np.maximum(refs - 2 * np.isin(np.arange(blocks), pages), 0)) and new == [[-1] * width]
+    assert fnpu.check() == 0
