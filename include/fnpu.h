@@ -542,7 +542,10 @@ int fnpu_kv8_attn_plan(const fnpu_attn_desc *desc, int32_t kv_format, int32_t nu
  * over the visible keys; all else is as in fnpu_mixed_attn_plan_ex, whose
  * arguments these are, and the plan is run, re-planned (with the same window),
  * checked and destroyed like any other. window >= the longest context is causal
- * attention; any window >= 1 and sinks >= 0 will do.
+ * attention; any window >= 1 and sinks >= 0 will do. The windowed kernels run whatever the
+ * window hides: they lack the forms that fnpu_mixed_attn_plan has for several tokens a
+ * sequence and for decodes of one or two kv heads of 64, so where nothing is hidden that
+ * call is the faster one for the same result (by 3 to 14% there).
  * Only what some query of the step sees is read. A block of a sequence that lies
  * wholly between its sinks and the window of its first query in the step may be
  * gone: its block-table entry may hold anything (-1, another sequence's block),
@@ -578,7 +581,9 @@ int fnpu_window_attn_plan(const fnpu_attn_desc *desc, int32_t window, int32_t si
  * loaded (the sequence's result is then undefined); either raises the library-wide
  * error flag (FNPU_EDEVICE_RANGE from fnpu_check). The first call on a device
  * loads the kernels' code: make it before a stream capture.
- * Supports what fnpu_window_attn_plan does for one-token decodes.
+ * Supports what fnpu_window_attn_plan does for one-token decodes. (Probabilities enter
+ * their product as two bf16 here, and in a plan of four kv heads as one: results of the two
+ * differ by that rounding, 2^-8 of a weight at most.)
  * Errors: FNPU_EINVAL for bad arguments or a workspace that is too small,
  * FNPU_EUNSUPPORTED, FNPU_ECUDA. Nothing is launched on error.
  */
@@ -596,14 +601,15 @@ int fnpu_window_decode(const fnpu_attn_desc *desc, int32_t window, int32_t sinks
  * continuation (b, v) has the total
  *   scores[b] + (x_v - m) - ln sum_u exp(x_u - m),   m = max_u x_u,
  * and the num_select best of a group come out in order, ties to the lowest b, then
- * the lowest v (within a row the order is that of the logits). A beam whose
+ * the lowest v; a row's candidates are its num_select largest logits, ties to the lowest v
+ * (-0 equals 0). A beam whose
  * `finished` flag is set has one continuation, end_token at its own score (none
  * with end_token -1); a logit of -inf or NaN is no candidate, +inf counts as the
  * largest finite value, and a beam whose score is -inf or NaN has no continuation
  * (the idle beams of a first step). Where a group has fewer than num_select, the
  * rest come out with score -inf, parent -1 and token -1.
- * Exponentials are summed in fp32; logarithms, totals and their comparison have 48
- * bits (pairs of fp32). Rows are cut by token numbers, so beams of equal logits and
+ * Exponentials are summed in fp32, whatever the size of the logits; logarithms, totals and
+ * their comparison have 48 bits (pairs of fp32). Rows are cut by token numbers, so beams of equal logits and
  * scores tie exactly, wherever their rows start. Scores are finite, -inf or NaN.
  *   logits        device, row_stride values between rows (>= vocab; the start of a
  *                 row needs the alignment of its type only)
